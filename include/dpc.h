@@ -339,6 +339,123 @@ int dpc_fitting_fwd_bwd(void* stream, void* blas, int nloc, const dpc_fitting_ne
                         const double* D, void* workspace, size_t workspace_bytes, double* E,
                         double* dE_dD);
 
+/* ---- Routing: tokens sorted by expert and back --------------------------
+ * A model with one fitting net per species (or a mixture of nets) sends each
+ * atom's descriptor row to the nets it chooses and brings their results back.
+ * Token t of ntok has topk choices; slot s = t * topk + j holds expert[s].
+ * A slot whose expert is outside [0, nexpert) is dropped: it owns no row.
+ * nslot = ntok * topk rows are laid out; the first offsets[nexpert] of them
+ * are the kept slots sorted by expert (ties by slot), the rest is empty.   */
+
+/* Types of the elements of rows (the routing and 8-bit calls). */
+typedef enum { DPC_ELEM_F64 = 0, DPC_ELEM_F32 = 1, DPC_ELEM_F16 = 2, DPC_ELEM_BF16 = 3 } dpc_elem;
+
+#define DPC_MAX_EXPERTS 1024
+#define DPC_MAX_TOPK 64
+
+/* Bytes of device workspace dpc_route_plan needs; 0 for bad sizes. */
+size_t dpc_route_workspace_bytes(int ntok, int topk, int nexpert);
+
+/* The plan of a routing.
+ *   expert   device int32 [ntok][topk]
+ *   workspace  device, 16-byte aligned, >= dpc_route_workspace_bytes()
+ *   offsets  device out int32 [nexpert + 1]: first row of each expert, and
+ *            the number of kept rows
+ *   rows     device out int32 [nslot]: slot of each row, -1 for empty rows
+ *   pos      device out int32 [nslot]: row of each slot, -1 for dropped slots
+ * Requires 1 <= topk <= DPC_MAX_TOPK, 1 <= nexpert <= DPC_MAX_EXPERTS
+ * (DPC_ENOTSUP above) and nslot <= 2^30 (DPC_ENOTSUP).  The result is the same
+ * on every call.  With ntok = 0 only the offsets (zeros) are written.       */
+int dpc_route_plan(void* stream, int ntok, int topk, int nexpert, const int* expert, void* workspace,
+                   size_t workspace_bytes, int* offsets, int* rows, int* pos);
+
+/* Rows of the tokens in the plan's order, and their gradient's half:
+ *   y[r] = weight[s] * x[s / topk],  s = rows[r];  zeros where rows[r] is not
+ *   a slot.
+ *   x       device [ntok] rows of `width` elements, ldx elements apart
+ *   weight  device [ntok][topk] (float64 for DPC_ELEM_F64, else float32) or
+ *           NULL for weights of 1.  With weights, this maps the gradient of
+ *           dpc_route_combine's y to that of its x.
+ *   y       device out [nslot] rows, ldy elements apart
+ * Products are rounded once from float64 (DPC_ELEM_F64) or float32.  Rows
+ * need the alignment of their elements alone.  Requires width >= 1, ldx and
+ * ldy >= width.  Inputs and outputs must not overlap.                       */
+int dpc_route_gather(void* stream, dpc_elem elem, int ntok, int topk, int width, const void* x,
+                     int64_t ldx, const void* weight, const int* rows, void* y, int64_t ldy);
+
+/* Rows back to their tokens, with weights:
+ *   y[t] = sum over j with pos[t][j] a row, j ascending, of
+ *          weight[t][j] * x[pos[t][j]]
+ * (zeros where a token has no row; what weight[t][j] holds for a dropped slot
+ * does not matter).  Summed in float64 (DPC_ELEM_F64) or float32, rounded once.
+ *   x  device [nslot] rows, ldx elements apart;  y  device out [ntok] rows
+ * Without weights (NULL) this is the gradient of dpc_route_gather in x.
+ * Other arguments as dpc_route_gather.                                      */
+int dpc_route_combine(void* stream, dpc_elem elem, int ntok, int topk, int width, const void* x,
+                      int64_t ldx, const void* weight, const int* pos, void* y, int64_t ldy);
+
+/* Gradient of dpc_route_combine from dE/dy:
+ *   dx[pos[t][j]] = weight[t][j] * dy[t]         (zeros in empty rows)
+ *   dweight[t][j] = sum_c dy[t][c] * x[pos[t][j]][c]   (0 for a dropped slot)
+ * in one pass over dy and x.  dx or dweight may be NULL (that half is left
+ * out); x may be NULL when dweight is.
+ *   dweight  device out [ntok][topk], the type of weight
+ * The sum over c has a fixed order.  Other arguments as above.              */
+int dpc_route_combine_bwd(void* stream, dpc_elem elem, int ntok, int topk, int width, const void* x,
+                          int64_t ldx, const void* weight, const int* rows, const int* pos,
+                          const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dweight);
+
+/* ---- Layers in 8-bit integers -------------------------------------------
+ * y = x W^T + b with x and W held as 8-bit codes: every row of x (an atom) and
+ * every row of W (an output channel) has a scale of its own.  A matrix of
+ * codes is int8 [rows][DPC_I8_LD(cols)], the columns past `cols` zero.      */
+#define DPC_I8_LD(cols) (((cols) + 127) / 128 * 128)
+#define DPC_MAX_I8_COLS 131071 /* sums of that many products fit 32 bits */
+
+/* Codes of rows.  With x[r] rounded to float32 and a = max_c |x[r][c]|,
+ *   scale[r] = a / 127,  q[r][c] = x[r][c] * (127 / a) to the nearest integer
+ *   (ties to even), every operation rounded to float32 on its own.
+ * A row with a < 2^-100 gets scale 0 and codes 0; a row with an infinity or a
+ * NaN gets scale NaN and codes 0.
+ *   x      device [nrows] rows of `ncols` elements, ldx elements apart
+ *   q      device out int8 [nrows][DPC_I8_LD(ncols)], 16-byte aligned
+ *   scale  device out float32 [nrows]
+ * Requires 1 <= ncols <= DPC_MAX_I8_COLS (DPC_ENOTSUP above), ldx >= ncols.
+ * The weights of a layer are coded once: their rows are output channels.    */
+int dpc_quant_rows(void* stream, dpc_elem elem, int nrows, int ncols, const void* x, int64_t ldx,
+                   int8_t* q, float* scale);
+
+/* Product of codes, for one layer or for the layer of each row's expert:
+ *   y[r][c] = (sum_i qx[t][i] qw[g][c][i]) * sx[t] * sw[g][c] + bias[g][c]
+ * for the ntok * topk rows r, c < n.  The sum over i < k is exact; the rest is
+ * float64 arithmetic, rounded to float32 (and from there to 16 bits, if so).
+ *   rows     NULL: t = r (topk must be 1); else from dpc_route_plan:
+ *            t = rows[r] / topk
+ *   offsets  NULL: one group (ngroup must be 1); else device int32
+ *            [ngroup + 1], offsets[0] = 0: g is the group with
+ *            offsets[g] <= r < offsets[g + 1].  Rows past offsets[ngroup] and
+ *            rows that own no slot are zero.
+ *   qx, sx   device codes [ntok][DPC_I8_LD(k)] and scales [ntok]
+ *   qw, sw   device codes [ngroup][n][DPC_I8_LD(k)] and scales [ngroup][n]
+ *   bias     device float32 [ngroup][n] or NULL
+ *   y        device out [ntok * topk] rows of n elements, ldy apart
+ * qx and qw 16-byte aligned.  Requires n >= 1, 1 <= k <= DPC_MAX_I8_COLS,
+ * ngroup <= DPC_MAX_EXPERTS, topk <= DPC_MAX_TOPK (DPC_ENOTSUP above).
+ * The gradient of y in x is the same product with the codes of the transposed
+ * weights (their rows are input channels).                                  */
+int dpc_matmul_i8(void* stream, dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup,
+                  const int8_t* qx, const float* sx, const int* rows, const int* offsets,
+                  const int8_t* qw, const float* sw, const float* bias, void* y, int64_t ldy);
+
+/* dpc_quant_rows of x [ntok][k] and dpc_matmul_i8 in one call, with the same
+ * result.  The workspace (device, 16-byte aligned) may hold the codes and
+ * scales of x in between.  dpc_linear_i8_workspace_bytes is 0 for bad sizes. */
+size_t dpc_linear_i8_workspace_bytes(int ntok, int k);
+int dpc_linear_i8(void* stream, dpc_elem elem_x, dpc_elem elem_y, int ntok, int topk, int n, int k,
+                  int ngroup, const void* x, int64_t ldx, const int* rows, const int* offsets,
+                  const int8_t* qw, const float* sw, const float* bias, void* workspace,
+                  size_t workspace_bytes, void* y, int64_t ldy);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,11 +31,15 @@ DPC_OK, DPC_EINVAL, DPC_ERANGE, DPC_EHIP, DPC_ENOTSUP, DPC_EOVERFLOW = 0, -1, -2
 DPC_F64, DPC_F32, DPC_F32_ACC64 = 0, 1, 2
 DPC_MAX_TYPES, DPC_MAX_M1 = 8, 256
 DPC_NLIST_NOALLOC_MAX_ATOMS = 524288
+DPC_ELEM_F64, DPC_ELEM_F32, DPC_ELEM_F16, DPC_ELEM_BF16 = 0, 1, 2, 3
+DPC_MAX_EXPERTS, DPC_MAX_TOPK, DPC_MAX_I8_COLS = 1024, 64, 131071
 EXPORTED = ("dpc_strerror", "dpc_last_hip_error", "dpc_version", "dpc_table_layout", "dpc_build_table",
             "dpc_se_a_tab_fwd", "dpc_se_a_tab_bwd", "dpc_descriptor_bwd", "dpc_env_mat_a",
             "dpc_nlist_reverse", "dpc_force_a", "dpc_fitting_workspace_bytes", "dpc_fitting_fwd_bwd",
             "dpc_nlist_workspace_bytes", "dpc_nlist_build", "dpc_nlist_build_noalloc",
-            "dpc_se_a_tab_bwd_from_dD")
+            "dpc_se_a_tab_bwd_from_dD", "dpc_route_workspace_bytes", "dpc_route_plan", "dpc_route_gather",
+            "dpc_route_combine", "dpc_route_combine_bwd", "dpc_quant_rows", "dpc_matmul_i8",
+            "dpc_linear_i8_workspace_bytes", "dpc_linear_i8")
 
 
 class dpc_range(C.Structure):
@@ -104,6 +108,25 @@ _lib.dpc_nlist_build_noalloc.argtypes = [C.c_void_p, C.c_int, C.c_int, C.POINTER
 _lib.dpc_descriptor_bwd.restype = C.c_int
 _lib.dpc_descriptor_bwd.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p,
                                     C.c_void_p, C.c_void_p]
+_P, _I, _L, _Z = C.c_void_p, C.c_int, C.c_int64, C.c_size_t
+_lib.dpc_route_workspace_bytes.restype = _Z
+_lib.dpc_route_workspace_bytes.argtypes = [_I, _I, _I]
+_lib.dpc_route_plan.restype = _I
+_lib.dpc_route_plan.argtypes = [_P, _I, _I, _I, _P, _P, _Z, _P, _P, _P]
+_lib.dpc_route_gather.restype = _I
+_lib.dpc_route_gather.argtypes = [_P, _I, _I, _I, _I, _P, _L, _P, _P, _P, _L]
+_lib.dpc_route_combine.restype = _I
+_lib.dpc_route_combine.argtypes = [_P, _I, _I, _I, _I, _P, _L, _P, _P, _P, _L]
+_lib.dpc_route_combine_bwd.restype = _I
+_lib.dpc_route_combine_bwd.argtypes = [_P, _I, _I, _I, _I, _P, _L, _P, _P, _P, _P, _L, _P, _L, _P]
+_lib.dpc_quant_rows.restype = _I
+_lib.dpc_quant_rows.argtypes = [_P, _I, _I, _I, _P, _L, _P, _P]
+_lib.dpc_matmul_i8.restype = _I
+_lib.dpc_matmul_i8.argtypes = [_P, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _L]
+_lib.dpc_linear_i8_workspace_bytes.restype = _Z
+_lib.dpc_linear_i8_workspace_bytes.argtypes = [_I, _I]
+_lib.dpc_linear_i8.restype = _I
+_lib.dpc_linear_i8.argtypes = [_P, _I, _I, _I, _I, _I, _I, _I, _P, _L, _P, _P, _P, _P, _P, _P, _Z, _P, _L]
 
 
 class DpcError(RuntimeError):
@@ -414,6 +437,151 @@ def dpc_fitting_fwd_bwd(stream, blas, nloc, net, D, workspace, workspace_bytes, 
                                     _ptr(workspace, name="workspace"), int(workspace_bytes),
                                     _ptr(E, name="E"), _ptr(dE_dD, name="dE_dD")),
            "dpc_fitting_fwd_bwd")
+
+
+# ---- routing and 8-bit layers: rows of any element type, with a row stride ----
+def elem_of(dtype):
+    """The dpc_elem of a torch dtype."""
+    e = {torch.float64: DPC_ELEM_F64, torch.float32: DPC_ELEM_F32, torch.float16: DPC_ELEM_F16,
+         torch.bfloat16: DPC_ELEM_BF16}.get(dtype)
+    if e is None:
+        raise TypeError(f"rows of {dtype} are not supported (float64, float32, float16, bfloat16)")
+    return e
+
+
+def i8_ld(cols):
+    """Bytes of a row of codes (DPC_I8_LD in dpc.h)."""
+    return (int(cols) + 127) // 128 * 128
+
+
+_ELEM_TORCH = {} if torch is None else {DPC_ELEM_F64: torch.float64, DPC_ELEM_F32: torch.float32,
+                                        DPC_ELEM_F16: torch.float16, DPC_ELEM_BF16: torch.bfloat16}
+
+
+def _elem_dtype(elem, name="elem"):
+    if int(elem) not in _ELEM_TORCH:
+        raise DpcError(DPC_EINVAL, name)
+    return _ELEM_TORCH[int(elem)]
+
+
+def _rows_ptr(x, nrows, width, ld, dtype, name):
+    """Address of the rows of a tensor: `nrows` rows of `width` elements, `ld`
+    elements apart, which the tensor's storage has to hold (its own shape is not
+    looked at).  An int is an address and taken as is."""
+    if x is None or isinstance(x, int):
+        return x
+    if x.dtype != dtype:
+        raise TypeError(f"{name} has dtype {x.dtype}, expected {dtype}")
+    have = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
+    need = (int(nrows) - 1) * int(ld) + int(width) if nrows > 0 else 0
+    if have < need:
+        raise ValueError(f"{name} holds {have} elements, needs {need}")
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a tensor on a GPU device, not {x.device}")
+    return x.data_ptr()
+
+
+def _flat_ptr(x, count, dtype, name):
+    """Address of a contiguous tensor of at least `count` elements."""
+    if x is None or isinstance(x, int):
+        return x
+    if not x.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return _rows_ptr(x, 1 if count > 0 else 0, count, count, dtype, name)
+
+
+def _same_device(stream, **tensors):
+    """Every tensor (and a torch stream) must be on one GPU."""
+    devs = {k: v.device.index for k, v in tensors.items() if v is not None and not isinstance(v, int)}
+    if stream is not None and not isinstance(stream, int) and hasattr(stream, "device"):
+        devs["stream"] = stream.device.index
+    if len(set(devs.values())) > 1:
+        raise ValueError("arguments on different devices: " + ", ".join(f"{k}=cuda:{d}" for k, d in devs.items()))
+
+
+def _wdtype(elem):
+    return torch.float64 if int(elem) == DPC_ELEM_F64 else torch.float32
+
+
+def dpc_route_workspace_bytes(ntok, topk, nexpert):
+    return int(_lib.dpc_route_workspace_bytes(int(ntok), int(topk), int(nexpert)))
+
+
+def dpc_route_plan(stream, ntok, topk, nexpert, expert, workspace, workspace_bytes, offsets, rows, pos):
+    m, i32 = int(ntok) * int(topk), torch.int32
+    args = (_flat_ptr(expert, m, i32, "expert"), _flat_ptr(workspace, int(workspace_bytes), torch.uint8, "workspace"),
+            int(workspace_bytes), _flat_ptr(offsets, int(nexpert) + 1, i32, "offsets"), _flat_ptr(rows, m, i32, "rows"),
+            _flat_ptr(pos, m, i32, "pos"))
+    _same_device(stream, expert=expert, workspace=workspace, offsets=offsets, rows=rows, pos=pos)
+    _check(_lib.dpc_route_plan(_stream(stream), int(ntok), int(topk), int(nexpert), *args), "dpc_route_plan")
+
+
+def dpc_route_gather(stream, elem, ntok, topk, width, x, ldx, weight, rows, y, ldy):
+    m, dt = int(ntok) * int(topk), _elem_dtype(elem, "dpc_route_gather")
+    args = (_rows_ptr(x, ntok, width, ldx, dt, "x"), int(ldx), _flat_ptr(weight, m, _wdtype(elem), "weight"),
+            _flat_ptr(rows, m, torch.int32, "rows"), _rows_ptr(y, m, width, ldy, dt, "y"), int(ldy))
+    _same_device(stream, x=x, weight=weight, rows=rows, y=y)
+    _check(_lib.dpc_route_gather(_stream(stream), int(elem), int(ntok), int(topk), int(width), *args),
+           "dpc_route_gather")
+
+
+def dpc_route_combine(stream, elem, ntok, topk, width, x, ldx, weight, pos, y, ldy):
+    m, dt = int(ntok) * int(topk), _elem_dtype(elem, "dpc_route_combine")
+    args = (_rows_ptr(x, m, width, ldx, dt, "x"), int(ldx), _flat_ptr(weight, m, _wdtype(elem), "weight"),
+            _flat_ptr(pos, m, torch.int32, "pos"), _rows_ptr(y, ntok, width, ldy, dt, "y"), int(ldy))
+    _same_device(stream, x=x, weight=weight, pos=pos, y=y)
+    _check(_lib.dpc_route_combine(_stream(stream), int(elem), int(ntok), int(topk), int(width), *args),
+           "dpc_route_combine")
+
+
+def dpc_route_combine_bwd(stream, elem, ntok, topk, width, x, ldx, weight, rows, pos, dy, lddy, dx, lddx, dweight):
+    m, dt = int(ntok) * int(topk), _elem_dtype(elem, "dpc_route_combine_bwd")
+    wt, i32 = _wdtype(elem), torch.int32
+    args = (_rows_ptr(x, m, width, ldx, dt, "x"), int(ldx), _flat_ptr(weight, m, wt, "weight"),
+            _flat_ptr(rows, m, i32, "rows"), _flat_ptr(pos, m, i32, "pos"), _rows_ptr(dy, ntok, width, lddy, dt, "dy"),
+            int(lddy), _rows_ptr(dx, m, width, lddx, dt, "dx"), int(lddx), _flat_ptr(dweight, m, wt, "dweight"))
+    _same_device(stream, x=x, weight=weight, rows=rows, pos=pos, dy=dy, dx=dx, dweight=dweight)
+    _check(_lib.dpc_route_combine_bwd(_stream(stream), int(elem), int(ntok), int(topk), int(width), *args),
+           "dpc_route_combine_bwd")
+
+
+def dpc_quant_rows(stream, elem, nrows, ncols, x, ldx, q, scale):
+    dt = _elem_dtype(elem, "dpc_quant_rows")
+    args = (_rows_ptr(x, nrows, ncols, ldx, dt, "x"), int(ldx),
+            _flat_ptr(q, int(nrows) * i8_ld(ncols), torch.int8, "q"),
+            _flat_ptr(scale, int(nrows), torch.float32, "scale"))
+    _same_device(stream, x=x, q=q, scale=scale)
+    _check(_lib.dpc_quant_rows(_stream(stream), int(elem), int(nrows), int(ncols), *args), "dpc_quant_rows")
+
+
+def _layer_args(elem_y, ntok, topk, n, k, ngroup, rows, offsets, qw, sw, bias, y, ldy, where):
+    m, f32 = int(ntok) * int(topk), torch.float32
+    head = (_flat_ptr(rows, m, torch.int32, "rows"), _flat_ptr(offsets, int(ngroup) + 1, torch.int32, "offsets"),
+            _flat_ptr(qw, int(ngroup) * int(n) * i8_ld(k), torch.int8, "qw"),
+            _flat_ptr(sw, int(ngroup) * int(n), f32, "sw"), _flat_ptr(bias, int(ngroup) * int(n), f32, "bias"))
+    return head, (_rows_ptr(y, m, n, ldy, _elem_dtype(elem_y, where), "y"), int(ldy))
+
+
+def dpc_matmul_i8(stream, elem_y, ntok, topk, n, k, ngroup, qx, sx, rows, offsets, qw, sw, bias, y, ldy):
+    head, tail = _layer_args(elem_y, ntok, topk, n, k, ngroup, rows, offsets, qw, sw, bias, y, ldy, "dpc_matmul_i8")
+    px = (_flat_ptr(qx, int(ntok) * i8_ld(k), torch.int8, "qx"), _flat_ptr(sx, int(ntok), torch.float32, "sx"))
+    _same_device(stream, qx=qx, sx=sx, rows=rows, offsets=offsets, qw=qw, sw=sw, bias=bias, y=y)
+    _check(_lib.dpc_matmul_i8(_stream(stream), int(elem_y), int(ntok), int(topk), int(n), int(k), int(ngroup), *px,
+                              *head, *tail), "dpc_matmul_i8")
+
+
+def dpc_linear_i8_workspace_bytes(ntok, k):
+    return int(_lib.dpc_linear_i8_workspace_bytes(int(ntok), int(k)))
+
+
+def dpc_linear_i8(stream, elem_x, elem_y, ntok, topk, n, k, ngroup, x, ldx, rows, offsets, qw, sw, bias, workspace,
+                  workspace_bytes, y, ldy):
+    head, tail = _layer_args(elem_y, ntok, topk, n, k, ngroup, rows, offsets, qw, sw, bias, y, ldy, "dpc_linear_i8")
+    px = _rows_ptr(x, ntok, k, ldx, _elem_dtype(elem_x, "dpc_linear_i8"), "x")
+    pw = _flat_ptr(workspace, int(workspace_bytes), torch.uint8, "workspace")
+    _same_device(stream, x=x, rows=rows, offsets=offsets, qw=qw, sw=sw, bias=bias, workspace=workspace, y=y)
+    _check(_lib.dpc_linear_i8(_stream(stream), int(elem_x), int(elem_y), int(ntok), int(topk), int(n), int(k),
+                              int(ngroup), px, int(ldx), *head, pw, int(workspace_bytes), *tail), "dpc_linear_i8")
 
 
 class RocblasHandle:

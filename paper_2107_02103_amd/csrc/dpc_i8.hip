@@ -1,0 +1,344 @@
+// Layers in 8-bit integers (dpc_quant_rows, dpc_matmul_i8, dpc_linear_i8).
+//
+// Codes: one read of a row into registers, the largest magnitude across its
+// lanes, then the codes.  Bound by HBM bandwidth.
+//
+// Product: y[r][c] = (sum_i qx[t][i] qw[g][c][i]) sx[t] sw[g][c] + bias[g][c].
+// The sum over i is exact in 32-bit integers, so its order is free.  On the
+// matrix cores W's rows are the rows and x's rows the columns of a tile: a
+// lane of the result then holds four consecutive channels of one row of y.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "dpc.h"
+#include "dpc_elem.h"
+#include "dpc_internal.h"
+
+namespace {
+
+constexpr int64_t kMaxRows = (int64_t)1 << 30;
+
+// ---------------------------------------------------------------------------
+// codes
+// ---------------------------------------------------------------------------
+constexpr int kHeld = 8;  // chunks of a row that a lane holds
+
+// Codes of one chunk: the product is rounded on its own, and adding 1.5 * 2^23
+// rounds it to the nearest integer (ties to even), whose low byte is the code.
+template <int VE>
+__device__ __forceinline__ void codes_of(const float* v, float u, int8_t* q) {
+#pragma clang fp contract(off)
+  unsigned char b[VE];
+#pragma unroll
+  for (int i = 0; i < VE; ++i) {
+    const float p = v[i] * u;
+    b[i] = (unsigned char)__float_as_uint(p + 12582912.0f);
+  }
+  __builtin_memcpy(__builtin_assume_aligned(q, VE), b, VE);
+}
+
+// LANES lanes of a row (up to 64: several rows in a wavefront; 256: a whole
+// workgroup).  HELD: the row fits the lanes' registers and is read once.
+template <typename T, int LANES, bool HELD>
+__global__ __launch_bounds__(256) void quant_kernel(int nrows, int ncols, const T* __restrict__ x, int64_t ldx,
+                                                    int8_t* __restrict__ q, float* __restrict__ scale) {
+  constexpr int VE = Chunk<T>::kElems;
+  const int lane = threadIdx.x & (LANES - 1);
+  const int ld = DPC_I8_LD(ncols), nch = ld / VE;
+  const int64_t groups = (int64_t)gridDim.x * (256 / LANES);
+  const int64_t rounds = (nrows + groups - 1) / groups;
+  int64_t r = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  for (int64_t i = 0; i < rounds; ++i, r += groups) {
+    const bool in = r < nrows;
+    const T* px = x + (in ? r : 0) * ldx;
+    auto fetch = [&](int c, float* v) __attribute__((always_inline)) {
+      if (c * VE + VE <= ncols) {
+        Chunk<T> ch;
+        ch.load(px + c * VE);
+#pragma unroll
+        for (int k = 0; k < VE; ++k) v[k] = (float)ch.v[k];
+      } else {
+#pragma unroll
+        for (int k = 0; k < VE; ++k) v[k] = c * VE + k < ncols ? (float)px[c * VE + k] : 0.0f;
+      }
+    };
+    float held[HELD ? kHeld : 1][VE];
+    // as whole numbers the magnitudes keep their order, and NaN is the largest
+    unsigned top = 0;
+    if (in) {
+      if (HELD) {
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h)
+          if (lane + h * LANES < nch) fetch(lane + h * LANES, held[h]);
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h)
+          if (lane + h * LANES < nch)
+#pragma unroll
+            for (int k = 0; k < VE; ++k) top = max(top, __float_as_uint(held[h][k]) & 0x7fffffffu);
+      } else {
+        for (int c = lane; c < nch; c += LANES) {
+          float v[VE];
+          fetch(c, v);
+#pragma unroll
+          for (int k = 0; k < VE; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
+        }
+      }
+    }
+#pragma unroll
+    for (int m = (LANES < 64 ? LANES : 64) >> 1; m; m >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, m));
+    if (LANES > 64) {
+      __shared__ unsigned tops[4];
+      __syncthreads();  // the row before has been read
+      if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+      __syncthreads();
+      top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+    }
+    if (!in) continue;
+    const float a = __uint_as_float(top);
+    const bool finite = top < 0x7f800000u, live = finite && a >= 0x1p-100f;
+    const float u = live ? 127.0f / a : 0.0f;
+    if (lane == 0) scale[r] = live ? a / 127.0f : finite ? 0.0f : __builtin_nanf("");
+    int8_t* pq = q + r * ld;
+    auto put = [&](int c, float* v) __attribute__((always_inline)) {
+      if (!finite)
+#pragma unroll
+        for (int k = 0; k < VE; ++k) v[k] = 0.0f;
+      codes_of<VE>(v, u, pq + c * VE);
+    };
+    if (HELD) {
+#pragma unroll
+      for (int h = 0; h < kHeld; ++h)
+        if (lane + h * LANES < nch) put(lane + h * LANES, held[h]);
+    } else {
+      for (int c = lane; c < nch; c += LANES) {
+        float v[VE];
+        fetch(c, v);
+        put(c, v);
+      }
+    }
+  }
+}
+
+template <typename T>
+void launch_quant(hipStream_t s, int nrows, int ncols, const T* x, int64_t ldx, int8_t* q, float* scale) {
+  const int nch = DPC_I8_LD(ncols) / Chunk<T>::kElems;
+  auto go = [&](auto kernel, int lanes) {
+    const int64_t per = 256 / lanes, blocks = (nrows + per - 1) / per, most = 1 << 20;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, s, nrows, ncols, x, ldx, q,
+                       scale);
+  };
+  // the fewest lanes that hold a row, at most two chunks each in short rows
+  if (nch <= 16 * 2) go(quant_kernel<T, 16, true>, 16);
+  else if (nch <= 64 * kHeld) go(quant_kernel<T, 64, true>, 64);
+  else if (nch <= 256 * kHeld) go(quant_kernel<T, 256, true>, 256);
+  else go(quant_kernel<T, 256, false>, 256);
+}
+
+int quant(hipStream_t s, dpc_elem elem, int nrows, int ncols, const void* x, int64_t ldx, int8_t* q, float* scale) {
+  (void)hipGetLastError();  // report only what this launch raises
+  switch (elem) {
+    case DPC_ELEM_F64: launch_quant(s, nrows, ncols, (const double*)x, ldx, q, scale); break;
+    case DPC_ELEM_F32: launch_quant(s, nrows, ncols, (const float*)x, ldx, q, scale); break;
+    case DPC_ELEM_F16: launch_quant(s, nrows, ncols, (const _Float16*)x, ldx, q, scale); break;
+    default: launch_quant(s, nrows, ncols, (const __bf16*)x, ldx, q, scale); break;
+  }
+  return dpc_internal_launch_status();
+}
+
+// ---------------------------------------------------------------------------
+// product
+// ---------------------------------------------------------------------------
+typedef int v4i __attribute__((ext_vector_type(4)));
+
+struct Product {
+  int ntok, topk, m, n, k, ld, ngroup;
+  const int8_t* qx;
+  const float* sx;
+  const int* rows;
+  const int* offsets;
+  const int8_t* qw;
+  const float* sw;
+  const float* bias;
+};
+
+// Rows [row0, end) of one tile of a group, or of the empty rows (group < 0);
+// end = row0 if the tile does not exist.
+struct Tile {
+  int group, row0, end;
+};
+
+// The tile-th tile of `size` rows: the tiles of group 0, of group 1, ... and of
+// the rows past the last group.  Whole wavefronts call this.
+__device__ __forceinline__ Tile find_tile(const Product& p, int size, int tile) {
+  if (!p.offsets) {
+    const int row0 = tile * size;
+    return Tile{0, row0 < p.m ? row0 : p.m, row0 + size < p.m ? row0 + size : p.m};
+  }
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int g0 = 0; g0 <= p.ngroup; g0 += 64) {
+    const int g = g0 + lane;
+    int first = p.m, last = p.m;
+    if (g <= p.ngroup) first = min(max(p.offsets[g], 0), p.m);
+    if (g < p.ngroup) last = max(min(max(p.offsets[g + 1], 0), p.m), first);
+    const int tiles = (last - first + size - 1) / size;
+    int sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(sum, d);
+      if (lane >= d) sum += up;
+    }
+    const unsigned long long past = __ballot(before + sum > tile);
+    if (past) {
+      const int at = __ffsll(past) - 1;
+      const int lo = __shfl(first, at), hi = __shfl(last, at);
+      const int row0 = lo + (tile - before - __shfl(sum - tiles, at)) * size;
+      return Tile{g0 + at < p.ngroup ? g0 + at : -1, row0, min(row0 + size, hi)};
+    }
+    before += __shfl(sum, 63);
+  }
+  return Tile{-1, p.m, p.m};
+}
+
+// Tiles of `size` rows that find_tile can be asked for.
+inline int64_t most_tiles(const Product& p, int size) {
+  if (!p.offsets) return ((int64_t)p.m + size - 1) / size;
+  // every group and the empty rows may end in a tile of their own
+  const int64_t t = (int64_t)p.m / size + p.ngroup + 1;
+  return t < p.m ? t : p.m;
+}
+
+// token of row r, or -1
+__device__ __forceinline__ int token_of(const Product& p, int r) {
+  if (!p.rows) return r;
+  const int s = p.rows[r];
+  return (unsigned)s < (unsigned)p.m ? (int)((unsigned)s / (unsigned)p.topk) : -1;
+}
+
+template <typename TY>
+__device__ __forceinline__ TY scaled(int acc, double sx, float sw, float bias) {
+  const double v = (double)acc * sx * (double)sw + (double)bias;
+  if constexpr (sizeof(TY) == 8) return v;
+  return (TY)(float)v;
+}
+
+// One wavefront makes 16 rows times 16 channels of y, operands straight from
+// memory.
+template <typename TY>
+__global__ __launch_bounds__(64) void product_kernel(Product p, TY* __restrict__ y, int64_t ldy) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const Tile t = find_tile(p, 16, blockIdx.y + gridDim.y * blockIdx.z);
+  if (t.row0 >= t.end) return;
+  const int r = t.row0 + l16, c0 = blockIdx.x * 16;
+  const int tok = r < t.end && t.group >= 0 ? token_of(p, r) : -1;
+  v4i acc = {0, 0, 0, 0};
+  if (t.group >= 0) {
+    const int8_t* px = p.qx + (int64_t)(tok < 0 ? 0 : tok) * p.ld + quad * 16;
+    const int cw = min(c0 + l16, p.n - 1);
+    const int8_t* pw = p.qw + ((int64_t)t.group * p.n + cw) * p.ld + quad * 16;
+    for (int k = 0; k < p.ld; k += 64) {
+      const v4i a = *reinterpret_cast<const v4i*>(pw + k);
+      const v4i b = *reinterpret_cast<const v4i*>(px + k);
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc, 0, 0, 0);
+    }
+  }
+  if (r >= t.end) return;
+  const double sx = tok < 0 ? 0.0 : (double)p.sx[tok];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = c0 + quad * 4 + i;
+    if (c >= p.n) break;
+    TY out = (TY)0;
+    if (tok >= 0) {
+      const int64_t gc = (int64_t)t.group * p.n + c;
+      out = scaled<TY>(acc[i], sx, p.sw[gc], p.bias ? p.bias[gc] : 0.0f);
+    }
+    y[(int64_t)r * ldy + c] = out;
+  }
+}
+
+template <typename TY>
+void launch_product(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
+  const int64_t tiles = most_tiles(p, 16);
+  const unsigned gy = (unsigned)(tiles < 32768 ? tiles : 32768);
+  hipLaunchKernelGGL((product_kernel<TY>), dim3((p.n + 15) / 16, gy, (unsigned)((tiles + gy - 1) / gy)), dim3(64), 0, s,
+                     p, y, ldy);
+}
+
+int product(hipStream_t s, dpc_elem elem_y, const Product& p, void* y, int64_t ldy) {
+  (void)hipGetLastError();  // report only what this launch raises
+  switch (elem_y) {
+    case DPC_ELEM_F64: launch_product(s, p, (double*)y, ldy); break;
+    case DPC_ELEM_F32: launch_product(s, p, (float*)y, ldy); break;
+    case DPC_ELEM_F16: launch_product(s, p, (_Float16*)y, ldy); break;
+    default: launch_product(s, p, (__bf16*)y, ldy); break;
+  }
+  return dpc_internal_launch_status();
+}
+
+int product_args(dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup) {
+  if (!elem_ok(elem_y) || ntok < 0 || topk < 1 || n < 1 || k < 1 || ngroup < 1) return DPC_EINVAL;
+  if (topk > DPC_MAX_TOPK || k > DPC_MAX_I8_COLS || ngroup > DPC_MAX_EXPERTS || (int64_t)ntok * topk > kMaxRows)
+    return DPC_ENOTSUP;
+  return DPC_OK;
+}
+
+bool product_ptrs(dpc_elem elem_y, int topk, int n, int ngroup, const int* rows, const int* offsets, const int8_t* qw,
+                  const float* sw, const float* bias, const void* y, int64_t ldy) {
+  if ((!rows && topk != 1) || (!offsets && ngroup != 1)) return false;
+  return qw && sw && y && ldy >= n && elem_aligned(qw, 16) && elem_aligned(sw, 4) && elem_aligned(bias, 4) &&
+         elem_aligned(rows, 4) && elem_aligned(offsets, 4) && elem_aligned(y, elem_size(elem_y));
+}
+
+}  // namespace
+
+extern "C" int dpc_quant_rows(void* stream, dpc_elem elem, int nrows, int ncols, const void* x, int64_t ldx, int8_t* q,
+                              float* scale) {
+  if (!elem_ok(elem) || nrows < 0 || ncols < 1) return DPC_EINVAL;
+  if (ncols > DPC_MAX_I8_COLS || nrows > kMaxRows) return DPC_ENOTSUP;
+  if (nrows == 0) return DPC_OK;
+  if (!x || !q || !scale || ldx < ncols || !elem_aligned(x, elem_size(elem)) || !elem_aligned(q, 16) ||
+      !elem_aligned(scale, 4))
+    return DPC_EINVAL;
+  return quant(static_cast<hipStream_t>(stream), elem, nrows, ncols, x, ldx, q, scale);
+}
+
+extern "C" int dpc_matmul_i8(void* stream, dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup,
+                             const int8_t* qx, const float* sx, const int* rows, const int* offsets, const int8_t* qw,
+                             const float* sw, const float* bias, void* y, int64_t ldy) {
+  const int st = product_args(elem_y, ntok, topk, n, k, ngroup);
+  if (st != DPC_OK) return st;
+  if (ntok == 0) return DPC_OK;
+  if (!qx || !sx || !elem_aligned(qx, 16) || !elem_aligned(sx, 4) ||
+      !product_ptrs(elem_y, topk, n, ngroup, rows, offsets, qw, sw, bias, y, ldy))
+    return DPC_EINVAL;
+  const Product p{ntok, topk, ntok * topk, n, k, DPC_I8_LD(k), ngroup, qx, sx, rows, offsets, qw, sw, bias};
+  return product(static_cast<hipStream_t>(stream), elem_y, p, y, ldy);
+}
+
+extern "C" size_t dpc_linear_i8_workspace_bytes(int ntok, int k) {
+  if (ntok < 0 || ntok > kMaxRows || k < 1 || k > DPC_MAX_I8_COLS) return 0;
+  return ((size_t)ntok * DPC_I8_LD(k) + (size_t)ntok * sizeof(float) + 255) / 256 * 256 + 256;
+}
+
+extern "C" int dpc_linear_i8(void* stream, dpc_elem elem_x, dpc_elem elem_y, int ntok, int topk, int n, int k,
+                             int ngroup, const void* x, int64_t ldx, const int* rows, const int* offsets,
+                             const int8_t* qw, const float* sw, const float* bias, void* workspace,
+                             size_t workspace_bytes, void* y, int64_t ldy) {
+  const int st = product_args(elem_y, ntok, topk, n, k, ngroup);
+  if (st != DPC_OK) return st;
+  if (!elem_ok(elem_x)) return DPC_EINVAL;
+  if (ntok == 0) return DPC_OK;
+  if (!x || ldx < k || !elem_aligned(x, elem_size(elem_x)) || !workspace || !elem_aligned(workspace, 16) ||
+      workspace_bytes < dpc_linear_i8_workspace_bytes(ntok, k) ||
+      !product_ptrs(elem_y, topk, n, ngroup, rows, offsets, qw, sw, bias, y, ldy))
+    return DPC_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  int8_t* q = static_cast<int8_t*>(workspace);
+  float* scale = reinterpret_cast<float*>(q + (size_t)ntok * DPC_I8_LD(k));
+  const int qs = quant(s, elem_x, ntok, k, x, ldx, q, scale);
+  if (qs != DPC_OK) return qs;
+  const Product p{ntok, topk, ntok * topk, n, k, DPC_I8_LD(k), ngroup, q, scale, rows, offsets, qw, sw, bias};
+  return product(s, elem_y, p, y, ldy);
+}
