@@ -369,19 +369,20 @@ size_t dpc_route_workspace_bytes(int ntok, int topk, int nexpert);
 int dpc_route_plan(void* stream, int ntok, int topk, int nexpert, const int* expert, void* workspace,
                    size_t workspace_bytes, int* offsets, int* rows, int* pos);
 
-/* Rows of the tokens in the plan's order, and their gradient's half:
- *   y[r] = weight[s] * x[s / topk],  s = rows[r];  zeros where rows[r] is not
- *   a slot.
+/* Rows of the tokens in the plan's order:
+ *   y[pos[t][j]] = weight[t][j] * x[t];  zeros in the empty rows.
  *   x       device [ntok] rows of `width` elements, ldx elements apart
  *   weight  device [ntok][topk] (float64 for DPC_ELEM_F64, else float32) or
  *           NULL for weights of 1.  With weights, this maps the gradient of
  *           dpc_route_combine's y to that of its x.
+ *   rows, pos  the plan
  *   y       device out [nslot] rows, ldy elements apart
  * Products are rounded once from float64 (DPC_ELEM_F64) or float32.  Rows
  * need the alignment of their elements alone.  Requires width >= 1, ldx and
  * ldy >= width.  Inputs and outputs must not overlap.                       */
 int dpc_route_gather(void* stream, dpc_elem elem, int ntok, int topk, int width, const void* x,
-                     int64_t ldx, const void* weight, const int* rows, void* y, int64_t ldy);
+                     int64_t ldx, const void* weight, const int* rows, const int* pos, void* y,
+                     int64_t ldy);
 
 /* Rows back to their tokens, with weights:
  *   y[t] = sum over j with pos[t][j] a row, j ascending, of

@@ -114,7 +114,7 @@ _lib.dpc_route_workspace_bytes.argtypes = [_I, _I, _I]
 _lib.dpc_route_plan.restype = _I
 _lib.dpc_route_plan.argtypes = [_P, _I, _I, _I, _P, _P, _Z, _P, _P, _P]
 _lib.dpc_route_gather.restype = _I
-_lib.dpc_route_gather.argtypes = [_P, _I, _I, _I, _I, _P, _L, _P, _P, _P, _L]
+_lib.dpc_route_gather.argtypes = [_P, _I, _I, _I, _I, _P, _L, _P, _P, _P, _P, _L]
 _lib.dpc_route_combine.restype = _I
 _lib.dpc_route_combine.argtypes = [_P, _I, _I, _I, _I, _P, _L, _P, _P, _P, _L]
 _lib.dpc_route_combine_bwd.restype = _I
@@ -516,11 +516,12 @@ def dpc_route_plan(stream, ntok, topk, nexpert, expert, workspace, workspace_byt
     _check(_lib.dpc_route_plan(_stream(stream), int(ntok), int(topk), int(nexpert), *args), "dpc_route_plan")
 
 
-def dpc_route_gather(stream, elem, ntok, topk, width, x, ldx, weight, rows, y, ldy):
+def dpc_route_gather(stream, elem, ntok, topk, width, x, ldx, weight, rows, pos, y, ldy):
     m, dt = int(ntok) * int(topk), _elem_dtype(elem, "dpc_route_gather")
     args = (_rows_ptr(x, ntok, width, ldx, dt, "x"), int(ldx), _flat_ptr(weight, m, _wdtype(elem), "weight"),
-            _flat_ptr(rows, m, torch.int32, "rows"), _rows_ptr(y, m, width, ldy, dt, "y"), int(ldy))
-    _same_device(stream, x=x, weight=weight, rows=rows, y=y)
+            _flat_ptr(rows, m, torch.int32, "rows"), _flat_ptr(pos, m, torch.int32, "pos"),
+            _rows_ptr(y, m, width, ldy, dt, "y"), int(ldy))
+    _same_device(stream, x=x, weight=weight, rows=rows, pos=pos, y=y)
     _check(_lib.dpc_route_gather(_stream(stream), int(elem), int(ntok), int(topk), int(width), *args),
            "dpc_route_gather")
 

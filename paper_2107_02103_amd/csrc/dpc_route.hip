@@ -32,7 +32,7 @@ constexpr int64_t kMaxSlots = (int64_t)1 << 30;
 // plan
 // ---------------------------------------------------------------------------
 constexpr int kOneBlockSlots = 16384;  // up to here one workgroup makes the whole plan
-constexpr int kPartSlots = 4096;       // slots of a workgroup beyond that, at least
+constexpr int kPartSlots = 1024;       // slots of a workgroup beyond that, at least
 constexpr int kMaxBlocks = 1024;
 constexpr int kPlanWaves = 4;          // wavefronts of a workgroup of the three-launch plan
 
@@ -258,49 +258,6 @@ __device__ __forceinline__ T times(typename ElemAcc<T>::type w, T v) {
 }
 
 template <typename T, bool WEIGHT>
-__global__ __launch_bounds__(kBlock) void gather_kernel(Shape sh, const T* __restrict__ x, int64_t ldx,
-                                                        const typename ElemAcc<T>::type* __restrict__ weight,
-                                                        const int* __restrict__ rows, T* __restrict__ y, int64_t ldy) {
-  typedef typename ElemAcc<T>::type A;
-  constexpr int VE = Chunk<T>::kElems, U = 4;
-  const int lanes = 1 << sh.lanes_log2, lane = threadIdx.x & (lanes - 1);
-  const int64_t groups = ((int64_t)gridDim.x * kBlock) >> sh.lanes_log2;
-  const int nch = (sh.width + VE - 1) / VE;
-  for (int64_t r = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> sh.lanes_log2; r < sh.nslot; r += groups) {
-    const int s = rows[r];
-    const bool live = (unsigned)s < (unsigned)sh.nslot;
-    const T* px = x + (live ? (int64_t)((unsigned)s / (unsigned)sh.topk) * ldx : 0);
-    T* py = y + r * ldy;
-    A w = (A)1;
-    if (WEIGHT) w = live ? weight[s] : (A)0;
-    if (sh.width < VE) {
-      for (int c = lane; c < sh.width; c += lanes)
-        py[c] = !live ? (T)0 : WEIGHT ? times<T>(w, px[c]) : px[c];
-      continue;
-    }
-    for (int c0 = lane; c0 < nch; c0 += U * lanes) {
-      Chunk<T> ch[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * lanes;
-        const int at = c * VE < sh.width - VE ? c * VE : sh.width - VE;
-        if (c < nch && live) ch[u].load(px + at);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * lanes;
-        const int at = c * VE < sh.width - VE ? c * VE : sh.width - VE;
-        if (c >= nch) break;
-#pragma unroll
-        for (int i = 0; i < VE; ++i)
-          ch[u].v[i] = !live ? (T)0 : WEIGHT ? times<T>(w, ch[u].v[i]) : ch[u].v[i];
-        ch[u].store(py + at);
-      }
-    }
-  }
-}
-
-template <typename T, bool WEIGHT>
 __global__ __launch_bounds__(kBlock) void combine_kernel(Shape sh, const T* __restrict__ x, int64_t ldx,
                                                          const typename ElemAcc<T>::type* __restrict__ weight,
                                                          const int* __restrict__ pos, T* __restrict__ y, int64_t ldy) {
@@ -347,8 +304,11 @@ __global__ __launch_bounds__(kBlock) void combine_kernel(Shape sh, const T* __re
   }
 }
 
-template <typename T, bool WEIGHT>
-__global__ __launch_bounds__(kBlock) void combine_bwd_kernel(
+// Sends dy to the rows of its token (times their weights), and with DOT takes
+// the dot product of each row with it.  Token by token, J of a token's rows at
+// a time: a token's dy is read from memory once, whatever its number of rows.
+template <typename T, bool WEIGHT, bool DOT, int J>
+__global__ __launch_bounds__(kBlock) void send_kernel(
     Shape sh, const T* __restrict__ x, int64_t ldx, const typename ElemAcc<T>::type* __restrict__ weight,
     const int* __restrict__ rows, const int* __restrict__ pos, const T* __restrict__ dy, int64_t lddy,
     T* __restrict__ dx, int64_t lddx, typename ElemAcc<T>::type* __restrict__ dweight) {
@@ -363,49 +323,76 @@ __global__ __launch_bounds__(kBlock) void combine_bwd_kernel(
   for (int64_t i = 0; i < rounds; ++i, t += groups) {
     const bool in = t < sh.ntok;
     const T* pdy = dy + (in ? t : 0) * lddy;
-    for (int j = 0; j < sh.topk; ++j) {
-      const int64_t s = (in ? t : 0) * sh.topk + j;
-      const int r = in ? pos[s] : -1;
-      const bool live = (unsigned)r < (unsigned)sh.nslot;
-      A w = (A)1;
-      if (WEIGHT) w = live ? weight[s] : (A)0;
-      A dot = (A)0;
-      if (live && sh.width < VE) {
+    for (int j0 = 0; j0 < sh.topk; j0 += J) {
+      const int64_t s0 = (in ? t : 0) * sh.topk + j0;
+      int r[J];
+      bool live[J], any = false;
+      A w[J], dot[J];
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const bool mine = in && j0 + j < sh.topk;
+        r[j] = mine ? pos[s0 + j] : -1;
+        live[j] = (unsigned)r[j] < (unsigned)sh.nslot;
+        any |= live[j];
+        w[j] = (A)1;
+        if (WEIGHT) w[j] = live[j] ? weight[s0 + j] : (A)0;
+        dot[j] = (A)0;
+      }
+      if (any && sh.width < VE) {
         for (int c = lane; c < sh.width; c += lanes) {
-          const A d = (A)pdy[c];
-          if (dweight) dot += d * (A)x[(int64_t)r * ldx + c];
-          if (dx) dx[(int64_t)r * lddx + c] = WEIGHT ? times<T>(w, pdy[c]) : pdy[c];
+          const T d = pdy[c];
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            if (!live[j]) continue;
+            if (DOT) dot[j] += (A)d * (A)x[(int64_t)r[j] * ldx + c];
+            if (dx) dx[(int64_t)r[j] * lddx + c] = WEIGHT ? times<T>(w[j], d) : d;
+          }
         }
-      } else if (live) {
+      } else if (any) {
         for (int c = lane; c < nch; c += lanes) {
           const int at = c * VE < sh.width - VE ? c * VE : sh.width - VE;
-          Chunk<T> d, v;
+          Chunk<T> d, v[J];
           d.load(pdy + at);
-          if (dweight) {
-            v.load(x + (int64_t)r * ldx + at);
+          if (DOT) {
 #pragma unroll
-            for (int k = 0; k < VE; ++k) {
-              // elements that the chunk before holds too count there
-              const A p = (A)d.v[k] * (A)v.v[k];
-              dot += at + k >= c * VE ? p : (A)0;
+            for (int j = 0; j < J; ++j)
+              if (live[j]) v[j].load(x + (int64_t)r[j] * ldx + at);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+              if (!live[j]) continue;
+#pragma unroll
+              for (int k = 0; k < VE; ++k) {
+                // elements that the chunk before holds too count there
+                const A p = (A)d.v[k] * (A)v[j].v[k];
+                dot[j] += at + k >= c * VE ? p : (A)0;
+              }
             }
           }
           if (dx) {
-            if (WEIGHT) {
 #pragma unroll
-              for (int k = 0; k < VE; ++k) d.v[k] = times<T>(w, d.v[k]);
+            for (int j = 0; j < J; ++j) {
+              if (!live[j]) continue;
+              Chunk<T> out = d;
+              if (WEIGHT) {
+#pragma unroll
+                for (int k = 0; k < VE; ++k) out.v[k] = times<T>(w[j], d.v[k]);
+              }
+              out.store(dx + (int64_t)r[j] * lddx + at);
             }
-            d.store(dx + (int64_t)r * lddx + at);
           }
         }
       }
-      if (dweight) {
-        for (int m = lanes >> 1; m; m >>= 1) dot += __shfl_xor(dot, m);
-        if (in && lane == 0) dweight[s] = dot;
-      }
-      // the empty rows: row s is looked at here
-      if (dx && in && (unsigned)rows[s] >= (unsigned)sh.nslot) {
-        for (int c = lane; c < sh.width; c += lanes) dx[s * lddx + c] = (T)0;
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        if (j0 + j >= sh.topk) break;
+        if (DOT) {
+          for (int m = lanes >> 1; m; m >>= 1) dot[j] += __shfl_xor(dot[j], m);
+          if (in && lane == 0) dweight[s0 + j] = dot[j];
+        }
+        // the empty rows: row s0 + j is looked at here
+        if (dx && in && (unsigned)rows[s0 + j] >= (unsigned)sh.nslot) {
+          for (int c = lane; c < sh.width; c += lanes) dx[(s0 + j) * lddx + c] = (T)0;
+        }
       }
     }
   }
@@ -450,6 +437,20 @@ int by_type(dpc_elem elem, bool weight, F f) {
     default: weight ? f(__bf16{}, std::true_type{}) : f(__bf16{}, std::false_type{}); break;
   }
   return dpc_internal_launch_status();
+}
+
+int send(void* stream, dpc_elem elem, const Shape& sh, const void* x, int64_t ldx, const void* weight, const int* rows,
+         const int* pos, const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dweight) {
+  return by_type(elem, weight != nullptr, [&](auto t, auto w) {
+    typedef decltype(t) T;
+    typedef typename ElemAcc<T>::type A;
+    constexpr bool W = decltype(w)::value;
+    const auto kernel = sh.topk == 1 ? (dweight ? send_kernel<T, W, true, 1> : send_kernel<T, W, false, 1>)
+                                     : (dweight ? send_kernel<T, W, true, 4> : send_kernel<T, W, false, 4>);
+    hipLaunchKernelGGL(kernel, dim3(grid_for(sh.ntok, sh.lanes_log2)), dim3(kBlock), 0,
+                       static_cast<hipStream_t>(stream), sh, (const T*)x, ldx, (const A*)weight, rows, pos,
+                       (const T*)dy, lddy, (T*)dx, lddx, (A*)dweight);
+  });
 }
 
 }  // namespace
@@ -498,20 +499,15 @@ extern "C" int dpc_route_plan(void* stream, int ntok, int topk, int nexpert, con
 }
 
 extern "C" int dpc_route_gather(void* stream, dpc_elem elem, int ntok, int topk, int width, const void* x, int64_t ldx,
-                                const void* weight, const int* rows, void* y, int64_t ldy) {
+                                const void* weight, const int* rows, const int* pos, void* y, int64_t ldy) {
   Shape sh;
   const int st = row_shape(elem, ntok, topk, width, &sh);
   if (st != DPC_OK) return st;
   if (ntok == 0) return DPC_OK;
   if (!rows_ok(elem, x, ldx, width) || !rows_ok(elem, y, ldy, width) || !weight_ok(elem, weight) || !rows ||
-      !elem_aligned(rows, 4))
+      !pos || !elem_aligned(rows, 4) || !elem_aligned(pos, 4))
     return DPC_EINVAL;
-  return by_type(elem, weight != nullptr, [&](auto t, auto w) {
-    typedef decltype(t) T;
-    hipLaunchKernelGGL((gather_kernel<T, decltype(w)::value>), dim3(grid_for(sh.nslot, sh.lanes_log2)), dim3(kBlock), 0,
-                       static_cast<hipStream_t>(stream), sh, (const T*)x, ldx,
-                       (const typename ElemAcc<T>::type*)weight, rows, (T*)y, ldy);
-  });
+  return send(stream, elem, sh, nullptr, 0, weight, rows, pos, x, ldx, y, ldy, nullptr);
 }
 
 extern "C" int dpc_route_combine(void* stream, dpc_elem elem, int ntok, int topk, int width, const void* x, int64_t ldx,
@@ -543,11 +539,5 @@ extern "C" int dpc_route_combine_bwd(void* stream, dpc_elem elem, int ntok, int 
       (dx && !rows_ok(elem, dx, lddx, width)) || !weight_ok(elem, weight) || !weight_ok(elem, dweight) || !rows ||
       !pos || !elem_aligned(rows, 4) || !elem_aligned(pos, 4))
     return DPC_EINVAL;
-  return by_type(elem, weight != nullptr, [&](auto t, auto w) {
-    typedef decltype(t) T;
-    typedef typename ElemAcc<T>::type A;
-    hipLaunchKernelGGL((combine_bwd_kernel<T, decltype(w)::value>), dim3(grid_for(ntok, sh.lanes_log2)), dim3(kBlock),
-                       0, static_cast<hipStream_t>(stream), sh, (const T*)x, ldx, (const A*)weight, rows, pos,
-                       (const T*)dy, lddy, (T*)dx, lddx, (A*)dweight);
-  });
+  return send(stream, elem, sh, x, ldx, weight, rows, pos, dy, lddy, dx, lddx, dweight);
 }

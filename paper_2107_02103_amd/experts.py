@@ -7,9 +7,26 @@ import torch
 from . import binding as B
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(stream):
     """Outputs and workspaces are allocated for the stream that uses them."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _HERE if stream is None else torch.cuda.stream(stream)
+
+
+def _raw(stream, device):
+    """hipStream_t of a torch stream, or of the device's current one."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
+def _check(status, where):
+    if status:
+        raise B.DpcError(status, where)
+
+
+def _elsewhere(t, device):
+    raise ValueError(f"a tensor is on {t.device}, the others are on cuda:{device}")
 
 
 def _matrix(x, name, rows=None, width=None, dtype=None):
@@ -61,8 +78,10 @@ class Route:
             self.offsets, self.rows = buf[:self.nexpert + 1], buf[self.nexpert + 1:self.nexpert + 1 + m]
             self.pos = buf[self.nexpert + 1 + m:].view(self.ntok, self.topk)
             ws = torch.empty(nb, dtype=torch.uint8, device=dev)
-            B.dpc_route_plan(stream or torch.cuda.current_stream(dev), self.ntok, self.topk, self.nexpert, expert, ws,
-                             nb, self.offsets, self.rows, self.pos)
+            at = buf.data_ptr()
+            _check(B._lib.dpc_route_plan(_raw(stream, dev.index), self.ntok, self.topk, self.nexpert,
+                                         expert.data_ptr(), ws.data_ptr(), nb, at, at + 4 * (self.nexpert + 1),
+                                         at + 4 * (self.nexpert + 1 + m)), "dpc_route_plan")
 
     @classmethod
     def from_plan(cls, offsets, rows, pos):
@@ -81,10 +100,17 @@ class Route:
     def _weight(self, weight, x):
         if weight is None:
             return None
-        want = B._wdtype(B.elem_of(x.dtype))
-        if weight.dtype != want or tuple(weight.shape) != (self.ntok, self.topk):
-            raise ValueError(f"weight must be {want} [tokens, topk]")
+        want = torch.float64 if x.dtype == torch.float64 else torch.float32
+        if weight.dtype != want or weight.shape != self.pos.shape or not weight.is_contiguous():
+            raise ValueError(f"weight must be contiguous {want} [tokens, topk]")
         return weight
+
+    def _call(self, name, stream, x, width, *args):
+        """args: tensors are passed by address"""
+        dev = self.pos.get_device()
+        args = [a if a is None or isinstance(a, int) else a.data_ptr() if a.get_device() == dev else
+                _elsewhere(a, dev) for a in args]
+        _check(getattr(B._lib, name)(_raw(stream, dev), B.elem_of(x.dtype), self.ntok, self.topk, width, *args), name)
 
     def gather(self, x, weight=None, out=None, stream=None):
         """[tokens * topk, width]: each row the token's row (times its weight),
@@ -93,8 +119,8 @@ class Route:
         m, width = self.ntok * self.topk, x.shape[1]
         with _on(stream):
             y = _out(out, m, width, x, "out")
-            B.dpc_route_gather(stream or torch.cuda.current_stream(x.device), B.elem_of(x.dtype), self.ntok, self.topk,
-                               width, x, ldx, self._weight(weight, x), self.rows, y, _matrix(y, "out"))
+            self._call("dpc_route_gather", stream, x, width, x, ldx, self._weight(weight, x), self.rows, self.pos, y,
+                       y.stride(0) if m > 1 else max(width, 1))
         return y
 
     def combine(self, x, weight=None, out=None, stream=None):
@@ -105,8 +131,8 @@ class Route:
         width = x.shape[1]
         with _on(stream):
             y = _out(out, self.ntok, width, x, "out")
-            B.dpc_route_combine(stream or torch.cuda.current_stream(x.device), B.elem_of(x.dtype), self.ntok, self.topk,
-                                width, x, ldx, self._weight(weight, x), self.pos, y, _matrix(y, "out"))
+            self._call("dpc_route_combine", stream, x, width, x, ldx, self._weight(weight, x), self.pos, y,
+                       y.stride(0) if self.ntok > 1 else max(width, 1))
         return y
 
     def combine_backward(self, x, dy, weight=None, need_rows=True, stream=None):
@@ -122,8 +148,8 @@ class Route:
         with _on(stream):
             dx = torch.empty((m, width), dtype=x.dtype, device=x.device) if need_rows else None
             dw = None if w is None else torch.empty_like(w, memory_format=torch.contiguous_format)
-            B.dpc_route_combine_bwd(stream or torch.cuda.current_stream(x.device), B.elem_of(x.dtype), self.ntok,
-                                    self.topk, width, x, ldx, w, self.rows, self.pos, dy, lddy, dx, max(width, 1), dw)
+            self._call("dpc_route_combine_bwd", stream, x, width, x, ldx, w, self.rows, self.pos, dy, lddy, dx,
+                       max(width, 1), dw)
         return dx, dw
 
 
@@ -142,8 +168,10 @@ class Int8Linear:
             raise ValueError("codes must be int8 [experts, outer, i8_ld(inner)]")
         self.experts, self.outer = codes.shape[:2]
         for name, t in (("scales", scales), ("bias", bias)):
-            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (self.experts, self.outer)):
-                raise ValueError(f"{name} must be float32 [experts, outer]")
+            if t is not None and (t.dtype != torch.float32 or t.shape != codes.shape[:2] or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous float32 [experts, outer]")
+        if not codes.is_contiguous() or not codes.is_cuda:
+            raise ValueError("codes must be a contiguous tensor on a GPU device")
         self.codes, self.scales, self.bias = codes, scales, bias
 
     @classmethod
@@ -175,6 +203,8 @@ class Int8Linear:
             if offsets is not None:
                 raise ValueError("give a route or offsets, not both")
             topk, rows, offsets = route.topk, route.rows, route.offsets
+        if offsets is not None and (offsets.dtype != torch.int32 or not offsets.is_contiguous()):
+            raise TypeError("offsets must be contiguous int32")
         if offsets is not None and len(offsets) != self.experts + 1:
             raise ValueError(f"offsets for {len(offsets) - 1} experts, layers for {self.experts}")
         if offsets is None and self.experts != 1:
@@ -185,7 +215,10 @@ class Int8Linear:
             ldy = _matrix(y, "out", ntok * topk, self.outer, dtype)
             nb = B.dpc_linear_i8_workspace_bytes(ntok, self.inner)
             ws = torch.empty(nb, dtype=torch.uint8, device=x.device)
-            B.dpc_linear_i8(stream or torch.cuda.current_stream(x.device), B.elem_of(x.dtype), B.elem_of(dtype), ntok,
-                            topk, self.outer, self.inner, self.experts, x, ldx, rows, offsets, self.codes,
-                            self.scales, self.bias, ws, nb, y, ldy)
+            dev = x.get_device()
+            args = [a if a is None else a.data_ptr() if a.get_device() == dev else _elsewhere(a, dev)
+                    for a in (rows, offsets, self.codes, self.scales, self.bias, y)]
+            _check(B._lib.dpc_linear_i8(_raw(stream, dev), B.elem_of(x.dtype), B.elem_of(dtype), ntok, topk,
+                                        self.outer, self.inner, self.experts, x.data_ptr(), ldx, *args[:5],
+                                        ws.data_ptr(), nb, args[5], ldy), "dpc_linear_i8")
         return y

@@ -34,16 +34,15 @@ def test_plan_validates_before_launch():
 
 
 def test_rows_validate_before_launch():
-    g = dict(stream=0, elem=P.DPC_ELEM_F32, ntok=4, topk=2, width=10, x=FAKE, ldx=10, weight=None, rows=FAKE, y=FAKE,
-             ldy=10)
+    g = dict(stream=0, elem=P.DPC_ELEM_F32, ntok=4, topk=2, width=10, x=FAKE, ldx=10, weight=None, rows=FAKE,
+             pos=FAKE, y=FAKE, ldy=10)
     common = [(dict(ntok=-1), B.DPC_EINVAL), (dict(topk=0), B.DPC_EINVAL), (dict(topk=65), B.DPC_ENOTSUP),
               (dict(width=0), B.DPC_EINVAL), (dict(ntok=1 << 30), B.DPC_ENOTSUP), (dict(x=0), B.DPC_EINVAL),
               (dict(x=FAKE + 2), B.DPC_EINVAL), (dict(ldx=9), B.DPC_EINVAL), (dict(weight=FAKE + 2), B.DPC_EINVAL),
               (dict(elem=7), B.DPC_EINVAL)]
     _refused(P.dpc_route_gather, g, common + [(dict(ldy=9), B.DPC_EINVAL), (dict(y=0), B.DPC_EINVAL),
-                                              (dict(rows=0), B.DPC_EINVAL)])
+                                              (dict(rows=0), B.DPC_EINVAL), (dict(pos=0), B.DPC_EINVAL)])
     c = {k: v for k, v in g.items() if k != "rows"}
-    c["pos"] = FAKE
     _refused(P.dpc_route_combine, c, common + [(dict(ldy=9), B.DPC_EINVAL), (dict(y=0), B.DPC_EINVAL),
                                                (dict(pos=0), B.DPC_EINVAL)])
     b = dict(stream=0, elem=P.DPC_ELEM_F64, ntok=4, topk=2, width=10, x=FAKE, ldx=10, weight=FAKE, rows=FAKE, pos=FAKE,
@@ -53,7 +52,7 @@ def test_rows_validate_before_launch():
         (dict(lddy=9), B.DPC_EINVAL), (dict(lddx=9), B.DPC_EINVAL), (dict(dweight=FAKE + 4), B.DPC_EINVAL),
         (dict(rows=0), B.DPC_EINVAL), (dict(pos=0), B.DPC_EINVAL), (dict(elem=-1), B.DPC_EINVAL)])
     # no tokens: no-ops
-    P.dpc_route_gather(**{**g, "ntok": 0, "x": 0, "y": 0, "rows": 0})
+    P.dpc_route_gather(**{**g, "ntok": 0, "x": 0, "y": 0, "rows": 0, "pos": 0})
     P.dpc_route_combine(**{**c, "ntok": 0, "x": 0, "y": 0, "pos": 0})
     P.dpc_route_combine_bwd(**{**b, "ntok": 0, "x": 0, "dy": 0, "rows": 0, "pos": 0})
 
@@ -98,9 +97,9 @@ def test_binding_refuses_wrong_tensors():
     f32 = lambda *s: torch.zeros(s)
     i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
     with pytest.raises(ValueError, match="x holds"):
-        P.dpc_route_gather(0, P.DPC_ELEM_F32, 4, 2, 10, f32(39), 10, None, FAKE, FAKE, 10)
+        P.dpc_route_gather(0, P.DPC_ELEM_F32, 4, 2, 10, f32(39), 10, None, FAKE, FAKE, FAKE, 10)
     with pytest.raises(ValueError, match="y holds"):
-        P.dpc_route_gather(0, P.DPC_ELEM_F32, 4, 2, 10, FAKE, 10, None, FAKE, f32(79), 10)
+        P.dpc_route_gather(0, P.DPC_ELEM_F32, 4, 2, 10, FAKE, 10, None, FAKE, FAKE, f32(79), 10)
     with pytest.raises(TypeError, match="x has dtype"):
         P.dpc_route_combine(0, P.DPC_ELEM_F16, 4, 2, 10, f32(80), 10, None, FAKE, FAKE, 10)
     with pytest.raises(ValueError, match="GPU"):
