@@ -25,6 +25,19 @@ struct Chunk {
   T v[kElems];
   __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(v, p, 16); }
   __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, v, 16); }
+  // for rows that no cache would hold until they are used again; p is 16-byte aligned
+  __device__ __forceinline__ void load_once(const T* p) {
+    const u4 w = __builtin_nontemporal_load(reinterpret_cast<const u4*>(p));
+    __builtin_memcpy(v, &w, 16);
+  }
+  __device__ __forceinline__ void store_once(T* p) const {
+    u4 w;
+    __builtin_memcpy(&w, v, 16);
+    __builtin_nontemporal_store(w, reinterpret_cast<u4*>(p));
+  }
+
+ private:
+  typedef unsigned u4 __attribute__((ext_vector_type(4)));
 };
 
 inline size_t elem_size(dpc_elem e) { return e == DPC_ELEM_F64 ? 8 : e == DPC_ELEM_F32 ? 4 : 2; }

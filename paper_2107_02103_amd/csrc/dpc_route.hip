@@ -245,6 +245,14 @@ struct Shape {
   int lanes_log2;  // lanes of a row
 };
 
+// Rows of 192 MiB and more (with their addresses and strides multiples of 16
+// bytes) are read and written past the caches: they would not be found there
+// by the call that uses them next.  Gather, combine and its gradient in a row:
+//   rows of 67 MB  68 us, past the caches 87;  105 MB 129 and 142;
+//   rows of 268 MB 284 us, past the caches 253;  319 MB 410 and 393.
+// Unaligned rows share cache lines between chunks (134 MB 146 us, 172).
+constexpr int64_t kOnceBytes = (int64_t)192 << 20;
+
 constexpr int kBlock = 256;
 
 // weight times an element: a product in the type of sums, rounded to it before it
@@ -257,7 +265,7 @@ __device__ __forceinline__ T times(typename ElemAcc<T>::type w, T v) {
   return (T)p;
 }
 
-template <typename T, bool WEIGHT>
+template <typename T, bool WEIGHT, bool ONCE>
 __global__ __launch_bounds__(kBlock) void combine_kernel(Shape sh, const T* __restrict__ x, int64_t ldx,
                                                          const typename ElemAcc<T>::type* __restrict__ weight,
                                                          const int* __restrict__ pos, T* __restrict__ y, int64_t ldy) {
@@ -291,7 +299,9 @@ __global__ __launch_bounds__(kBlock) void combine_kernel(Shape sh, const T* __re
         const int r = pt[j];
         if ((unsigned)r >= (unsigned)sh.nslot) continue;
         Chunk<T> ch;
-        ch.load(x + (int64_t)r * ldx + at);
+        const T* px = x + (int64_t)r * ldx + at;
+        if (ONCE) ch.load_once(px);
+        else ch.load(px);
         const A w = WEIGHT ? weight[t * sh.topk + j] : (A)1;
 #pragma unroll
         for (int i = 0; i < VE; ++i) acc[i] += WEIGHT ? w * (A)ch.v[i] : (A)ch.v[i];
@@ -299,7 +309,8 @@ __global__ __launch_bounds__(kBlock) void combine_kernel(Shape sh, const T* __re
       Chunk<T> out;
 #pragma unroll
       for (int i = 0; i < VE; ++i) out.v[i] = (T)acc[i];
-      out.store(py + at);
+      if (ONCE) out.store_once(py + at);
+      else out.store(py + at);
     }
   }
 }
@@ -307,7 +318,7 @@ __global__ __launch_bounds__(kBlock) void combine_kernel(Shape sh, const T* __re
 // Sends dy to the rows of its token (times their weights), and with DOT takes
 // the dot product of each row with it.  Token by token, J of a token's rows at
 // a time: a token's dy is read from memory once, whatever its number of rows.
-template <typename T, bool WEIGHT, bool DOT, int J>
+template <typename T, bool WEIGHT, bool DOT, int J, bool ONCE>
 __global__ __launch_bounds__(kBlock) void send_kernel(
     Shape sh, const T* __restrict__ x, int64_t ldx, const typename ElemAcc<T>::type* __restrict__ weight,
     const int* __restrict__ rows, const int* __restrict__ pos, const T* __restrict__ dy, int64_t lddy,
@@ -356,7 +367,11 @@ __global__ __launch_bounds__(kBlock) void send_kernel(
           if (DOT) {
 #pragma unroll
             for (int j = 0; j < J; ++j)
-              if (live[j]) v[j].load(x + (int64_t)r[j] * ldx + at);
+              if (live[j]) {
+                const T* px = x + (int64_t)r[j] * ldx + at;
+                if (ONCE) v[j].load_once(px);
+                else v[j].load(px);
+              }
 #pragma unroll
             for (int j = 0; j < J; ++j) {
               if (!live[j]) continue;
@@ -377,7 +392,9 @@ __global__ __launch_bounds__(kBlock) void send_kernel(
 #pragma unroll
                 for (int k = 0; k < VE; ++k) out.v[k] = times<T>(w[j], d.v[k]);
               }
-              out.store(dx + (int64_t)r[j] * lddx + at);
+              T* px = dx + (int64_t)r[j] * lddx + at;
+              if (ONCE) out.store_once(px);
+              else out.store(px);
             }
           }
         }
@@ -421,32 +438,48 @@ int row_shape(dpc_elem elem, int ntok, int topk, int width, Shape* sh) {
   return DPC_OK;
 }
 
+// whether the chunks of all rows start at multiples of 16 bytes
+bool chunks_aligned(dpc_elem elem, const Shape& sh, const void* a, int64_t lda, const void* b, int64_t ldb) {
+  const size_t es = elem_size(elem);
+  return sh.width * es % 16 == 0 && (!a || (elem_aligned(a, 16) && lda * es % 16 == 0)) &&
+         (!b || (elem_aligned(b, 16) && ldb * es % 16 == 0));
+}
+bool past_caches(dpc_elem elem, const Shape& sh) {
+  return sh.nslot * sh.width * (int64_t)elem_size(elem) >= kOnceBytes;
+}
+
 bool rows_ok(dpc_elem elem, const void* p, int64_t ld, int width) {
   return p && elem_aligned(p, elem_size(elem)) && ld >= width;
 }
 bool weight_ok(dpc_elem elem, const void* p) { return elem_aligned(p, elem == DPC_ELEM_F64 ? 8 : 4); }
 
-// F<T, WEIGHT>: calls f with the element type and whether there are weights
+// Calls f with the element type, whether there are weights and whether the rows
+// go past the caches
 template <typename F>
-int by_type(dpc_elem elem, bool weight, F f) {
+int by_type(dpc_elem elem, bool weight, bool once, F f) {
   (void)hipGetLastError();  // report only what this launch raises
+  const auto with = [&](auto t) {
+    if (weight) once ? f(t, std::true_type{}, std::true_type{}) : f(t, std::true_type{}, std::false_type{});
+    else once ? f(t, std::false_type{}, std::true_type{}) : f(t, std::false_type{}, std::false_type{});
+  };
   switch (elem) {
-    case DPC_ELEM_F64: weight ? f(double{}, std::true_type{}) : f(double{}, std::false_type{}); break;
-    case DPC_ELEM_F32: weight ? f(float{}, std::true_type{}) : f(float{}, std::false_type{}); break;
-    case DPC_ELEM_F16: weight ? f(_Float16{}, std::true_type{}) : f(_Float16{}, std::false_type{}); break;
-    default: weight ? f(__bf16{}, std::true_type{}) : f(__bf16{}, std::false_type{}); break;
+    case DPC_ELEM_F64: with(double{}); break;
+    case DPC_ELEM_F32: with(float{}); break;
+    case DPC_ELEM_F16: with(_Float16{}); break;
+    default: with(__bf16{}); break;
   }
   return dpc_internal_launch_status();
 }
 
 int send(void* stream, dpc_elem elem, const Shape& sh, const void* x, int64_t ldx, const void* weight, const int* rows,
          const int* pos, const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dweight) {
-  return by_type(elem, weight != nullptr, [&](auto t, auto w) {
+  const bool once = past_caches(elem, sh) && chunks_aligned(elem, sh, dweight ? x : nullptr, ldx, dx, lddx);
+  return by_type(elem, weight != nullptr, once, [&](auto t, auto w, auto o) {
     typedef decltype(t) T;
     typedef typename ElemAcc<T>::type A;
-    constexpr bool W = decltype(w)::value;
-    const auto kernel = sh.topk == 1 ? (dweight ? send_kernel<T, W, true, 1> : send_kernel<T, W, false, 1>)
-                                     : (dweight ? send_kernel<T, W, true, 4> : send_kernel<T, W, false, 4>);
+    constexpr bool W = decltype(w)::value, ONCE = decltype(o)::value;
+    const auto kernel = sh.topk == 1 ? (dweight ? send_kernel<T, W, true, 1, ONCE> : send_kernel<T, W, false, 1, ONCE>)
+                                     : (dweight ? send_kernel<T, W, true, 4, ONCE> : send_kernel<T, W, false, 4, ONCE>);
     hipLaunchKernelGGL(kernel, dim3(grid_for(sh.ntok, sh.lanes_log2)), dim3(kBlock), 0,
                        static_cast<hipStream_t>(stream), sh, (const T*)x, ldx, (const A*)weight, rows, pos,
                        (const T*)dy, lddy, (T*)dx, lddx, (A*)dweight);
@@ -519,9 +552,10 @@ extern "C" int dpc_route_combine(void* stream, dpc_elem elem, int ntok, int topk
   if (!rows_ok(elem, x, ldx, width) || !rows_ok(elem, y, ldy, width) || !weight_ok(elem, weight) || !pos ||
       !elem_aligned(pos, 4))
     return DPC_EINVAL;
-  return by_type(elem, weight != nullptr, [&](auto t, auto w) {
+  const bool once = past_caches(elem, sh) && chunks_aligned(elem, sh, x, ldx, y, ldy);
+  return by_type(elem, weight != nullptr, once, [&](auto t, auto w, auto o) {
     typedef decltype(t) T;
-    hipLaunchKernelGGL((combine_kernel<T, decltype(w)::value>), dim3(grid_for(ntok, sh.lanes_log2)), dim3(kBlock), 0,
+    hipLaunchKernelGGL((combine_kernel<T, decltype(w)::value, decltype(o)::value>), dim3(grid_for(ntok, sh.lanes_log2)), dim3(kBlock), 0,
                        static_cast<hipStream_t>(stream), sh, (const T*)x, ldx,
                        (const typename ElemAcc<T>::type*)weight, pos, (T*)y, ldy);
   });

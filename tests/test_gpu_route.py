@@ -179,6 +179,26 @@ def test_large_values_and_empty_experts():
     assert torch.allclose(dw[[n // 2, n - 1], 0].double(), want, rtol=1e-5) and int((dw != 0).sum()) == 2
 
 
+@pytest.mark.parametrize("t", ["f64", "f32", "bf16"])
+def test_rows_past_the_caches(t):
+    # over 192 MiB of aligned rows take another way than the same rows one element further apart
+    import paper_2107_02103_amd as P
+    n, k, W = (201 << 20) // 4 // 4096 // TYPES[t].itemsize, 4, 4096
+    rng = np.random.default_rng(8)
+    e = _choices(rng, n, k, 6)
+    r = P.Route(torch.from_numpy(e).cuda(), 6)
+    wt = torch.float64 if t == "f64" else torch.float32
+    w = torch.randn((n, k), device="cuda", dtype=wt)
+    x = torch.randn((n, W), device="cuda").to(TYPES[t])
+    z = torch.randn((n * k, W), device="cuda").to(TYPES[t])
+    apart = torch.zeros((n * k, W + 1), device="cuda", dtype=TYPES[t])[:, :W]
+    apart.copy_(z)
+    assert torch.equal(r.combine(z, w), r.combine(apart, w))
+    assert torch.equal(r.gather(x, w), r.gather(x, w, out=torch.zeros((n * k, W + 1), device="cuda", dtype=TYPES[t])[:, :W]))
+    (a, b), (c, d) = r.combine_backward(z, x, w), r.combine_backward(apart, x, w)
+    assert torch.equal(a, c) and torch.equal(b, d) and torch.equal(a, r.gather(x, w))
+
+
 def test_another_stream_and_repeats():
     import paper_2107_02103_amd as P
     rng = np.random.default_rng(5)
