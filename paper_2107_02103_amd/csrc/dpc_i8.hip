@@ -216,11 +216,15 @@ __device__ __forceinline__ int token_of(const Product& p, int r) {
   return (unsigned)s < (unsigned)p.m ? (int)((unsigned)s / (unsigned)p.topk) : -1;
 }
 
+// One result from its sum: in float64, where neither scale nor their product
+// leaves the range, rounded to float32 and from there to 16 bits.
 template <typename TY>
 __device__ __forceinline__ TY scaled(int acc, double sx, float sw, float bias) {
-  const double v = (double)acc * sx * (double)sw + (double)bias;
+  const double v = fma((double)acc, sx * (double)sw, (double)bias);
   if constexpr (sizeof(TY) == 8) return v;
-  return (TY)(float)v;
+  float f = (float)v;
+  if constexpr (sizeof(TY) == 2) asm("" : "+v"(f));  // two roundings: one from float64 takes eight instructions
+  return (TY)f;
 }
 
 // One wavefront makes 16 rows times 16 channels of y, operands straight from
@@ -258,8 +262,212 @@ __global__ __launch_bounds__(64) void product_kernel(Product p, TY* __restrict__
   }
 }
 
+// Tiles of BM rows times BN channels, K in steps of 128 bytes: both operands
+// go from memory to LDS without passing registers, the next step's while the
+// matrix cores work on this one's.  A row of a step is 8 chunks of 16 bytes;
+// chunk c of row r lies in slot c ^ (r & 7), so that the lanes of one LDS read
+// (16 rows, the same chunk) meet all banks.  WM x WN wavefronts.
+typedef const __attribute__((address_space(1))) void* GlobalPtr;
+typedef __attribute__((address_space(3))) void* LdsPtr;
+
+template <typename TY, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, int row_tiles, int col_tiles,
+                                                                     TY* __restrict__ y, int64_t ldy, bool fours) {
+  constexpr int kWaves = WM * WN, TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
+  constexpr int kStep = 128, kRows = BM + BN;
+  constexpr int kLoads = kRows / 8 / kWaves;  // 8 rows each
+  static_assert(kLoads * kWaves * 8 == kRows, "every load takes 8 rows");
+  __shared__ __attribute__((aligned(16))) int8_t lds[2][kRows * kStep];
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave % WM, wn = wave / WM;
+
+  // consecutive workgroups go to different XCDs: each XCD gets a run of tiles
+  // of its own, in bands of 8 row tiles, so that its L2 serves tiles that share rows
+  const int total = row_tiles * col_tiles, per = (total + 7) / 8;
+  const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || id >= total) return;
+  const int band = id / (8 * col_tiles), in = id - band * 8 * col_tiles;
+  const int high = min(8, row_tiles - band * 8);
+  const int ct = in / high, rt = band * 8 + in % high;
+
+  const Tile t = find_tile(p, BM, rt);
+  if (t.row0 >= t.end) return;
+  const int c0 = ct * BN;
+
+  if (t.group < 0) {  // rows of no expert
+    const int high_rows = t.end - t.row0, wide = min(BN, p.n - c0);
+    for (int e = threadIdx.x; e < high_rows * wide; e += 64 * kWaves)
+      y[(int64_t)(t.row0 + e / wide) * ldy + c0 + e % wide] = (TY)0;
+    return;
+  }
+
+  v4i acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = v4i{0, 0, 0, 0};
+
+  // this lane's rows of the loads: x rows first, then rows of W
+  const int8_t* src[kLoads];
+  int dst[kLoads];
+#pragma unroll
+  for (int l = 0; l < kLoads; ++l) {
+    const int r8 = (wave * kLoads + l) * 8, r = r8 + (lane >> 3);
+    const int chunk = (lane & 7) ^ (r & 7);
+    const int8_t* row;
+    if (r < BM) {
+      const int tok = token_of(p, min(t.row0 + r, t.end - 1));
+      row = p.qx + (int64_t)(tok < 0 ? 0 : tok) * p.ld;
+    } else {
+      row = p.qw + ((int64_t)t.group * p.n + min(c0 + r - BM, p.n - 1)) * p.ld;
+    }
+    src[l] = row + chunk * 16;
+    dst[l] = r8 * kStep;
+  }
+  auto fetch = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+      __builtin_amdgcn_global_load_lds((GlobalPtr)src[l], (LdsPtr)(&lds[buf][dst[l]]), 16, 0, 0);
+      src[l] += kStep;
+    }
+  };
+  const int steps = p.ld / kStep;
+  fetch(0);
+  for (int s = 0; s < steps; ++s) {
+    // vmcnt(0), lgkmcnt(0): this step's rows are in LDS, the step before has
+    // been read; the barrier says so for every wavefront
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (s + 1 < steps) fetch((s + 1) & 1);
+    const int8_t* xs = &lds[s & 1][wm * TM * kStep];
+    const int8_t* ws = &lds[s & 1][(BM + wn * TN) * kStep];
+    v4i a[2][NI], b[2][MI];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int slot = ((k * 4 + quad) ^ (l16 & 7)) * 16;
+#pragma unroll
+      for (int j = 0; j < NI; ++j) a[k][j] = *reinterpret_cast<const v4i*>(ws + (j * 16 + l16) * kStep + slot);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) b[k][i] = *reinterpret_cast<const v4i*>(xs + (i * 16 + l16) * kStep + slot);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[k][j], b[k][i], acc[i][j], 0, 0, 0);
+    // LDS reads of the second half between the products of the first: one after
+    // every other product (left alone, the reads come in clumps with a wait
+    // behind each; 8192 x 8192 x 8192: 530 -> 513 us)
+    constexpr int kReads = NI + MI, kSpaced = 2 * kReads <= MI * NI ? 2 : 1;
+    __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+#pragma unroll
+    for (int q = 0; q < kReads; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, kSpaced, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 2 * MI * NI - kSpaced * kReads, 0);
+    asm volatile("" ::: "memory");
+  }
+
+  // this lane's results: row l16 of each row tile, channels 4 quad .. 4 quad + 3 of each channel tile
+  const int first = c0 + wn * TN + quad * 4;
+  float sw[NI][4], bias[NI][4];
+  const float* psw = p.sw + (int64_t)t.group * p.n;
+  const float* pbias = p.bias ? p.bias + (int64_t)t.group * p.n : psw;
+  if (fours) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int c = min(first + j * 16, p.n - 4);
+      __builtin_memcpy(sw[j], psw + c, 16);
+      __builtin_memcpy(bias[j], pbias + c, 16);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = min(first + j * 16 + q, p.n - 1);
+        sw[j][q] = psw[c];
+        bias[j][q] = pbias[c];
+      }
+  }
+  if (!p.bias) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) bias[j][q] = 0.0f;
+  }
+  int tok[MI];
+  float sx[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) tok[i] = token_of(p, min(t.row0 + wm * TM + i * 16 + l16, t.end - 1));
+#pragma unroll
+  for (int i = 0; i < MI; ++i) sx[i] = p.sx[max(tok[i], 0)];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int r = t.row0 + wm * TM + i * 16 + l16;
+    TY* py = y + (int64_t)r * ldy + first;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      TY out[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        out[q] = scaled<TY>(acc[i][j][q], (double)sx[i], sw[j][q], bias[j][q]);
+        if (tok[i] < 0) out[q] = (TY)0;  // a row of the group that no slot owns
+      }
+      const int left = r < t.end ? p.n - (first + j * 16) : 0;
+      if (fours) {
+        if (left > 0) __builtin_memcpy(__builtin_assume_aligned(py + j * 16, 4 * sizeof(TY) < 16 ? 4 * sizeof(TY) : 16), out, 4 * sizeof(TY));
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (q < left) py[j * 16 + q] = out[q];
+      }
+    }
+  }
+}
+
+template <typename TY, int BM, int BN, int WM, int WN>
+void launch_tiled(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
+  const int row_tiles = (int)most_tiles(p, BM), col_tiles = (p.n + BN - 1) / BN;
+  // four channels at a time: rows of y, scales and biases of every group start at multiples of four
+  const bool fours = elem_aligned(y, 4 * sizeof(TY) < 16 ? 4 * sizeof(TY) : 16) && ldy % 4 == 0 && p.n % 4 == 0;
+  const unsigned per = ((unsigned)row_tiles * (unsigned)col_tiles + 7) / 8;
+  hipLaunchKernelGGL((product_tiled_kernel<TY, BM, BN, WM, WN>), dim3(per * 8), dim3(64 * WM * WN), 0, s, p, row_tiles,
+                     col_tiles, y, ldy, fours);
+}
+
+// Time of the tiled product: a fixed part, and for each step of K the larger of
+// one tile's time alone and the time of the tiles of a CU one after the other.
+// Measured on 256 CUs (us, bf16 results; 256x256, 128x128, 128x64, 64x64 tiles):
+//   4096 x 4096 x 4096   76.8  87.5 106.8 124.4     1024 x 8192 x 4096  54.0 39.0 48.7 55.7
+//   2048 x 2048 x 2048   32.4  16.4  14.4  17.4     32000 x 240 x 1600  28.8 21.9 26.1 26.8
+//   512 x 4096 x 4096    50.3  23.6  19.8  18.2     16000 x 240 x 1600  25.6 14.6 13.2 14.9
+//   256 x 4096 x 4096    50.3  21.5  14.4  11.4     4000 x 240 x 1600   24.4 12.1  8.3  6.8
+double tiled_cost(const Product& p, int bm, int bn, double fixed, double alone, double each) {
+  const int64_t tiles = most_tiles(p, bm) * ((p.n + bn - 1) / bn);
+  const double cu = each * (double)((tiles + 255) / 256);
+  return fixed + p.ld / 128 * (alone > cu ? alone : cu);
+}
+
 template <typename TY>
 void launch_product(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
+  // rows that share an expert's weights, at most: few of them go straight
+  // through the matrix cores, more through LDS in the tile that a model of the
+  // time (microseconds, from the shapes measured) takes for the fastest
+  const int64_t shared = p.offsets ? ((int64_t)p.m + p.ngroup - 1) / p.ngroup : p.m;
+  if (shared > 16) {
+    const double big = tiled_cost(p, 256, 256, 8.0, 1.35, 2.1), mid = tiled_cost(p, 128, 128, 5.0, 0.7, 0.6),
+                 low = tiled_cost(p, 128, 64, 4.0, 0.5, 0.35), small = tiled_cost(p, 64, 64, 3.3, 0.25, 0.22);
+    if (big <= mid && big <= low && big <= small) return launch_tiled<TY, 256, 256, 2, 4>(s, p, y, ldy);
+    if (mid <= low && mid <= small) return launch_tiled<TY, 128, 128, 2, 2>(s, p, y, ldy);
+    if (low <= small) return launch_tiled<TY, 128, 64, 2, 2>(s, p, y, ldy);
+    return launch_tiled<TY, 64, 64, 2, 2>(s, p, y, ldy);
+  }
   const int64_t tiles = most_tiles(p, 16);
   const unsigned gy = (unsigned)(tiles < 32768 ? tiles : 32768);
   hipLaunchKernelGGL((product_kernel<TY>), dim3((p.n + 15) / 16, gy, (unsigned)((tiles + gy - 1) / gy)), dim3(64), 0, s,
