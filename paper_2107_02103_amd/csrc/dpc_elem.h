@@ -25,7 +25,7 @@ struct Chunk {
   T v[kElems];
   __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(v, p, 16); }
   __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, v, 16); }
-  // for rows that no cache would hold until they are used again; p is 16-byte aligned
+  // past the caches, for what is not used again before they would have lost it
   __device__ __forceinline__ void load_once(const T* p) {
     const u4 w = __builtin_nontemporal_load(reinterpret_cast<const u4*>(p));
     __builtin_memcpy(v, &w, 16);
@@ -37,7 +37,7 @@ struct Chunk {
   }
 
  private:
-  typedef unsigned u4 __attribute__((ext_vector_type(4)));
+  typedef unsigned u4 __attribute__((ext_vector_type(4), aligned(2)));  // of its elements, at least
 };
 
 inline size_t elem_size(dpc_elem e) { return e == DPC_ELEM_F64 ? 8 : e == DPC_ELEM_F32 ? 4 : 2; }

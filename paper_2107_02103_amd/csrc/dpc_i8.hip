@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "dpc.h"
 #include "dpc_elem.h"
@@ -36,6 +37,39 @@ __device__ __forceinline__ void codes_of(const float* v, float u, int8_t* q) {
     b[i] = (unsigned char)__float_as_uint(p + 12582912.0f);
   }
   __builtin_memcpy(__builtin_assume_aligned(q, VE), b, VE);
+}
+
+// The largest magnitude of floats, as bits: as whole numbers magnitudes keep
+// their order, with NaN the largest.  Of the bits with their signs, the largest
+// signed number is the largest positive value, the largest unsigned one the
+// largest negative value (or a positive one, if there is no negative).
+struct Largest {
+  int pos = 0;
+  unsigned neg = 0;
+  __device__ __forceinline__ void take(float v) {
+    pos = max(pos, __float_as_int(v));
+    neg = max(neg, __float_as_uint(v));
+  }
+  __device__ __forceinline__ unsigned bits() const { return max((unsigned)pos, neg & 0x7fffffffu); }
+};
+
+// The largest of a wavefront's values, for all of them.
+__device__ __forceinline__ unsigned wave_max(unsigned v) {
+  v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));  // row_shr:1
+  v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
+  v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
+  v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
+  v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));  // row_bcast:15
+  v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));  // row_bcast:31
+  return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// Scale and inverse of a row whose largest magnitude has the bits `top`.
+__device__ __forceinline__ void scale_of(unsigned top, float* scale, float* inverse) {
+  const float a = __uint_as_float(top);
+  const bool finite = top < 0x7f800000u, live = finite && a >= 0x1p-100f;
+  *inverse = live ? 127.0f / a : 0.0f;
+  *scale = live ? a / 127.0f : finite ? 0.0f : __builtin_nanf("");
 }
 
 // LANES lanes of a row (up to 64: several rows in a wavefront; 256: a whole
@@ -95,10 +129,10 @@ __global__ __launch_bounds__(256) void quant_kernel(int nrows, int ncols, const 
       top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
     }
     if (!in) continue;
-    const float a = __uint_as_float(top);
-    const bool finite = top < 0x7f800000u, live = finite && a >= 0x1p-100f;
-    const float u = live ? 127.0f / a : 0.0f;
-    if (lane == 0) scale[r] = live ? a / 127.0f : finite ? 0.0f : __builtin_nanf("");
+    const bool finite = top < 0x7f800000u;
+    float row_scale, u;
+    scale_of(top, &row_scale, &u);
+    if (lane == 0) scale[r] = row_scale;
     int8_t* pq = q + r * ld;
     auto put = [&](int c, float* v) __attribute__((always_inline)) {
       if (!finite)
@@ -227,39 +261,162 @@ __device__ __forceinline__ TY scaled(int acc, double sx, float sw, float bias) {
   return (TY)f;
 }
 
-// One wavefront makes 16 rows times 16 channels of y, operands straight from
-// memory.
-template <typename TY>
-__global__ __launch_bounds__(64) void product_kernel(Product p, TY* __restrict__ y, int64_t ldy) {
+// 16 rows of 64 bytes, loaded with the 4 chunks of a row in neighbouring lanes,
+// to the lanes of a product's operand: row l % 16, chunk l / 16.  (Loaded in
+// those lanes at once, every lane of a load meets another cache line than its
+// neighbours, and the cache's tags take four times as long.)
+__device__ __forceinline__ v4i to_rows(v4i w) {
+  const int lane = threadIdx.x & 63, from = ((lane & 15) * 4 + (lane >> 4)) * 4;
+  v4i r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ds_bpermute(from, w[i]);
+  return r;
+}
+
+// Few rows: 16 rows times 16 channels of y for each workgroup, whose 8
+// wavefronts share K (step s is wavefront s % 8's) and whose sums are added in
+// LDS.  W is read once, 8 KiB of it under way in every wavefront: bound by that
+// read, or for short rows by latency.  TX is the type of rows that the workgroup
+// codes itself (into LDS), or int8_t for rows that are codes already.
+constexpr int kFewWaves = 8, kFewAhead = 4;
+
+template <typename TX, typename TY>
+__global__ __launch_bounds__(64 * kFewWaves) void few_product_kernel(Product p, const TX* __restrict__ x, int64_t ldx,
+                                                                     TY* __restrict__ y, int64_t ldy) {
+  constexpr bool kCoded = sizeof(TX) == 1;
+  extern __shared__ __attribute__((aligned(16))) int8_t codes[];  // 16 rows of codes, if they are made here
+  __shared__ int sums[kFewWaves][256];
+  __shared__ float scales[16];
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Tile t = find_tile(p, 16, blockIdx.y + gridDim.y * blockIdx.z);
   if (t.row0 >= t.end) return;
-  const int r = t.row0 + l16, c0 = blockIdx.x * 16;
-  const int tok = r < t.end && t.group >= 0 ? token_of(p, r) : -1;
-  v4i acc = {0, 0, 0, 0};
-  if (t.group >= 0) {
-    const int8_t* px = p.qx + (int64_t)(tok < 0 ? 0 : tok) * p.ld + quad * 16;
-    const int cw = min(c0 + l16, p.n - 1);
-    const int8_t* pw = p.qw + ((int64_t)t.group * p.n + cw) * p.ld + quad * 16;
-    for (int k = 0; k < p.ld; k += 64) {
-      const v4i a = *reinterpret_cast<const v4i*>(pw + k);
-      const v4i b = *reinterpret_cast<const v4i*>(px + k);
-      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc, 0, 0, 0);
-    }
-  }
-  if (r >= t.end) return;
-  const double sx = tok < 0 ? 0.0 : (double)p.sx[tok];
+  const int c0 = blockIdx.x * 16, steps = p.ld / 128, group = max(t.group, 0);
+  const int8_t* pw = p.qw + ((int64_t)group * p.n + min(c0 + (lane >> 2), p.n - 1)) * p.ld + (lane & 3) * 16;
+  const int mine = t.group < 0 ? -1 : token_of(p, min(t.row0 + (lane >> 2), t.end - 1));
+  const int8_t* pq = kCoded ? (const int8_t*)x + (int64_t)max(mine, 0) * p.ld + (lane & 3) * 16 : nullptr;
+  v4i w[kFewAhead][2], q[kFewAhead][2];
+  auto fetch = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = c0 + quad * 4 + i;
-    if (c >= p.n) break;
-    TY out = (TY)0;
-    if (tok >= 0) {
-      const int64_t gc = (int64_t)t.group * p.n + c;
-      out = scaled<TY>(acc[i], sx, p.sw[gc], p.bias ? p.bias[gc] : 0.0f);
+    for (int u = 0; u < kFewAhead; ++u) {
+      const int s = min(s0 + u * kFewWaves, steps - 1);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        w[u][k] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(pw + s * 128 + k * 64));
+        if (kCoded) q[u][k] = *reinterpret_cast<const v4i*>(pq + s * 128 + k * 64);
+      }
     }
-    y[(int64_t)r * ldy + c] = out;
+  };
+  fetch(wave);
+  if constexpr (!kCoded) {
+    constexpr int VE = Chunk<TX>::kElems;
+    for (int row = wave; row < 16; row += kFewWaves) {
+      if (t.row0 + row >= t.end) break;
+      const int tok = __builtin_amdgcn_readfirstlane(t.group < 0 ? -1 : token_of(p, t.row0 + row));
+      const TX* px = x + (int64_t)max(tok, 0) * ldx;
+      auto element = [&](int i) { return i < p.k ? (float)px[i] : 0.0f; };
+      Largest most;
+      for (int c = lane * VE; c < p.k; c += 64 * VE) {
+        if (c + VE <= p.k) {
+          Chunk<TX> ch;
+          ch.load(px + c);
+#pragma unroll
+          for (int e = 0; e < VE; ++e) most.take((float)ch.v[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) most.take(element(c + e));
+        }
+      }
+      const unsigned top = wave_max(most.bits());
+      const bool finite = top < 0x7f800000u;
+      float scale, u;
+      scale_of(top, &scale, &u);
+      if (lane == 0) scales[row] = scale;
+      for (int c = lane * VE; c < p.ld; c += 64 * VE) {
+        float v[VE];
+        if (c + VE <= p.k) {
+          Chunk<TX> ch;
+          ch.load(px + c);
+#pragma unroll
+          for (int e = 0; e < VE; ++e) v[e] = finite ? (float)ch.v[e] : 0.0f;
+        } else {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) v[e] = finite ? element(c + e) : 0.0f;
+        }
+        codes_of<VE>(v, u, codes + row * p.ld + (c ^ ((row & 7) << 4)));
+      }
+    }
+    __syncthreads();
   }
+  const int high = min(t.end - t.row0, 16) - 1;  // rows of the tile past its end repeat its last one
+  v4i acc = {0, 0, 0, 0};
+  for (int s0 = wave; s0 < steps; s0 += kFewWaves * kFewAhead) {
+#pragma unroll
+    for (int u = 0; u < kFewAhead; ++u) {
+      const int s = s0 + u * kFewWaves;
+      if (s >= steps) break;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        v4i b;
+        if constexpr (kCoded) {
+          b = to_rows(q[u][k]);
+        } else {
+          const int row = min(l16, high);
+          b = *reinterpret_cast<const v4i*>(codes + row * p.ld + s * 128 + (((k * 4 + quad) ^ (row & 7)) << 4));
+        }
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(to_rows(w[u][k]), b, acc, 0, 0, 0);
+      }
+    }
+    if (s0 + kFewWaves * kFewAhead < steps) fetch(s0 + kFewWaves * kFewAhead);
+  }
+  // this lane: row l16, channels 4 quad .. 4 quad + 3
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sums[wave][l16 * 16 + quad * 4 + i] = acc[i];
+  __syncthreads();
+  if (threadIdx.x >= 256) return;
+  const int row = threadIdx.x >> 4, c = c0 + (threadIdx.x & 15), r = t.row0 + row;
+  if (r >= t.end || c >= p.n) return;
+  int sum = 0;
+#pragma unroll
+  for (int v = 0; v < kFewWaves; ++v) sum += sums[v][threadIdx.x];
+  const int tok = t.group < 0 ? -1 : token_of(p, r);
+  TY out = (TY)0;
+  if (tok >= 0) {
+    const int64_t gc = (int64_t)group * p.n + c;
+    out = scaled<TY>(sum, (double)(kCoded ? p.sx[tok] : scales[row]), p.sw[gc], p.bias ? p.bias[gc] : 0.0f);
+  }
+  y[(int64_t)r * ldy + c] = out;
+}
+
+// Whether at most 16 rows share an expert's weights, on average.
+inline bool few_rows(const Product& p) {
+  return (p.offsets ? ((int64_t)p.m + p.ngroup - 1) / p.ngroup : p.m) <= 16;
+}
+
+template <typename TX, typename TY>
+void launch_few(hipStream_t s, const Product& p, const TX* x, int64_t ldx, TY* y, int64_t ldy) {
+  const int64_t tiles = most_tiles(p, 16);
+  const unsigned gy = (unsigned)(tiles < 32768 ? tiles : 32768);
+  hipLaunchKernelGGL((few_product_kernel<TX, TY>), dim3((p.n + 15) / 16, gy, (unsigned)((tiles + gy - 1) / gy)),
+                     dim3(64 * kFewWaves), sizeof(TX) == 1 ? 0 : (size_t)(p.m < 16 ? p.m : 16) * p.ld, s, p, x, ldx, y, ldy);
+}
+
+// Four consecutive results of a row, of which `left` exist; fours: all or none
+// of them do, and their address is a multiple of their size (up to 16 bytes).
+template <typename TY>
+__device__ __forceinline__ void put4(TY* p, const TY* v, int left, bool fours) {
+  if (fours) {
+    if (left > 0) __builtin_memcpy(__builtin_assume_aligned(p, 4 * sizeof(TY) < 16 ? 4 * sizeof(TY) : 16), v, 4 * sizeof(TY));
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (q < left) p[q] = v[q];
+}
+
+template <typename TY>
+bool in_fours(const Product& p, const TY* y, int64_t ldy) {
+  return elem_aligned(y, 4 * sizeof(TY) < 16 ? 4 * sizeof(TY) : 16) && ldy % 4 == 0 && p.n % 4 == 0;
 }
 
 // Tiles of BM rows times BN channels, K in steps of 128 bytes: both operands
@@ -420,13 +577,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
         if (tok[i] < 0) out[q] = (TY)0;  // a row of the group that no slot owns
       }
       const int left = r < t.end ? p.n - (first + j * 16) : 0;
-      if (fours) {
-        if (left > 0) __builtin_memcpy(__builtin_assume_aligned(py + j * 16, 4 * sizeof(TY) < 16 ? 4 * sizeof(TY) : 16), out, 4 * sizeof(TY));
-      } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (q < left) py[j * 16 + q] = out[q];
-      }
+      put4(py + j * 16, out, left, fours);
     }
   }
 }
@@ -434,11 +585,9 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
 template <typename TY, int BM, int BN, int WM, int WN>
 void launch_tiled(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
   const int row_tiles = (int)most_tiles(p, BM), col_tiles = (p.n + BN - 1) / BN;
-  // four channels at a time: rows of y, scales and biases of every group start at multiples of four
-  const bool fours = elem_aligned(y, 4 * sizeof(TY) < 16 ? 4 * sizeof(TY) : 16) && ldy % 4 == 0 && p.n % 4 == 0;
   const unsigned per = ((unsigned)row_tiles * (unsigned)col_tiles + 7) / 8;
   hipLaunchKernelGGL((product_tiled_kernel<TY, BM, BN, WM, WN>), dim3(per * 8), dim3(64 * WM * WN), 0, s, p, row_tiles,
-                     col_tiles, y, ldy, fours);
+                     col_tiles, y, ldy, in_fours(p, y, ldy));
 }
 
 // Time of the tiled product: a fixed part, and for each step of K the larger of
@@ -456,22 +605,13 @@ double tiled_cost(const Product& p, int bm, int bn, double fixed, double alone, 
 
 template <typename TY>
 void launch_product(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
-  // rows that share an expert's weights, at most: few of them go straight
-  // through the matrix cores, more through LDS in the tile that a model of the
-  // time (microseconds, from the shapes measured) takes for the fastest
-  const int64_t shared = p.offsets ? ((int64_t)p.m + p.ngroup - 1) / p.ngroup : p.m;
-  if (shared > 16) {
-    const double big = tiled_cost(p, 256, 256, 8.0, 1.35, 2.1), mid = tiled_cost(p, 128, 128, 5.0, 0.7, 0.6),
-                 low = tiled_cost(p, 128, 64, 4.0, 0.5, 0.35), small = tiled_cost(p, 64, 64, 3.3, 0.25, 0.22);
-    if (big <= mid && big <= low && big <= small) return launch_tiled<TY, 256, 256, 2, 4>(s, p, y, ldy);
-    if (mid <= low && mid <= small) return launch_tiled<TY, 128, 128, 2, 2>(s, p, y, ldy);
-    if (low <= small) return launch_tiled<TY, 128, 64, 2, 2>(s, p, y, ldy);
-    return launch_tiled<TY, 64, 64, 2, 2>(s, p, y, ldy);
-  }
-  const int64_t tiles = most_tiles(p, 16);
-  const unsigned gy = (unsigned)(tiles < 32768 ? tiles : 32768);
-  hipLaunchKernelGGL((product_kernel<TY>), dim3((p.n + 15) / 16, gy, (unsigned)((tiles + gy - 1) / gy)), dim3(64), 0, s,
-                     p, y, ldy);
+  if (few_rows(p)) return launch_few(s, p, p.qx, 0, y, ldy);
+  const double big = tiled_cost(p, 256, 256, 8.0, 1.35, 1.9), mid = tiled_cost(p, 128, 128, 5.0, 0.7, 0.64),
+               low = tiled_cost(p, 128, 64, 4.0, 0.5, 0.35), small = tiled_cost(p, 64, 64, 3.3, 0.25, 0.22);
+  if (big <= mid && big <= low && big <= small) return launch_tiled<TY, 256, 256, 2, 4>(s, p, y, ldy);
+  if (mid <= low && mid <= small) return launch_tiled<TY, 128, 128, 2, 2>(s, p, y, ldy);
+  if (low <= small) return launch_tiled<TY, 128, 64, 2, 2>(s, p, y, ldy);
+  return launch_tiled<TY, 64, 64, 2, 2>(s, p, y, ldy);
 }
 
 int product(hipStream_t s, dpc_elem elem_y, const Product& p, void* y, int64_t ldy) {
@@ -483,6 +623,236 @@ int product(hipStream_t s, dpc_elem elem_y, const Product& p, void* y, int64_t l
     default: launch_product(s, p, (__bf16*)y, ldy); break;
   }
   return dpc_internal_launch_status();
+}
+
+// Four results in the type of y, of which `left` exist.
+__device__ __forceinline__ void put4_as(dpc_elem elem, void* y, int64_t at, v4i acc, double sx, const float* sw,
+                                        const float* bias, bool owned, int left, bool fours) {
+  auto put = [&](auto* py) __attribute__((always_inline)) {
+    typedef std::remove_pointer_t<decltype(py)> TY;
+    TY out[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) out[q] = owned ? scaled<TY>(acc[q], sx, sw[q], bias[q]) : (TY)0;
+    put4(py + at, out, left, fours);
+  };
+  switch (elem) {
+    case DPC_ELEM_F64: put((double*)y); break;
+    case DPC_ELEM_F32: put((float*)y); break;
+    case DPC_ELEM_F16: put((_Float16*)y); break;
+    default: put((__bf16*)y); break;
+  }
+}
+
+// Codes and product in one, for layers of few channels: the codes of 32 rows
+// stay in LDS and never see memory.  Each of 8 wavefronts codes 4 rows, the next
+// one on its way while it codes one; a lane holds TURNS chunks of a row.  Then
+// wavefront w makes channels 32 w .. 32 w + 31 of each 256, with W's rows
+// straight from L2 (each of them meets all 32 rows of the workgroup at once).
+// Chunks of codes lie as in the tiles above.
+constexpr int kCodedRows = 32, kCodedLd = 2048;
+
+template <typename TX, int TURNS>
+__global__ __launch_bounds__(512, 4) void coded_product_kernel(Product p, dpc_elem elem_y, const TX* __restrict__ x,
+                                                               int64_t ldx, void* __restrict__ y, int64_t ldy,
+                                                               bool fours) {
+  constexpr int VE = Chunk<TX>::kElems, kTurn = 64 * VE, kPitch = TURNS * kTurn;
+  __shared__ __attribute__((aligned(16))) int8_t codes[kCodedRows * kPitch];
+  __shared__ float scales[kCodedRows];
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Tile t = find_tile(p, kCodedRows, blockIdx.x);
+  if (t.row0 >= t.end) return;
+
+  // elements of this lane's chunks; those that reach past the end take the row's
+  // last ones instead (no branch: one around each load would make it wait for
+  // the load before), which changes no maximum and gets the code 0 below
+  int at[TURNS];
+#pragma unroll
+  for (int h = 0; h < TURNS; ++h) at[h] = min(lane * VE + h * kTurn, p.k - VE);
+  auto row_of = [&](int a) __attribute__((always_inline)) {
+    const int tok = t.group < 0 ? -1 : token_of(p, min(t.row0 + wave * 4 + a, t.end - 1));
+    return x + (int64_t)max(__builtin_amdgcn_readfirstlane(tok), 0) * ldx;
+  };
+  auto take = [&](const TX* px, Chunk<TX> (&held)[TURNS]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < TURNS; ++h) held[h].load_once(px + (unsigned)at[h]);
+  };
+  auto code = [&](int a, const TX* px, const Chunk<TX> (&held)[TURNS]) __attribute__((always_inline)) {
+    Largest most;
+#pragma unroll
+    for (int h = 0; h < TURNS; ++h)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) most.take((float)held[h].v[e]);
+    const unsigned top = wave_max(most.bits());
+    const int row = wave * 4 + a, turn = (row & 7) << 4;
+    float scale, u;
+    scale_of(top, &scale, &u);
+    if (lane == 0) scales[row] = scale;
+    // byte b of the row, its 16-byte chunk moved among the 8 of its step
+    int8_t* to = codes + row * kPitch;
+    const bool finite = top < 0x7f800000u;
+#pragma unroll
+    for (int h = 0; h < TURNS; ++h) {
+      const float uc = lane * VE + h * kTurn + VE <= p.k ? u : 0.0f;  // whole chunks
+      float v[VE];
+#pragma unroll
+      for (int e = 0; e < VE; ++e) v[e] = finite ? (float)held[h].v[e] : 0.0f;
+      codes_of<VE>(v, uc, to + ((lane * VE) ^ turn) + h * kTurn);
+    }
+    const int rest = p.k % VE;  // elements behind the last whole chunk: over the zeros written there
+    if (rest && lane < rest) {
+      const int last = p.k - rest + lane;
+      const float v = finite ? (float)px[last] : 0.0f;
+      codes_of<1>(&v, u, to + (last ^ turn));
+    }
+  };
+  {
+    Chunk<TX> held[2][TURNS];
+    const TX *px0 = row_of(0), *px1;
+    take(px0, held[0]);
+    px1 = row_of(1);
+    take(px1, held[1]);
+    code(0, px0, held[0]);
+    px0 = row_of(2);
+    take(px0, held[0]);
+    code(1, px1, held[1]);
+    px1 = row_of(3);
+    take(px1, held[1]);
+    code(2, px0, held[0]);
+    code(3, px1, held[1]);
+  }
+  __syncthreads();
+
+  const int group = max(t.group, 0), steps = p.ld / 128;
+  for (int c0 = wave * 32; c0 < p.n; c0 += 256) {
+    const int8_t* pw[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      pw[j] = p.qw + ((int64_t)group * p.n + min(c0 + j * 16 + (lane >> 2), p.n - 1)) * p.ld + (lane & 3) * 16;
+    v4i acc[2][2], a0[2][2], a1[2][2];  // a0, a1: W of two steps, on their way
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[i][j] = v4i{0, 0, 0, 0};
+    auto fetch = [&](int s, v4i (&w)[2][2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) w[k][j] = *reinterpret_cast<const v4i*>(pw[j] + min(s, steps - 1) * 128 + k * 64);
+    };
+    // step s with w, which then takes step s + 2
+    auto step = [&](int s, v4i (&w)[2][2]) __attribute__((always_inline)) {
+      v4i a[2][2], b[2][2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          a[k][i] = to_rows(w[k][i]);
+          b[k][i] = *reinterpret_cast<const v4i*>(codes + (i * 16 + l16) * kPitch + s * 128 + (((k * 4 + quad) ^ (l16 & 7)) << 4));
+        }
+      fetch(s + 2, w);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[k][j], b[k][i], acc[i][j], 0, 0, 0);
+    };
+    fetch(0, a0);
+    fetch(1, a1);
+    int s = 0;
+    for (; s + 1 < steps; s += 2) {
+      step(s, a0);
+      step(s + 1, a1);
+    }
+    if (s < steps) step(s, a0);
+    const float* psw = p.sw + (int64_t)group * p.n;
+    const float* pbias = p.bias ? p.bias + (int64_t)group * p.n : psw;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int c = c0 + j * 16 + quad * 4;
+      float sw[4], bias[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        sw[q] = psw[min(c + q, p.n - 1)];
+        bias[q] = pbias[min(c + q, p.n - 1)];
+        if (!p.bias) bias[q] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = t.row0 + i * 16 + l16;
+        const bool owned = t.group >= 0 && r < t.end && token_of(p, r) >= 0;
+        put4_as(elem_y, y, (int64_t)r * ldy + c, acc[i][j], (double)scales[i * 16 + l16], sw, bias, owned,
+                r < t.end ? p.n - c : 0, fours);
+      }
+    }
+  }
+}
+
+// Whether the rows of the layer are few enough to be held: a chunk at least, and
+// the codes of 32 rows twice in LDS.
+template <typename TX>
+bool coded_fits(const Product& p) {
+  return p.k >= Chunk<TX>::kElems && p.ld <= kCodedLd;
+}
+
+template <typename TX, int TURNS = 1>
+void launch_coded(hipStream_t s, const Product& p, dpc_elem elem_y, const TX* x, int64_t ldx, void* y, int64_t ldy) {
+  constexpr int kTurn = 64 * Chunk<TX>::kElems;
+  if constexpr (TURNS * kTurn < kCodedLd) {
+    // float64: 1, 2, 4, 8, 16 turns; others every number
+    if (p.ld > TURNS * kTurn)
+      return launch_coded<TX, sizeof(TX) == 8 ? 2 * TURNS : TURNS + 1>(s, p, elem_y, x, ldx, y, ldy);
+  }
+  const bool fours = elem_y == DPC_ELEM_F64   ? in_fours(p, (double*)y, ldy)
+                     : elem_y == DPC_ELEM_F32 ? in_fours(p, (float*)y, ldy)
+                                              : in_fours(p, (_Float16*)y, ldy);
+  hipLaunchKernelGGL((coded_product_kernel<TX, TURNS>), dim3((unsigned)most_tiles(p, kCodedRows)), dim3(512), 0, s, p,
+                     elem_y, x, ldx, y, ldy, fours);
+}
+
+template <typename TX>
+void few_by_type(hipStream_t s, const Product& p, dpc_elem elem_y, const TX* x, int64_t ldx, void* y, int64_t ldy) {
+  switch (elem_y) {
+    case DPC_ELEM_F64: launch_few(s, p, x, ldx, (double*)y, ldy); break;
+    case DPC_ELEM_F32: launch_few(s, p, x, ldx, (float*)y, ldy); break;
+    case DPC_ELEM_F16: launch_few(s, p, x, ldx, (_Float16*)y, ldy); break;
+    default: launch_few(s, p, x, ldx, (__bf16*)y, ldy); break;
+  }
+}
+
+// The layer in one kernel, if it is one for that: true and its status.
+bool coded_product(hipStream_t s, dpc_elem elem_x, dpc_elem elem_y, const Product& p, const void* x, int64_t ldx, void* y,
+                   int64_t ldy, int* status) {
+  // both sides, us (float32 rows of 1,600; 240 channels): 2,048 rows 13.9 here
+  // and 16.0 in two kernels, 8,192 18.1 and 26.2, 262,144 500 and 581; with 512
+  // channels the products take longer here than the codes' way through memory
+  // (2,048 rows 21.5 and 16.4, 32,000 99 and 92, 262,144 742 and 730).  Rows
+  // that go to several experts would be coded once for each.
+  // Few rows in all, short ones: every workgroup codes them again, one row in
+  // each wavefront, which costs less than a launch (one row of 1,600 to 240
+  // channels 5.4 us and 7.2 in two kernels, 8 rows 6.2 and 7.6; but 16 rows
+  // 9.2 and 7.9, one row of 4,096 to 4,096 channels 9.7 and 8.0).
+  const bool few = p.m <= kFewWaves && p.ld <= 2048;
+  if (!few && (p.topk != 1 || p.n > 256 || few_rows(p))) return false;
+  (void)hipGetLastError();  // report only what this launch raises
+  const auto go = [&](auto* px) {
+    if (few) {
+      few_by_type(s, p, elem_y, px, ldx, y, ldy);
+    } else {
+      if (!coded_fits<std::remove_const_t<std::remove_pointer_t<decltype(px)>>>(p)) return false;
+      launch_coded(s, p, elem_y, px, ldx, y, ldy);
+    }
+    *status = dpc_internal_launch_status();
+    return true;
+  };
+  switch (elem_x) {
+    case DPC_ELEM_F64: return go((const double*)x);
+    case DPC_ELEM_F32: return go((const float*)x);
+    case DPC_ELEM_F16: return go((const _Float16*)x);
+    default: return go((const __bf16*)x);
+  }
 }
 
 int product_args(dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup) {
@@ -545,8 +915,10 @@ extern "C" int dpc_linear_i8(void* stream, dpc_elem elem_x, dpc_elem elem_y, int
   hipStream_t s = static_cast<hipStream_t>(stream);
   int8_t* q = static_cast<int8_t*>(workspace);
   float* scale = reinterpret_cast<float*>(q + (size_t)ntok * DPC_I8_LD(k));
+  Product p{ntok, topk, ntok * topk, n, k, DPC_I8_LD(k), ngroup, q, scale, rows, offsets, qw, sw, bias};
+  int coded;
+  if (coded_product(s, elem_x, elem_y, p, x, ldx, y, ldy, &coded)) return coded;
   const int qs = quant(s, elem_x, ntok, k, x, ldx, q, scale);
   if (qs != DPC_OK) return qs;
-  const Product p{ntok, topk, ntok * topk, n, k, DPC_I8_LD(k), ngroup, q, scale, rows, offsets, qw, sw, bias};
   return product(s, elem_y, p, y, ldy);
 }
