@@ -273,16 +273,16 @@ __device__ __forceinline__ v4i to_rows(v4i w) {
   return r;
 }
 
-// Few rows: 16 rows times 16 channels of y for each workgroup, whose 8
-// wavefronts share K (step s is wavefront s % 8's) and whose sums are added in
+// Few rows: 16 rows times 16 channels of y for each `share` wavefronts of a
+// workgroup of 8, which take the steps of K in turn and whose sums are added in
 // LDS.  W is read once, 8 KiB of it under way in every wavefront: bound by that
 // read, or for short rows by latency.  TX is the type of rows that the workgroup
 // codes itself (into LDS), or int8_t for rows that are codes already.
 constexpr int kFewWaves = 8, kFewAhead = 4;
 
 template <typename TX, typename TY>
-__global__ __launch_bounds__(64 * kFewWaves) void few_product_kernel(Product p, const TX* __restrict__ x, int64_t ldx,
-                                                                     TY* __restrict__ y, int64_t ldy) {
+__global__ __launch_bounds__(64 * kFewWaves) void few_product_kernel(Product p, int share, const TX* __restrict__ x,
+                                                                     int64_t ldx, TY* __restrict__ y, int64_t ldy) {
   constexpr bool kCoded = sizeof(TX) == 1;
   extern __shared__ __attribute__((aligned(16))) int8_t codes[];  // 16 rows of codes, if they are made here
   __shared__ int sums[kFewWaves][256];
@@ -291,7 +291,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_product_kernel(Product p, 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Tile t = find_tile(p, 16, blockIdx.y + gridDim.y * blockIdx.z);
   if (t.row0 >= t.end) return;
-  const int c0 = blockIdx.x * 16, steps = p.ld / 128, group = max(t.group, 0);
+  const int tiles = kFewWaves / share;  // channel tiles of the workgroup
+  const int c0 = (blockIdx.x * tiles + wave / share) * 16, part = wave % share;
+  const int steps = p.ld / 128, group = max(t.group, 0);
   const int8_t* pw = p.qw + ((int64_t)group * p.n + min(c0 + (lane >> 2), p.n - 1)) * p.ld + (lane & 3) * 16;
   const int mine = t.group < 0 ? -1 : token_of(p, min(t.row0 + (lane >> 2), t.end - 1));
   const int8_t* pq = kCoded ? (const int8_t*)x + (int64_t)max(mine, 0) * p.ld + (lane & 3) * 16 : nullptr;
@@ -299,15 +301,15 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_product_kernel(Product p, 
   auto fetch = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < kFewAhead; ++u) {
-      const int s = min(s0 + u * kFewWaves, steps - 1);
+      const int s = min(s0 + u * share, steps - 1);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        w[u][k] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(pw + s * 128 + k * 64));
+        w[u][k] = *reinterpret_cast<const v4i*>(pw + s * 128 + k * 64);
         if (kCoded) q[u][k] = *reinterpret_cast<const v4i*>(pq + s * 128 + k * 64);
       }
     }
   };
-  fetch(wave);
+  fetch(part);
   if constexpr (!kCoded) {
     constexpr int VE = Chunk<TX>::kElems;
     for (int row = wave; row < 16; row += kFewWaves) {
@@ -350,10 +352,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_product_kernel(Product p, 
   }
   const int high = min(t.end - t.row0, 16) - 1;  // rows of the tile past its end repeat its last one
   v4i acc = {0, 0, 0, 0};
-  for (int s0 = wave; s0 < steps; s0 += kFewWaves * kFewAhead) {
+  for (int s0 = part; s0 < steps; s0 += share * kFewAhead) {
 #pragma unroll
     for (int u = 0; u < kFewAhead; ++u) {
-      const int s = s0 + u * kFewWaves;
+      const int s = s0 + u * share;
       if (s >= steps) break;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -367,25 +369,25 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_product_kernel(Product p, 
         acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(to_rows(w[u][k]), b, acc, 0, 0, 0);
       }
     }
-    if (s0 + kFewWaves * kFewAhead < steps) fetch(s0 + kFewWaves * kFewAhead);
+    if (s0 + share * kFewAhead < steps) fetch(s0 + share * kFewAhead);
   }
   // this lane: row l16, channels 4 quad .. 4 quad + 3
 #pragma unroll
   for (int i = 0; i < 4; ++i) sums[wave][l16 * 16 + quad * 4 + i] = acc[i];
   __syncthreads();
-  if (threadIdx.x >= 256) return;
-  const int row = threadIdx.x >> 4, c = c0 + (threadIdx.x & 15), r = t.row0 + row;
-  if (r >= t.end || c >= p.n) return;
-  int sum = 0;
-#pragma unroll
-  for (int v = 0; v < kFewWaves; ++v) sum += sums[v][threadIdx.x];
-  const int tok = t.group < 0 ? -1 : token_of(p, r);
-  TY out = (TY)0;
-  if (tok >= 0) {
-    const int64_t gc = (int64_t)group * p.n + c;
-    out = scaled<TY>(sum, (double)(kCoded ? p.sx[tok] : scales[row]), p.sw[gc], p.bias ? p.bias[gc] : 0.0f);
+  for (int e = threadIdx.x; e < tiles * 256; e += 64 * kFewWaves) {
+    const int tile = e >> 8, row = e >> 4 & 15, c = (blockIdx.x * tiles + tile) * 16 + (e & 15), r = t.row0 + row;
+    if (r >= t.end || c >= p.n) continue;
+    int sum = 0;
+    for (int v = 0; v < share; ++v) sum += sums[tile * share + v][e & 255];
+    const int tok = t.group < 0 ? -1 : token_of(p, r);
+    TY out = (TY)0;
+    if (tok >= 0) {
+      const int64_t gc = (int64_t)group * p.n + c;
+      out = scaled<TY>(sum, (double)(kCoded ? p.sx[tok] : scales[row]), p.sw[gc], p.bias ? p.bias[gc] : 0.0f);
+    }
+    y[(int64_t)r * ldy + c] = out;
   }
-  y[(int64_t)r * ldy + c] = out;
 }
 
 // Whether at most 16 rows share an expert's weights, on average.
@@ -397,8 +399,16 @@ template <typename TX, typename TY>
 void launch_few(hipStream_t s, const Product& p, const TX* x, int64_t ldx, TY* y, int64_t ldy) {
   const int64_t tiles = most_tiles(p, 16);
   const unsigned gy = (unsigned)(tiles < 32768 ? tiles : 32768);
-  hipLaunchKernelGGL((few_product_kernel<TX, TY>), dim3((p.n + 15) / 16, gy, (unsigned)((tiles + gy - 1) / gy)),
-                     dim3(64 * kFewWaves), sizeof(TX) == 1 ? 0 : (size_t)(p.m < 16 ? p.m : 16) * p.ld, s, p, x, ldx, y, ldy);
+  // wavefronts that share a tile: about 16 in all for each of 256 CUs (16 rows
+  // of 2,048 for 16 of 64 experts with 2,048 channels: 15.8 us with 2, 24.7 with
+  // 8; 16 rows through 8,192 x 8,192: 14.3 with 8, 19.2 with 2)
+  const int64_t wide = (p.n + 15) / 16;
+  int share = kFewWaves;
+  while (share > 1 && wide * tiles * share > 4096) share /= 2;
+  hipLaunchKernelGGL((few_product_kernel<TX, TY>),
+                     dim3((unsigned)((wide * share + kFewWaves - 1) / kFewWaves), gy, (unsigned)((tiles + gy - 1) / gy)),
+                     dim3(64 * kFewWaves), sizeof(TX) == 1 ? 0 : (size_t)(p.m < 16 ? p.m : 16) * p.ld, s, p, share, x,
+                     ldx, y, ldy);
 }
 
 // Four consecutive results of a row, of which `left` exist; fours: all or none
