@@ -440,10 +440,13 @@ def dpc_fitting_fwd_bwd(stream, blas, nloc, net, D, workspace, workspace_bytes, 
 
 
 # ---- routing and 8-bit layers: rows of any element type, with a row stride ----
+_TORCH_ELEM = {} if torch is None else {torch.float64: DPC_ELEM_F64, torch.float32: DPC_ELEM_F32,
+                                        torch.float16: DPC_ELEM_F16, torch.bfloat16: DPC_ELEM_BF16}
+
+
 def elem_of(dtype):
     """The dpc_elem of a torch dtype."""
-    e = {torch.float64: DPC_ELEM_F64, torch.float32: DPC_ELEM_F32, torch.float16: DPC_ELEM_F16,
-         torch.bfloat16: DPC_ELEM_BF16}.get(dtype)
+    e = _TORCH_ELEM.get(dtype)
     if e is None:
         raise TypeError(f"rows of {dtype} are not supported (float64, float32, float16, bfloat16)")
     return e
@@ -454,8 +457,7 @@ def i8_ld(cols):
     return (int(cols) + 127) // 128 * 128
 
 
-_ELEM_TORCH = {} if torch is None else {DPC_ELEM_F64: torch.float64, DPC_ELEM_F32: torch.float32,
-                                        DPC_ELEM_F16: torch.float16, DPC_ELEM_BF16: torch.bfloat16}
+_ELEM_TORCH = {e: t for t, e in _TORCH_ELEM.items()}
 
 
 def _elem_dtype(elem, name="elem"):

@@ -1,23 +1,15 @@
 """Convenience objects of the routing and 8-bit calls: they check arguments and
-allocate outputs as torch tensors.  All arithmetic happens in libdpc."""
-import contextlib
+allocate outputs as torch tensors.  All arithmetic happens in libdpc.
 
+A call with few rows is over in microseconds, so these methods check what they
+are given once and call the library by address, without the checks of the
+binding's functions of the same names."""
 import torch
 
 from . import binding as B
 
-
-_HERE = contextlib.nullcontext()
-
-
-def _on(stream):
-    """Outputs and workspaces are allocated for the stream that uses them."""
-    return _HERE if stream is None else torch.cuda.stream(stream)
-
-
-def _raw(stream, device):
-    """hipStream_t of a torch stream, or of the device's current one."""
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+_lib, _elem_of = B._lib, B.elem_of
+_raw_stream = torch._C._cuda_getCurrentRawStream   # hipStream_t of a device's current stream
 
 
 def _check(status, where):
@@ -25,31 +17,30 @@ def _check(status, where):
         raise B.DpcError(status, where)
 
 
-def _elsewhere(t, device):
-    raise ValueError(f"a tensor is on {t.device}, the others are on cuda:{device}")
-
-
-def _matrix(x, name, rows=None, width=None, dtype=None):
+def _rows(x, name, n=None, width=None, dtype=None, device=None):
     """Checks a tensor of rows (unit stride inside a row, rows apart by any
     stride that does not make them overlap); returns its row stride."""
-    if x.dim() != 2 or (rows is not None and x.shape[0] != rows) or (width is not None and x.shape[1] != width):
-        want = f"[{'rows' if rows is None else rows}, {'width' if width is None else width}]"
-        raise ValueError(f"{name} has shape {tuple(x.shape)}, expected {want}")
+    shape = x.shape
+    if len(shape) != 2 or (n is not None and shape[0] != n) or (width is not None and shape[1] != width):
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected [{'rows' if n is None else n}, "
+                         f"{'width' if width is None else width}]")
     if dtype is not None and x.dtype != dtype:
         raise TypeError(f"{name} has dtype {x.dtype}, expected {dtype}")
-    if not x.is_cuda:
-        raise ValueError(f"{name} must be a tensor on a GPU device, not {x.device}")
-    n, w = x.shape
-    if (w > 1 and x.stride(1) != 1) or (n > 1 and x.stride(0) < w):
+    _on(x, device, name)
+    n, w = shape
+    between, inside = x.stride()
+    if (w > 1 and inside != 1) or (n > 1 and between < w):
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return x.stride(0) if n > 1 else max(w, 1)
+    return between if n > 1 else w or 1
 
 
-def _out(out, rows, width, like, name):
-    if out is None:
-        return torch.empty((rows, width), dtype=like.dtype, device=like.device)
-    _matrix(out, name, rows, width, like.dtype)
-    return out
+def _on(x, device, name):
+    """Checks that a tensor is on a GPU (that of the others)."""
+    at = x.get_device()
+    if at < 0:
+        raise ValueError(f"{name} must be a tensor on a GPU device, not {x.device}")
+    if device is not None and at != device:
+        raise ValueError(f"{name} is on {x.device}, the others are on cuda:{device}")
 
 
 class Route:
@@ -61,27 +52,31 @@ class Route:
              are in use
     rows     int32 [tokens * topk]: slot token * topk + j of each row, -1 for the
              empty rows at the end
-    pos      int32 [tokens, topk]: row of each choice, -1 if it is dropped"""
+    pos      int32 [tokens, topk]: row of each choice, -1 if it is dropped
+
+    stream: a torch stream that the call runs on, and for which its outputs are
+    allocated (default: the current one)."""
 
     def __init__(self, expert, nexpert, stream=None):
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return Route.__init__(self, expert, nexpert)
         if expert.dtype != torch.int32 or expert.dim() not in (1, 2) or not expert.is_contiguous():
             raise ValueError("expert must be contiguous int32 [tokens, topk] or [tokens]")
-        if not expert.is_cuda:
-            raise ValueError(f"expert must be a tensor on a GPU device, not {expert.device}")
-        self.ntok, self.topk = expert.shape[0], 1 if expert.dim() == 1 else expert.shape[1]
+        _on(expert, None, "expert")
+        self._device = dev = expert.get_device()
+        self.ntok, self.topk = expert.shape if expert.dim() == 2 else (expert.shape[0], 1)
         self.nexpert = int(nexpert)
-        m, dev = self.ntok * self.topk, expert.device
-        with _on(stream):
-            nb = B.dpc_route_workspace_bytes(self.ntok, self.topk, self.nexpert)
-            # offsets, rows and positions in one allocation
-            buf = torch.empty(max(self.nexpert, 0) + 1 + 2 * m, dtype=torch.int32, device=dev)
-            self.offsets, self.rows = buf[:self.nexpert + 1], buf[self.nexpert + 1:self.nexpert + 1 + m]
-            self.pos = buf[self.nexpert + 1 + m:].view(self.ntok, self.topk)
-            ws = torch.empty(nb, dtype=torch.uint8, device=dev)
-            at = buf.data_ptr()
-            _check(B._lib.dpc_route_plan(_raw(stream, dev.index), self.ntok, self.topk, self.nexpert,
-                                         expert.data_ptr(), ws.data_ptr(), nb, at, at + 4 * (self.nexpert + 1),
-                                         at + 4 * (self.nexpert + 1 + m)), "dpc_route_plan")
+        m, head = self.ntok * self.topk, max(self.nexpert, 0) + 1
+        nb = _lib.dpc_route_workspace_bytes(self.ntok, self.topk, self.nexpert)
+        # the three of the plan in one allocation
+        buf = expert.new_empty(head + 2 * m)
+        ws = expert.new_empty((nb + 3) // 4)
+        self.offsets, self.rows, pos = buf.split_with_sizes((head, m, m))
+        self.pos = pos.view(self.ntok, self.topk)
+        at = buf.data_ptr()
+        _check(_lib.dpc_route_plan(_raw_stream(dev), self.ntok, self.topk, self.nexpert, expert.data_ptr(),
+                                   ws.data_ptr(), nb, at, at + 4 * head, at + 4 * (head + m)), "dpc_route_plan")
 
     @classmethod
     def from_plan(cls, offsets, rows, pos):
@@ -89,67 +84,78 @@ class Route:
         r = cls.__new__(cls)
         if pos.dim() != 2 or rows.dim() != 1 or offsets.dim() != 1 or rows.shape[0] != pos.numel() or len(offsets) < 2:
             raise ValueError("offsets, rows and pos do not belong together")
+        r._device = pos.get_device()
         for name, t in (("offsets", offsets), ("rows", rows), ("pos", pos)):
-            if t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda:
-                raise ValueError(f"{name} must be a contiguous int32 tensor on a GPU device")
+            if t.dtype != torch.int32 or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous int32 tensor")
+            _on(t, r._device, name)
         r.offsets, r.rows, r.pos = offsets, rows, pos
         r.ntok, r.topk = pos.shape
         r.nexpert = len(offsets) - 1
         return r
 
     def _weight(self, weight, x):
+        """Address of the weights of a call on rows x."""
         if weight is None:
             return None
         want = torch.float64 if x.dtype == torch.float64 else torch.float32
         if weight.dtype != want or weight.shape != self.pos.shape or not weight.is_contiguous():
             raise ValueError(f"weight must be contiguous {want} [tokens, topk]")
-        return weight
-
-    def _call(self, name, stream, x, width, *args):
-        """args: tensors are passed by address"""
-        dev = self.pos.get_device()
-        args = [a if a is None or isinstance(a, int) else a.data_ptr() if a.get_device() == dev else
-                _elsewhere(a, dev) for a in args]
-        _check(getattr(B._lib, name)(_raw(stream, dev), B.elem_of(x.dtype), self.ntok, self.topk, width, *args), name)
+        _on(weight, self._device, "weight")
+        return weight.data_ptr()
 
     def gather(self, x, weight=None, out=None, stream=None):
         """[tokens * topk, width]: each row the token's row (times its weight),
         zeros in the empty rows.  With weights, the gradient of combine()."""
-        ldx = _matrix(x, "x", self.ntok)
-        m, width = self.ntok * self.topk, x.shape[1]
-        with _on(stream):
-            y = _out(out, m, width, x, "out")
-            self._call("dpc_route_gather", stream, x, width, x, ldx, self._weight(weight, x), self.rows, self.pos, y,
-                       y.stride(0) if m > 1 else max(width, 1))
-        return y
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.gather(x, weight, out)
+        dev, m = self._device, self.ntok * self.topk
+        ldx, width = _rows(x, "x", self.ntok, None, None, dev), x.shape[1]
+        if out is None:
+            out, ldy = x.new_empty((m, width)), width or 1
+        else:
+            ldy = _rows(out, "out", m, width, x.dtype, dev)
+        _check(_lib.dpc_route_gather(_raw_stream(dev), _elem_of(x.dtype), self.ntok, self.topk, width, x.data_ptr(), ldx,
+                                     self._weight(weight, x), self.rows.data_ptr(), self.pos.data_ptr(),
+                                     out.data_ptr(), ldy), "dpc_route_gather")
+        return out
 
     def combine(self, x, weight=None, out=None, stream=None):
         """[tokens, width]: the sum of each token's rows (times their weights);
         without weights, the gradient of gather()."""
-        m = self.ntok * self.topk
-        ldx = _matrix(x, "rows", m)
-        width = x.shape[1]
-        with _on(stream):
-            y = _out(out, self.ntok, width, x, "out")
-            self._call("dpc_route_combine", stream, x, width, x, ldx, self._weight(weight, x), self.pos, y,
-                       y.stride(0) if self.ntok > 1 else max(width, 1))
-        return y
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.combine(x, weight, out)
+        dev = self._device
+        ldx, width = _rows(x, "rows", self.ntok * self.topk, None, None, dev), x.shape[1]
+        if out is None:
+            out, ldy = x.new_empty((self.ntok, width)), width or 1
+        else:
+            ldy = _rows(out, "out", self.ntok, width, x.dtype, dev)
+        _check(_lib.dpc_route_combine(_raw_stream(dev), _elem_of(x.dtype), self.ntok, self.topk, width, x.data_ptr(), ldx,
+                                      self._weight(weight, x), self.pos.data_ptr(), out.data_ptr(), ldy),
+               "dpc_route_combine")
+        return out
 
     def combine_backward(self, x, dy, weight=None, need_rows=True, stream=None):
         """Gradient of combine(x, weight) from dE/dy: (dE/dx, dE/dweight); the
         second is None without weights, the first with need_rows=False."""
-        m = self.ntok * self.topk
-        ldx = _matrix(x, "rows", m)
-        width = x.shape[1]
-        lddy = _matrix(dy, "dy", self.ntok, width, x.dtype)
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.combine_backward(x, dy, weight, need_rows)
+        dev, m = self._device, self.ntok * self.topk
+        ldx, width = _rows(x, "rows", m, None, None, dev), x.shape[1]
+        lddy = _rows(dy, "dy", self.ntok, width, x.dtype, dev)
         w = self._weight(weight, x)
-        if w is None and not need_rows:
+        if weight is None and not need_rows:
             return None, None
-        with _on(stream):
-            dx = torch.empty((m, width), dtype=x.dtype, device=x.device) if need_rows else None
-            dw = None if w is None else torch.empty_like(w, memory_format=torch.contiguous_format)
-            self._call("dpc_route_combine_bwd", stream, x, width, x, ldx, w, self.rows, self.pos, dy, lddy, dx,
-                       max(width, 1), dw)
+        dx = x.new_empty((m, width)) if need_rows else None
+        dw = None if weight is None else weight.new_empty(weight.shape)
+        _check(_lib.dpc_route_combine_bwd(_raw_stream(dev), _elem_of(x.dtype), self.ntok, self.topk, width, x.data_ptr(),
+                                          ldx, w, self.rows.data_ptr(), self.pos.data_ptr(), dy.data_ptr(), lddy,
+                                          None if dx is None else dx.data_ptr(), width or 1,
+                                          None if dw is None else dw.data_ptr()), "dpc_route_combine_bwd")
         return dx, dw
 
 
@@ -164,32 +170,39 @@ class Int8Linear:
             codes, scales = codes[None], scales[None]
             bias = None if bias is None else bias[None]
         self.inner = int(inner)
-        if codes.dim() != 3 or codes.dtype != torch.int8 or codes.shape[2] != B.i8_ld(self.inner):
-            raise ValueError("codes must be int8 [experts, outer, i8_ld(inner)]")
-        self.experts, self.outer = codes.shape[:2]
+        shape = codes.shape
+        if len(shape) != 3 or codes.dtype != torch.int8 or shape[2] != B.i8_ld(self.inner) or not codes.is_contiguous():
+            raise ValueError("codes must be contiguous int8 [experts, outer, i8_ld(inner)]")
+        self._device = codes.get_device()
+        _on(codes, None, "codes")
+        self.experts, self.outer = shape[:2]
         for name, t in (("scales", scales), ("bias", bias)):
-            if t is not None and (t.dtype != torch.float32 or t.shape != codes.shape[:2] or not t.is_contiguous()):
+            if t is None:
+                continue
+            if t.dtype != torch.float32 or t.shape != shape[:2] or not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous float32 [experts, outer]")
-        if not codes.is_contiguous() or not codes.is_cuda:
-            raise ValueError("codes must be a contiguous tensor on a GPU device")
+            _on(t, self._device, name)
         self.codes, self.scales, self.bias = codes, scales, bias
 
     @classmethod
     def from_weight(cls, weight, bias=None, stream=None):
         """Codes the rows (output channels) of weight [experts, outer, inner] or
         [outer, inner]; bias of any floating type."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return cls.from_weight(weight, bias)
         w = weight[None] if weight.dim() == 2 else weight
         if w.dim() != 3:
             raise ValueError("weight must be [experts, outer, inner] or [outer, inner]")
+        _on(w, None, "weight")
         g, n, k = w.shape
-        with _on(stream):
-            w = w.contiguous().view(g * n, k)
-            codes = torch.empty((g, n, B.i8_ld(k)), dtype=torch.int8, device=w.device)
-            scales = torch.empty((g, n), dtype=torch.float32, device=w.device)
-            B.dpc_quant_rows(stream or torch.cuda.current_stream(w.device), B.elem_of(w.dtype), g * n, k, w, k,
-                             codes, scales)
-            if bias is not None:
-                bias = bias.to(torch.float32).reshape(g, n).contiguous()
+        w = w.contiguous()
+        codes = torch.empty((g, n, B.i8_ld(k)), dtype=torch.int8, device=w.device)
+        scales = torch.empty((g, n), dtype=torch.float32, device=w.device)
+        _check(_lib.dpc_quant_rows(_raw_stream(w.get_device()), _elem_of(w.dtype), g * n, k, w.data_ptr(), k,
+                                   codes.data_ptr(), scales.data_ptr()), "dpc_quant_rows")
+        if bias is not None:
+            bias = bias.to(torch.float32).reshape(g, n).contiguous()
         return cls(codes, scales, k, bias)
 
     def __call__(self, x, route=None, offsets=None, dtype=None, out=None, stream=None):
@@ -197,28 +210,35 @@ class Int8Linear:
         tokens and y its rows (each from its expert's layer); with offsets
         (int32 [experts + 1]), the rows of x are sorted by expert already.
         dtype: type of y (default: that of x)."""
-        ldx = _matrix(x, "x", None if route is None else route.ntok, self.inner)
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self(x, route, offsets, dtype, out)
+        dev = self._device
+        ldx = _rows(x, "x", None if route is None else route.ntok, self.inner, None, dev)
         ntok, topk, rows = x.shape[0], 1, None
         if route is not None:
             if offsets is not None:
                 raise ValueError("give a route or offsets, not both")
-            topk, rows, offsets = route.topk, route.rows, route.offsets
-        if offsets is not None and (offsets.dtype != torch.int32 or not offsets.is_contiguous()):
-            raise TypeError("offsets must be contiguous int32")
-        if offsets is not None and len(offsets) != self.experts + 1:
-            raise ValueError(f"offsets for {len(offsets) - 1} experts, layers for {self.experts}")
-        if offsets is None and self.experts != 1:
+            topk, rows, offsets = route.topk, route.rows.data_ptr(), route.offsets
+        if offsets is not None:
+            if offsets.dtype != torch.int32 or not offsets.is_contiguous():
+                raise TypeError("offsets must be contiguous int32")
+            if len(offsets) != self.experts + 1:
+                raise ValueError(f"offsets for {len(offsets) - 1} experts, layers for {self.experts}")
+            _on(offsets, dev, "offsets")
+            offsets = offsets.data_ptr()
+        elif self.experts != 1:
             raise ValueError("layers of several experts need a route or offsets")
-        dtype = x.dtype if dtype is None else dtype
-        with _on(stream):
-            y = torch.empty((ntok * topk, self.outer), dtype=dtype, device=x.device) if out is None else out
-            ldy = _matrix(y, "out", ntok * topk, self.outer, dtype)
-            nb = B.dpc_linear_i8_workspace_bytes(ntok, self.inner)
-            ws = torch.empty(nb, dtype=torch.uint8, device=x.device)
-            dev = x.get_device()
-            args = [a if a is None else a.data_ptr() if a.get_device() == dev else _elsewhere(a, dev)
-                    for a in (rows, offsets, self.codes, self.scales, self.bias, y)]
-            _check(B._lib.dpc_linear_i8(_raw(stream, dev), B.elem_of(x.dtype), B.elem_of(dtype), ntok, topk,
-                                        self.outer, self.inner, self.experts, x.data_ptr(), ldx, *args[:5],
-                                        ws.data_ptr(), nb, args[5], ldy), "dpc_linear_i8")
-        return y
+        if dtype is None:
+            dtype = x.dtype
+        if out is None:
+            out, ldy = torch.empty((ntok * topk, self.outer), dtype=dtype, device=x.device), self.outer
+        else:
+            ldy = _rows(out, "out", ntok * topk, self.outer, dtype, dev)
+        nb = _lib.dpc_linear_i8_workspace_bytes(ntok, self.inner)
+        ws = self.codes.new_empty(nb)
+        _check(_lib.dpc_linear_i8(_raw_stream(dev), _elem_of(x.dtype), _elem_of(dtype), ntok, topk, self.outer,
+                                  self.inner, self.experts, x.data_ptr(), ldx, rows, offsets, self.codes.data_ptr(),
+                                  self.scales.data_ptr(), None if self.bias is None else self.bias.data_ptr(),
+                                  ws.data_ptr(), nb, out.data_ptr(), ldy), "dpc_linear_i8")
+        return out
