@@ -440,8 +440,9 @@ int dpc_quant_rows(void* stream, dpc_elem elem, int nrows, int ncols, const void
  *   qw, sw   device codes [ngroup][n][DPC_I8_LD(k)] and scales [ngroup][n]
  *   bias     device float32 [ngroup][n] or NULL
  *   y        device out [ntok * topk] rows of n elements, ldy apart
- * qx and qw 16-byte aligned.  Requires n >= 1, 1 <= k <= DPC_MAX_I8_COLS,
- * ngroup <= DPC_MAX_EXPERTS, topk <= DPC_MAX_TOPK (DPC_ENOTSUP above).
+ * qx and qw 16-byte aligned.  Requires 1 <= n <= 2^24, 1 <= k <=
+ * DPC_MAX_I8_COLS, ngroup <= DPC_MAX_EXPERTS, topk <= DPC_MAX_TOPK and
+ * ntok * topk <= 2^27 (DPC_ENOTSUP above).
  * The gradient of y in x is the same product with the codes of the transposed
  * weights (their rows are input channels).                                  */
 int dpc_matmul_i8(void* stream, dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup,

@@ -18,7 +18,9 @@
 
 namespace {
 
-constexpr int64_t kMaxRows = (int64_t)1 << 30;
+constexpr int64_t kMaxRows = (int64_t)1 << 30;      // rows of codes
+constexpr int64_t kMaxProduct = (int64_t)1 << 27;   // rows of a product (a launch has under 2^32 threads)
+constexpr int kMaxChannels = 1 << 24;
 
 // ---------------------------------------------------------------------------
 // codes
@@ -235,6 +237,21 @@ __device__ __forceinline__ Tile find_tile(const Product& p, int size, int tile) 
   return Tile{-1, p.m, p.m};
 }
 
+// Tiles of `size` rows that exist, on the device.
+__device__ __forceinline__ int count_tiles(const Product& p, int size) {
+  if (!p.offsets) return (p.m + size - 1) / size;
+  const int lane = threadIdx.x & 63;
+  int sum = 0;
+  for (int g = lane; g <= p.ngroup; g += 64) {
+    const int first = min(max(p.offsets[g], 0), p.m);
+    const int last = g < p.ngroup ? max(min(max(p.offsets[g + 1], 0), p.m), first) : p.m;
+    sum += (last - first + size - 1) / size;
+  }
+#pragma unroll
+  for (int m = 32; m; m >>= 1) sum += __shfl_xor(sum, m);
+  return __builtin_amdgcn_readfirstlane(sum);
+}
+
 // Tiles of `size` rows that find_tile can be asked for.
 inline int64_t most_tiles(const Product& p, int size) {
   if (!p.offsets) return ((int64_t)p.m + size - 1) / size;
@@ -438,7 +455,7 @@ typedef const __attribute__((address_space(1))) void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
 template <typename TY, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, int row_tiles, int col_tiles,
+__global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, int col_tiles,
                                                                      TY* __restrict__ y, int64_t ldy, bool fours) {
   constexpr int kWaves = WM * WN, TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
   constexpr int kStep = 128, kRows = BM + BN;
@@ -450,7 +467,9 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
   const int wm = wave % WM, wn = wave / WM;
 
   // consecutive workgroups go to different XCDs: each XCD gets a run of tiles
-  // of its own, in bands of 8 row tiles, so that its L2 serves tiles that share rows
+  // of its own, in bands of 8 row tiles, so that its L2 serves tiles that share
+  // rows; the runs are cut from the tiles that exist, for equal work
+  const int row_tiles = count_tiles(p, BM);
   const int total = row_tiles * col_tiles, per = (total + 7) / 8;
   const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= per || id >= total) return;
@@ -594,10 +613,10 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
 
 template <typename TY, int BM, int BN, int WM, int WN>
 void launch_tiled(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
-  const int row_tiles = (int)most_tiles(p, BM), col_tiles = (p.n + BN - 1) / BN;
-  const unsigned per = ((unsigned)row_tiles * (unsigned)col_tiles + 7) / 8;
-  hipLaunchKernelGGL((product_tiled_kernel<TY, BM, BN, WM, WN>), dim3(per * 8), dim3(64 * WM * WN), 0, s, p, row_tiles,
-                     col_tiles, y, ldy, in_fours(p, y, ldy));
+  const int col_tiles = (p.n + BN - 1) / BN;
+  const unsigned per = ((unsigned)most_tiles(p, BM) * (unsigned)col_tiles + 7) / 8;
+  hipLaunchKernelGGL((product_tiled_kernel<TY, BM, BN, WM, WN>), dim3(per * 8), dim3(64 * WM * WN), 0, s, p, col_tiles,
+                     y, ldy, in_fours(p, y, ldy));
 }
 
 // Time of the tiled product: a fixed part, and for each step of K the larger of
@@ -609,6 +628,7 @@ void launch_tiled(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
 //   256 x 4096 x 4096    50.3  21.5  14.4  11.4     4000 x 240 x 1600   24.4 12.1  8.3  6.8
 double tiled_cost(const Product& p, int bm, int bn, double fixed, double alone, double each) {
   const int64_t tiles = most_tiles(p, bm) * ((p.n + bn - 1) / bn);
+  if (tiles >= 1 << 22) fixed += 1e30 / bm;  // more threads than a launch has: the largest tile, if any
   const double cu = each * (double)((tiles + 255) / 256);
   return fixed + p.ld / 128 * (alone > cu ? alone : cu);
 }
@@ -867,7 +887,8 @@ bool coded_product(hipStream_t s, dpc_elem elem_x, dpc_elem elem_y, const Produc
 
 int product_args(dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup) {
   if (!elem_ok(elem_y) || ntok < 0 || topk < 1 || n < 1 || k < 1 || ngroup < 1) return DPC_EINVAL;
-  if (topk > DPC_MAX_TOPK || k > DPC_MAX_I8_COLS || ngroup > DPC_MAX_EXPERTS || (int64_t)ntok * topk > kMaxRows)
+  if (topk > DPC_MAX_TOPK || k > DPC_MAX_I8_COLS || ngroup > DPC_MAX_EXPERTS || n > kMaxChannels ||
+      (int64_t)ntok * topk > kMaxProduct)
     return DPC_ENOTSUP;
   return DPC_OK;
 }

@@ -69,6 +69,7 @@ def test_8_bit_calls_validate_before_launch():
     shared = [(dict(ntok=-1), B.DPC_EINVAL), (dict(n=0, ldy=0), B.DPC_EINVAL), (dict(k=0), B.DPC_EINVAL),
               (dict(topk=0), B.DPC_EINVAL), (dict(ngroup=0), B.DPC_EINVAL), (dict(ngroup=1025), B.DPC_ENOTSUP),
               (dict(topk=65), B.DPC_ENOTSUP), (dict(ntok=1 << 30), B.DPC_ENOTSUP),
+              (dict(ntok=(1 << 26) + 1), B.DPC_ENOTSUP), (dict(n=(1 << 24) + 1, ldy=1 << 25), B.DPC_ENOTSUP),
               (dict(rows=None), B.DPC_EINVAL), (dict(offsets=None), B.DPC_EINVAL), (dict(qw=0), B.DPC_EINVAL),
               (dict(qw=FAKE + 4), B.DPC_EINVAL), (dict(sw=0), B.DPC_EINVAL), (dict(bias=FAKE + 2), B.DPC_EINVAL),
               (dict(y=0), B.DPC_EINVAL), (dict(ldy=11), B.DPC_EINVAL), (dict(y=FAKE + 2), B.DPC_EINVAL)]
