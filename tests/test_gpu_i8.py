@@ -292,3 +292,89 @@ def test_refusals():
     with pytest.raises(ValueError):
         lin(x, offsets=off, out=torch.zeros((4, 7), device="cuda"))
     assert lin(x[:0], offsets=off).shape == (0, 8)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+def test_narrow_layers_of_every_width(t):
+    # layers of up to 256 channels, rows from one element to past what their kernel holds, with and without experts
+    import paper_2107_02103_amd as P
+    rng = np.random.default_rng(11)
+    for k in (1, 2, 3, 4, 5, 7, 8, 9, 63, 100, 128, 129, 255, 256, 257, 500, 512, 513, 700, 768, 770, 1024, 1027, 1280,
+              1401, 1536, 1699, 1792, 1793, 2047, 2048, 2049, 2177):
+        m, n, G = 75, (50, 256, 33, 241)[k % 4], 3
+        x = torch.from_numpy(rng.standard_normal((m, k)) * np.exp(rng.standard_normal((m, 1)))).to(TYPES[t]).cuda()
+        x[20] = 0
+        x[21, k - 1] = float("nan")
+        x[22, 0] = float("-inf")
+        qx, sx = ox.codes(x.cpu().double().numpy())
+        e = rng.integers(-1, G, (m, 1)).astype(np.int32)
+        off, rows, _ = ox.plan(e, G)
+        r = P.Route(torch.from_numpy(e).cuda(), G)
+        qw, sw, b = _layer(rng, G, n, k)
+        lin = P.Int8Linear(_padded(qw, P.i8_ld(k)), torch.from_numpy(sw).cuda(), k, torch.from_numpy(b).cuda())
+        tok = np.maximum(rows, 0)
+        want, mag = ox.product(qx[tok], sx[tok], qw, sw, b, _groups(off, m, G))
+        _check(lin(x, route=r, dtype=torch.float32), want, mag, "f32")
+        one = P.Int8Linear(lin.codes[1], lin.scales[1], k)
+        want, mag = ox.product(qx, sx, qw[1:2], sw[1:2])
+        _check(one(x, dtype=torch.float32), want, mag, "f32")
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 20, 300), (5, 40000, 130), (8, 3000, 2048), (9, 3000, 2048), (16, 9000, 700),
+                                   (16, 70000, 64), (3, 64, 5000), (16, 100, 8200)])
+def test_few_rows(m, n, k):
+    # every number of wavefronts that share a tile, rows coded inside the kernel and before it
+    import paper_2107_02103_amd as P
+    rng = np.random.default_rng(m + n)
+    x = torch.from_numpy(rng.standard_normal((m, k)).astype(np.float32)).cuda()
+    qw, sw, b = _layer(rng, 1, n, k)
+    lin = P.Int8Linear(_padded(qw, P.i8_ld(k)), torch.from_numpy(sw).cuda(), k, torch.from_numpy(b).cuda())
+    qx, sx = ox.codes(x.cpu().numpy())
+    want, mag = ox.product(qx, sx, qw, sw, b)
+    _check(lin(x), want, mag, "f32")
+    _check(lin(x, dtype=torch.bfloat16), want, mag, "bf16")
+
+
+@pytest.mark.parametrize("m,n,k", [(4096, 4096, 1000), (16000, 512, 1600), (2048, 2048, 1000), (3000, 300, 2500)])
+@pytest.mark.parametrize("G", [1, 5])
+def test_every_tile(m, n, k, G):
+    # sizes that take the tiles of 256 x 256, 128 x 128, 128 x 64 and 64 x 64, for one layer and for experts of
+    # uneven numbers of rows (one without any) and rows of none
+    import paper_2107_02103_amd as P
+    rng = np.random.default_rng(m + G)
+    qx = rng.integers(-127, 128, (m, k)).astype(np.int8)
+    sx = (rng.random(m) * 0.1).astype(np.float32)
+    qw, sw, b = _layer(rng, G, n, k)
+    off, groups = None, None
+    if G > 1:
+        off = np.array([0, m // 3 + 5, m // 3 + 5, m // 2, m // 2 + 1, m - 7], np.int64)
+        groups = _groups(off, m, G)
+        off = torch.from_numpy(off.astype(np.int32)).cuda()
+    want, mag = ox.product(qx, sx, qw, sw, b, groups)
+    for t in ("f32", "bf16"):
+        y = torch.full((m, n), 9.0, dtype=TYPES[t], device="cuda")
+        P.dpc_matmul_i8(torch.cuda.current_stream(), P.elem_of(y.dtype), m, 1, n, k, G, _padded(qx, P.i8_ld(k)),
+                        torch.from_numpy(sx).cuda(), None, off, _padded(qw, P.i8_ld(k)), torch.from_numpy(sw).cuda(),
+                        torch.from_numpy(b).cuda(), y, n)
+        _check(y, want, mag, t)
+
+
+@pytest.mark.parametrize("n", [40, 300])
+def test_rows_past_32_bits(n):
+    # elements and bytes of x past 2^31 and 2^32, in one kernel (n = 40) and by way of the codes
+    import paper_2107_02103_amd as P
+    m, k = 1400000, 1600
+    x = torch.zeros((m, k), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    pick = torch.tensor([0, 1, m // 2, m - 33, m - 1], device="cuda")
+    x[pick] = torch.randn((5, k), generator=g, device="cuda").to(torch.bfloat16)
+    rng = np.random.default_rng(3)
+    qw, sw, b = _layer(rng, 1, n, k)
+    lin = P.Int8Linear(_padded(qw, P.i8_ld(k)), torch.from_numpy(sw).cuda(), k, torch.from_numpy(b).cuda())
+    y = lin(x, dtype=torch.bfloat16)
+    qx, sx = ox.codes(x[pick].cpu().double().numpy())
+    want, mag = ox.product(qx, sx, qw, sw, b)
+    _check(y[pick], want, mag, "bf16")
+    rest = torch.ones(m, dtype=torch.bool, device="cuda")
+    rest[pick] = False
+    assert bool((y[rest] == lin.bias[0].to(torch.bfloat16)).all())
