@@ -1,7 +1,9 @@
 // Layers in 8-bit integers (dpc_quant_rows, dpc_matmul_i8, dpc_linear_i8).
 //
 // Codes: one read of a row into registers, the largest magnitude across its
-// lanes, then the codes.  Bound by HBM bandwidth.
+// lanes, then the codes.  Bound by HBM bandwidth (16,384 bfloat16 rows of 4,096:
+// 201 MB read and written in 47 us), or by the latency of one load and two
+// reductions for a few rows (16 rows of 8,192: 5.2 us).
 //
 // Product: y[r][c] = (sum_i qx[t][i] qw[g][c][i]) sx[t] sw[g][c] + bias[g][c].
 // The sum over i is exact in 32-bit integers, so its order is free.  On the
@@ -75,7 +77,10 @@ __device__ __forceinline__ void scale_of(unsigned top, float* scale, float* inve
 }
 
 // LANES lanes of a row (up to 64: several rows in a wavefront; 256: a whole
-// workgroup).  HELD: the row fits the lanes' registers and is read once.
+// workgroup).  HELD: the row has a chunk and fits the lanes' registers, and is
+// read once: chunks that reach past its end take its last elements instead (no
+// branch: one around each load would make it wait for the load before), which
+// changes no maximum, and get the code 0 or are read again.
 template <typename T, int LANES, bool HELD>
 __global__ __launch_bounds__(256) void quant_kernel(int nrows, int ncols, const T* __restrict__ x, int64_t ldx,
                                                     int8_t* __restrict__ q, float* __restrict__ scale) {
@@ -87,42 +92,39 @@ __global__ __launch_bounds__(256) void quant_kernel(int nrows, int ncols, const 
   int64_t r = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   for (int64_t i = 0; i < rounds; ++i, r += groups) {
     const bool in = r < nrows;
-    const T* px = x + (in ? r : 0) * ldx;
-    auto fetch = [&](int c, float* v) __attribute__((always_inline)) {
-      if (c * VE + VE <= ncols) {
-        Chunk<T> ch;
-        ch.load(px + c * VE);
+    int row = in ? (int)r : 0;
+    if (LANES >= 64) row = __builtin_amdgcn_readfirstlane(row);
+    const T* px = x + (int64_t)row * ldx;
+    auto single = [&](int c, float* v) __attribute__((always_inline)) {  // an element at a time
 #pragma unroll
-        for (int k = 0; k < VE; ++k) v[k] = (float)ch.v[k];
-      } else {
-#pragma unroll
-        for (int k = 0; k < VE; ++k) v[k] = c * VE + k < ncols ? (float)px[c * VE + k] : 0.0f;
-      }
+      for (int k = 0; k < VE; ++k) v[k] = c * VE + k < ncols ? (float)px[c * VE + k] : 0.0f;
     };
-    float held[HELD ? kHeld : 1][VE];
-    // as whole numbers the magnitudes keep their order, and NaN is the largest
-    unsigned top = 0;
-    if (in) {
-      if (HELD) {
+    Chunk<T> held[HELD ? kHeld : 1];
+    Largest most;
+    if (HELD) {
 #pragma unroll
-        for (int h = 0; h < kHeld; ++h)
-          if (lane + h * LANES < nch) fetch(lane + h * LANES, held[h]);
+      for (int h = 0; h < kHeld; ++h)
+        if (h * LANES < nch) held[h].load(px + (unsigned)min((lane + h * LANES) * VE, ncols - VE));
 #pragma unroll
-        for (int h = 0; h < kHeld; ++h)
-          if (lane + h * LANES < nch)
+      for (int h = 0; h < kHeld; ++h)
+        if (h * LANES < nch)
 #pragma unroll
-            for (int k = 0; k < VE; ++k) top = max(top, __float_as_uint(held[h][k]) & 0x7fffffffu);
-      } else {
-        for (int c = lane; c < nch; c += LANES) {
-          float v[VE];
-          fetch(c, v);
+          for (int k = 0; k < VE; ++k) most.take((float)held[h].v[k]);
+    } else {
+      for (int c = lane; c < nch; c += LANES) {
+        float v[VE];
+        single(c, v);
 #pragma unroll
-          for (int k = 0; k < VE; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
-        }
+        for (int k = 0; k < VE; ++k) most.take(v[k]);
       }
     }
+    unsigned top = most.bits();
+    if (LANES < 64) {
 #pragma unroll
-    for (int m = (LANES < 64 ? LANES : 64) >> 1; m; m >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, m));
+      for (int m = LANES >> 1; m; m >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, m));
+    } else {
+      top = wave_max(top);
+    }
     if (LANES > 64) {
       __shared__ unsigned tops[4];
       __syncthreads();  // the row before has been read
@@ -136,21 +138,32 @@ __global__ __launch_bounds__(256) void quant_kernel(int nrows, int ncols, const 
     scale_of(top, &row_scale, &u);
     if (lane == 0) scale[r] = row_scale;
     int8_t* pq = q + r * ld;
-    auto put = [&](int c, float* v) __attribute__((always_inline)) {
-      if (!finite)
+    auto put = [&](int c, const float* v, float u) __attribute__((always_inline)) {
+      float w[VE];
 #pragma unroll
-        for (int k = 0; k < VE; ++k) v[k] = 0.0f;
-      codes_of<VE>(v, u, pq + c * VE);
+      for (int k = 0; k < VE; ++k) w[k] = finite ? v[k] : 0.0f;
+      codes_of<VE>(w, u, pq + c * VE);
     };
     if (HELD) {
 #pragma unroll
-      for (int h = 0; h < kHeld; ++h)
-        if (lane + h * LANES < nch) put(lane + h * LANES, held[h]);
+      for (int h = 0; h < kHeld; ++h) {
+        const int c = lane + h * LANES;
+        if (c >= nch) continue;
+        float v[VE];
+#pragma unroll
+        for (int k = 0; k < VE; ++k) v[k] = (float)held[h].v[k];
+        put(c, v, c * VE + VE <= ncols ? u : 0.0f);
+      }
+      if (ncols % VE && lane == ncols / VE % LANES) {  // the lane that wrote zeros there
+        float v[VE];
+        single(ncols / VE, v);
+        put(ncols / VE, v, u);
+      }
     } else {
       for (int c = lane; c < nch; c += LANES) {
         float v[VE];
-        fetch(c, v);
-        put(c, v);
+        single(c, v);
+        put(c, v, u);
       }
     }
   }
@@ -165,7 +178,8 @@ void launch_quant(hipStream_t s, int nrows, int ncols, const T* x, int64_t ldx, 
                        scale);
   };
   // the fewest lanes that hold a row, at most two chunks each in short rows
-  if (nch <= 16 * 2) go(quant_kernel<T, 16, true>, 16);
+  if (ncols < Chunk<T>::kElems) go(quant_kernel<T, 16, false>, 16);
+  else if (nch <= 16 * 2) go(quant_kernel<T, 16, true>, 16);
   else if (nch <= 64 * kHeld) go(quant_kernel<T, 64, true>, 64);
   else if (nch <= 256 * kHeld) go(quant_kernel<T, 256, true>, 256);
   else go(quant_kernel<T, 256, false>, 256);
@@ -451,6 +465,13 @@ bool in_fours(const Product& p, const TY* y, int64_t ldy) {
 // matrix cores work on this one's.  A row of a step is 8 chunks of 16 bytes;
 // chunk c of row r lies in slot c ^ (r & 7), so that the lanes of one LDS read
 // (16 rows, the same chunk) meet all banks.  WM x WN wavefronts.
+//
+// 8192 x 8192 x 8192 in 460 to 530 us (2.1 to 2.4e15 operations a second, the
+// more the cooler the card), 32,768 rows for 16 experts' 4096 x 4096 in 590 to
+// 650.  In the largest tile a step's LDS reads and writes (1,536 + 512 clocks)
+// take as long as its products (2,048): the matrix cores are 56% busy, at 1.8 to
+// 2.1 GHz.  Tried without gain: 32 x 32 products (610 us), four wavefronts of
+// 128 x 128 (600), wavefronts of 64 x 128 (466, with spills), priorities.
 typedef const __attribute__((address_space(1))) void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
@@ -679,6 +700,13 @@ __device__ __forceinline__ void put4_as(dpc_elem elem, void* y, int64_t at, v4i 
 // wavefront w makes channels 32 w .. 32 w + 31 of each 256, with W's rows
 // straight from L2 (each of them meets all 32 rows of the workgroup at once).
 // Chunks of codes lie as in the tiles above.
+//
+// Bound by the read of x: 1,048,576 float32 rows of 1,600 to 240 channels (7.7
+// GB) in 1.84 to 1.88 ms, 1.67 without the products, which two workgroups of a
+// CU do not hide entirely; 32,000 rows in 68 us.  Reading x past the caches
+// leaves L2 to W (1.90 -> 1.87 ms).  Tried without gain: 16 wavefronts (2.7 ms,
+// spills), three workgroups (3.2 ms, spills), W asked for before the codes are
+// done, swizzled lanes for to_rows (its bank conflicts cost nothing).
 constexpr int kCodedRows = 32, kCodedLd = 2048;
 
 template <typename TX, int TURNS>

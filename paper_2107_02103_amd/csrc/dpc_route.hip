@@ -7,7 +7,9 @@
 // A part is what one wavefront walks, 64 slots at a time: lanes with the same
 // expert find each other by one ballot per bit of the expert's number, and
 // their rank is the number of such lanes below.  No atomics: the order is the
-// same on every call.
+// same on every call.  Bound by latency: one workgroup and 3.1 us up to 16,384
+// slots, three launches and 18 us for 331,776 (1,024 slots to a workgroup; with
+// 4,096 31 us).
 //
 // Rows: the gather, the combine and its gradient move each row once and do
 // one or two FMA per element, so they are bound by HBM bandwidth (or by the
@@ -15,7 +17,9 @@
 // cut into 16-byte chunks, and the lanes of a wavefront take the chunks of one
 // row, or of several rows if a row has fewer than 33.  The last chunk of a row
 // whose width is no multiple of a chunk overlaps the one before it, so that
-// odd widths run at the same loads.
+// odd widths run at the same loads.  65,536 tokens of 8 KiB to 4 experts each:
+// gather 522 us (2.7 GB: 5.1 TB/s), combine 460 (2.7 GB: 5.8), gradient 914 (4.8
+// GB: 5.3); a copy of 2 GiB runs at 4.9 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
