@@ -7,9 +7,8 @@
 // A part is what one wavefront walks, 64 slots at a time: lanes with the same
 // expert find each other by one ballot per bit of the expert's number, and
 // their rank is the number of such lanes below.  No atomics: the order is the
-// same on every call.  Bound by latency: one workgroup and 3.1 us up to 16,384
-// slots, three launches and 18 us for 331,776 (1,024 slots to a workgroup; with
-// 4,096 31 us).
+// same on every call.  Bound by latency: 3 us for a few slots, 12 to 16 us for
+// 331,776 in three launches of 1,024 slots to a workgroup (with 4,096 31 us).
 //
 // Rows: the gather, the combine and its gradient move each row once and do
 // one or two FMA per element, so they are bound by HBM bandwidth (or by the
@@ -35,7 +34,10 @@ constexpr int64_t kMaxSlots = (int64_t)1 << 30;
 // ---------------------------------------------------------------------------
 // plan
 // ---------------------------------------------------------------------------
-constexpr int kOneBlockSlots = 16384;  // up to here one workgroup makes the whole plan
+// Up to here one workgroup makes the whole plan.  With 64 experts, us: 4,096
+// slots 9.4 so and 13.6 in three launches, 8,192 14.4 and 14.1, 16,384 24.3 and
+// 14.1 (2 experts 6.9, 10.5; 9.5, 10.6; 14.8, 10.9).
+constexpr int kOneBlockSlots = 8192;
 constexpr int kPartSlots = 1024;       // slots of a workgroup beyond that, at least
 constexpr int kMaxBlocks = 1024;
 constexpr int kPlanWaves = 4;          // wavefronts of a workgroup of the three-launch plan

@@ -61,6 +61,13 @@ def test_plan(n, k, E):
             np.testing.assert_array_equal(g, w, err_msg=name)
 
 
+@pytest.mark.parametrize("n,k,E", [(8192, 1, 5), (8193, 1, 5), (4096, 2, 70), (4097, 2, 1024), (8191, 1, 1024)])
+def test_plan_where_its_kernels_change(n, k, E):
+    e = _choices(np.random.default_rng(n), n, k, E)
+    for g, w in zip(_guarded_plan(e, E), ox.plan(e, E)):
+        np.testing.assert_array_equal(g, w)
+
+
 @pytest.mark.parametrize("n", [1, 300, 20000])
 def test_plan_of_dropped_choices_alone_and_of_one_expert(n):
     off, rows, pos = _guarded_plan(np.full((n, 2), -1, np.int32), 5)
