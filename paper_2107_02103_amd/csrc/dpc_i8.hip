@@ -442,22 +442,43 @@ void launch_few(hipStream_t s, const Product& p, const TX* x, int64_t ldx, TY* y
                      ldx, y, ldy);
 }
 
-// Four consecutive results of a row, of which `left` exist; fours: all or none
-// of them do, and their address is a multiple of their size (up to 16 bytes).
+// Which channel stands in row r of channel tile j.  A lane of the products ends
+// with rows 4 quad .. 4 quad + 3 of every tile; W's rows are dealt to the tiles so
+// that these are runs of VE channels (16 bytes of results), and the four lanes
+// that share a row of x store 64 bytes in a piece: result 4 j + q of a lane is
+// channel (4 j + q) / VE * 4 VE + quad VE + (4 j + q) % VE.  (262,144 rows of 256
+// to 1,024 channels, us, bf16, float32, float64: 211, 273, 461; with 4 channels
+// a lane for each type and a branch around each store 237, 343, 571, and these
+// past the caches 418, 305, 616.)
+template <int VE>
+__device__ __forceinline__ constexpr int channel_of(int j, int r) {
+  const int at = 4 * j + r % 4;
+  return at / VE * 4 * VE + r / 4 * VE + at % VE;
+}
+
+// r & 7 of the row r that a channel stands in: moves its chunks in LDS, so that
+// 8 lanes that read one chunk of 8 rows meet all banks.
+template <int VE>
+__device__ __forceinline__ int turn_of(int channel) {
+  return VE == 8   ? (channel & 3) | (channel >> 1 & 4)
+         : VE == 4 ? channel & 7
+                   : (channel & 1) | (channel >> 2 & 2) | (channel << 1 & 4);
+}
+
+// A run of results, of which `left` exist.
 template <typename TY>
-__device__ __forceinline__ void put4(TY* p, const TY* v, int left, bool fours) {
-  if (fours) {
-    if (left > 0) __builtin_memcpy(__builtin_assume_aligned(p, 4 * sizeof(TY) < 16 ? 4 * sizeof(TY) : 16), v, 4 * sizeof(TY));
+__device__ __forceinline__ void put_run(TY* p, const TY* v, int left) {
+  constexpr int VE = 16 / sizeof(TY);
+  typedef int Run __attribute__((ext_vector_type(4), aligned(2)));  // any address that an element may have
+  if (left >= VE) {
+    Run t;
+    __builtin_memcpy(&t, v, 16);
+    *reinterpret_cast<Run*>(p) = t;
     return;
   }
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
+  for (int q = 0; q < VE; ++q)
     if (q < left) p[q] = v[q];
-}
-
-template <typename TY>
-bool in_fours(const Product& p, const TY* y, int64_t ldy) {
-  return elem_aligned(y, 4 * sizeof(TY) < 16 ? 4 * sizeof(TY) : 16) && ldy % 4 == 0 && p.n % 4 == 0;
 }
 
 // Tiles of BM rows times BN channels, K in steps of 128 bytes: both operands
@@ -466,18 +487,20 @@ bool in_fours(const Product& p, const TY* y, int64_t ldy) {
 // chunk c of row r lies in slot c ^ (r & 7), so that the lanes of one LDS read
 // (16 rows, the same chunk) meet all banks.  WM x WN wavefronts.
 //
-// 8192 x 8192 x 8192 in 460 to 530 us (2.1 to 2.4e15 operations a second, the
-// more the cooler the card), 32,768 rows for 16 experts' 4096 x 4096 in 590 to
-// 650.  In the largest tile a step's LDS reads and writes (1,536 + 512 clocks)
+// 8192 x 8192 x 8192 in 440 to 510 us (2.2 to 2.5e15 operations a second, the
+// more the cooler the card), 32,768 rows for 16 experts' 4096 x 4096 in 540 to
+// 600.  In the largest tile a step's LDS reads and writes (1,536 + 512 clocks)
 // take as long as its products (2,048): the matrix cores are 56% busy, at 1.8 to
 // 2.1 GHz.  Tried without gain: 32 x 32 products (610 us), four wavefronts of
-// 128 x 128 (600), wavefronts of 64 x 128 (466, with spills), priorities.
+// 128 x 128 (600), wavefronts of 64 x 128 (466, with spills), priorities, halves
+// of the wavefronts that take turns at LDS and the matrix cores (463 for 446).
 typedef const __attribute__((address_space(1))) void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
 template <typename TY, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, int col_tiles,
-                                                                     TY* __restrict__ y, int64_t ldy, bool fours) {
+                                                                     TY* __restrict__ y, int64_t ldy) {
+  constexpr int VE = 16 / sizeof(TY);
   constexpr int kWaves = WM * WN, TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
   constexpr int kStep = 128, kRows = BM + BN;
   constexpr int kLoads = kRows / 8 / kWaves;  // 8 rows each
@@ -521,7 +544,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
 #pragma unroll
   for (int l = 0; l < kLoads; ++l) {
     const int r8 = (wave * kLoads + l) * 8, r = r8 + (lane >> 3);
-    const int chunk = (lane & 7) ^ (r & 7);
+    const int chunk = (lane & 7) ^ (r < BM ? r & 7 : turn_of<VE>(r));
     const int8_t* row;
     if (r < BM) {
       const int tok = token_of(p, min(t.row0 + r, t.end - 1));
@@ -555,7 +578,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
     for (int k = 0; k < 2; ++k) {
       const int slot = ((k * 4 + quad) ^ (l16 & 7)) * 16;
 #pragma unroll
-      for (int j = 0; j < NI; ++j) a[k][j] = *reinterpret_cast<const v4i*>(ws + (j * 16 + l16) * kStep + slot);
+      for (int j = 0; j < NI; ++j) a[k][j] = *reinterpret_cast<const v4i*>(ws + (channel_of<VE>(j, 0) + channel_of<VE>(0, l16)) * kStep + slot);
 #pragma unroll
       for (int i = 0; i < MI; ++i) b[k][i] = *reinterpret_cast<const v4i*>(xs + (i * 16 + l16) * kStep + slot);
     }
@@ -580,33 +603,35 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
     asm volatile("" ::: "memory");
   }
 
-  // this lane's results: row l16 of each row tile, channels 4 quad .. 4 quad + 3 of each channel tile
-  const int first = c0 + wn * TN + quad * 4;
-  float sw[NI][4], bias[NI][4];
+  // this lane's results: row l16 of each row tile, runs of VE channels from
+  // first, first + 4 VE, ...
+  constexpr int kRuns = NI * 4 / VE;
+  const int first = c0 + wn * TN + quad * VE;
+  const bool whole = c0 + BN <= p.n;
+  float sw[kRuns][VE], bias[kRuns][VE];
   const float* psw = p.sw + (int64_t)t.group * p.n;
   const float* pbias = p.bias ? p.bias + (int64_t)t.group * p.n : psw;
-  if (fours) {
+  if (whole) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int c = min(first + j * 16, p.n - 4);
-      __builtin_memcpy(sw[j], psw + c, 16);
-      __builtin_memcpy(bias[j], pbias + c, 16);
+    for (int g = 0; g < kRuns; ++g) {
+      __builtin_memcpy(sw[g], psw + first + g * 4 * VE, 4 * VE);
+      __builtin_memcpy(bias[g], pbias + first + g * 4 * VE, 4 * VE);
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
+    for (int g = 0; g < kRuns; ++g)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = min(first + j * 16 + q, p.n - 1);
-        sw[j][q] = psw[c];
-        bias[j][q] = pbias[c];
+      for (int e = 0; e < VE; ++e) {
+        const int c = min(first + g * 4 * VE + e, p.n - 1);
+        sw[g][e] = psw[c];
+        bias[g][e] = pbias[c];
       }
   }
   if (!p.bias) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
+    for (int g = 0; g < kRuns; ++g)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) bias[j][q] = 0.0f;
+      for (int e = 0; e < VE; ++e) bias[g][e] = 0.0f;
   }
   int tok[MI];
   float sx[MI];
@@ -619,15 +644,15 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
     const int r = t.row0 + wm * TM + i * 16 + l16;
     TY* py = y + (int64_t)r * ldy + first;
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      TY out[4];
+    for (int g = 0; g < kRuns; ++g) {
+      TY out[VE];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        out[q] = scaled<TY>(acc[i][j][q], (double)sx[i], sw[j][q], bias[j][q]);
-        if (tok[i] < 0) out[q] = (TY)0;  // a row of the group that no slot owns
+      for (int e = 0; e < VE; ++e) {
+        out[e] = scaled<TY>(acc[i][(g * VE + e) / 4][(g * VE + e) % 4], (double)sx[i], sw[g][e], bias[g][e]);
+        if (tok[i] < 0) out[e] = (TY)0;  // a row of the group that no slot owns
       }
-      const int left = r < t.end ? p.n - (first + j * 16) : 0;
-      put4(py + j * 16, out, left, fours);
+      const int left = r >= t.end ? 0 : whole ? VE : p.n - (first + g * 4 * VE);
+      put_run(py + g * 4 * VE, out, left);
     }
   }
 }
@@ -637,7 +662,7 @@ void launch_tiled(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
   const int col_tiles = (p.n + BN - 1) / BN;
   const unsigned per = ((unsigned)most_tiles(p, BM) * (unsigned)col_tiles + 7) / 8;
   hipLaunchKernelGGL((product_tiled_kernel<TY, BM, BN, WM, WN>), dim3(per * 8), dim3(64 * WM * WN), 0, s, p, col_tiles,
-                     y, ldy, in_fours(p, y, ldy));
+                     y, ldy);
 }
 
 // Time of the tiled product: a fixed part, and for each step of K the larger of
@@ -676,21 +701,20 @@ int product(hipStream_t s, dpc_elem elem_y, const Product& p, void* y, int64_t l
   return dpc_internal_launch_status();
 }
 
-// Four results in the type of y, of which `left` exist.
-__device__ __forceinline__ void put4_as(dpc_elem elem, void* y, int64_t at, v4i acc, double sx, const float* sw,
-                                        const float* bias, bool owned, int left, bool fours) {
-  auto put = [&](auto* py) __attribute__((always_inline)) {
-    typedef std::remove_pointer_t<decltype(py)> TY;
-    TY out[4];
+// A lane's 8 results of a row in the type of y, runs at c, c + 4 VE, ... of n.
+template <typename TY>
+__device__ __forceinline__ void put_row(TY* y, int c, int n, const v4i (&acc)[2], double sx, const float* sw,
+                                        const float* bias, bool exists, bool owned) {
+  constexpr int VE = 16 / sizeof(TY);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) out[q] = owned ? scaled<TY>(acc[q], sx, sw[q], bias[q]) : (TY)0;
-    put4(py + at, out, left, fours);
-  };
-  switch (elem) {
-    case DPC_ELEM_F64: put((double*)y); break;
-    case DPC_ELEM_F32: put((float*)y); break;
-    case DPC_ELEM_F16: put((_Float16*)y); break;
-    default: put((__bf16*)y); break;
+  for (int g = 0; g < 8 / VE; ++g) {
+    TY out[VE];
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const int at = g * VE + e;
+      out[e] = owned ? scaled<TY>(acc[at / 4][at % 4], sx, sw[at], bias[at]) : (TY)0;
+    }
+    put_run(y + c + g * 4 * VE, out, exists ? n - c - g * 4 * VE : 0);
   }
 }
 
@@ -702,8 +726,8 @@ __device__ __forceinline__ void put4_as(dpc_elem elem, void* y, int64_t at, v4i 
 // Chunks of codes lie as in the tiles above.
 //
 // Bound by the read of x: 1,048,576 float32 rows of 1,600 to 240 channels (7.7
-// GB) in 1.84 to 1.88 ms, 1.67 without the products, which two workgroups of a
-// CU do not hide entirely; 32,000 rows in 68 us.  Reading x past the caches
+// GB) in 1.83 to 1.87 ms, 1.67 without the products, which two workgroups of a
+// CU do not hide entirely; 32,000 rows in 64 us.  Reading x past the caches
 // leaves L2 to W (1.90 -> 1.87 ms).  Tried without gain: 16 wavefronts (2.7 ms,
 // spills), three workgroups (3.2 ms, spills), W asked for before the codes are
 // done, swizzled lanes for to_rows (its bank conflicts cost nothing).
@@ -711,8 +735,7 @@ constexpr int kCodedRows = 32, kCodedLd = 2048;
 
 template <typename TX, int TURNS>
 __global__ __launch_bounds__(512, 4) void coded_product_kernel(Product p, dpc_elem elem_y, const TX* __restrict__ x,
-                                                               int64_t ldx, void* __restrict__ y, int64_t ldy,
-                                                               bool fours) {
+                                                               int64_t ldx, void* __restrict__ y, int64_t ldy) {
   constexpr int VE = Chunk<TX>::kElems, kTurn = 64 * VE, kPitch = TURNS * kTurn;
   __shared__ __attribute__((aligned(16))) int8_t codes[kCodedRows * kPitch];
   __shared__ float scales[kCodedRows];
@@ -782,11 +805,15 @@ __global__ __launch_bounds__(512, 4) void coded_product_kernel(Product p, dpc_el
   __syncthreads();
 
   const int group = max(t.group, 0), steps = p.ld / 128;
+  const int ve = elem_y == DPC_ELEM_F64 ? 2 : elem_y == DPC_ELEM_F32 ? 4 : 8;
+  auto channel = [&](int j, int r) __attribute__((always_inline)) {
+    return ve == 2 ? channel_of<2>(j, r) : ve == 4 ? channel_of<4>(j, r) : channel_of<8>(j, r);
+  };
   for (int c0 = wave * 32; c0 < p.n; c0 += 256) {
     const int8_t* pw[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
-      pw[j] = p.qw + ((int64_t)group * p.n + min(c0 + j * 16 + (lane >> 2), p.n - 1)) * p.ld + (lane & 3) * 16;
+      pw[j] = p.qw + ((int64_t)group * p.n + min(c0 + channel(j, lane >> 2), p.n - 1)) * p.ld + (lane & 3) * 16;
     v4i acc[2][2], a0[2][2], a1[2][2];  // a0, a1: W of two steps, on their way
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -827,22 +854,27 @@ __global__ __launch_bounds__(512, 4) void coded_product_kernel(Product p, dpc_el
     if (s < steps) step(s, a0);
     const float* psw = p.sw + (int64_t)group * p.n;
     const float* pbias = p.bias ? p.bias + (int64_t)group * p.n : psw;
+    float sw[8], bias[8];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int c = c0 + j * 16 + quad * 4;
-      float sw[4], bias[4];
+    for (int q = 0; q < 8; ++q) {
+      const int c = min(c0 + channel(q / 4, quad * 4 + q % 4), p.n - 1);
+      sw[q] = psw[c];
+      bias[q] = pbias[c];
+      if (!p.bias) bias[q] = 0.0f;
+    }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        sw[q] = psw[min(c + q, p.n - 1)];
-        bias[q] = pbias[min(c + q, p.n - 1)];
-        if (!p.bias) bias[q] = 0.0f;
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = t.row0 + i * 16 + l16;
-        const bool owned = t.group >= 0 && r < t.end && token_of(p, r) >= 0;
-        put4_as(elem_y, y, (int64_t)r * ldy + c, acc[i][j], (double)scales[i * 16 + l16], sw, bias, owned,
-                r < t.end ? p.n - c : 0, fours);
+    for (int i = 0; i < 2; ++i) {
+      const int r = t.row0 + i * 16 + l16, c = c0 + quad * ve;
+      const bool exists = r < t.end, owned = exists && t.group >= 0 && token_of(p, r) >= 0;
+      const double sx = (double)scales[i * 16 + l16];
+      auto put = [&](auto* py) __attribute__((always_inline)) {
+        put_row(py + (int64_t)r * ldy, c, p.n, acc[i], sx, sw, bias, exists, owned);
+      };
+      switch (elem_y) {
+        case DPC_ELEM_F64: put((double*)y); break;
+        case DPC_ELEM_F32: put((float*)y); break;
+        case DPC_ELEM_F16: put((_Float16*)y); break;
+        default: put((__bf16*)y); break;
       }
     }
   }
@@ -863,11 +895,8 @@ void launch_coded(hipStream_t s, const Product& p, dpc_elem elem_y, const TX* x,
     if (p.ld > TURNS * kTurn)
       return launch_coded<TX, sizeof(TX) == 8 ? 2 * TURNS : TURNS + 1>(s, p, elem_y, x, ldx, y, ldy);
   }
-  const bool fours = elem_y == DPC_ELEM_F64   ? in_fours(p, (double*)y, ldy)
-                     : elem_y == DPC_ELEM_F32 ? in_fours(p, (float*)y, ldy)
-                                              : in_fours(p, (_Float16*)y, ldy);
   hipLaunchKernelGGL((coded_product_kernel<TX, TURNS>), dim3((unsigned)most_tiles(p, kCodedRows)), dim3(512), 0, s, p,
-                     elem_y, x, ldx, y, ldy, fours);
+                     elem_y, x, ldx, y, ldy);
 }
 
 template <typename TX>
