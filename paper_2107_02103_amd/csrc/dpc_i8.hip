@@ -665,25 +665,28 @@ void launch_tiled(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
                      y, ldy);
 }
 
-// Time of the tiled product: a fixed part, and for each step of K the larger of
-// one tile's time alone and the time of the tiles of a CU one after the other.
+// Time of the tiled product: a fixed part, for each step of K the larger of one
+// tile's time alone and the time of the tiles of a CU one after the other, and
+// each tile's start and stores.
 // Measured on 256 CUs (us, bf16 results; 256x256, 128x128, 128x64, 64x64 tiles):
-//   4096 x 4096 x 4096   76.8  87.5 106.8 124.4     1024 x 8192 x 4096  54.0 39.0 48.7 55.7
-//   2048 x 2048 x 2048   32.4  16.4  14.4  17.4     32000 x 240 x 1600  28.8 21.9 26.1 26.8
-//   512 x 4096 x 4096    50.3  23.6  19.8  18.2     16000 x 240 x 1600  25.6 14.6 13.2 14.9
-//   256 x 4096 x 4096    50.3  21.5  14.4  11.4     4000 x 240 x 1600   24.4 12.1  8.3  6.8
-double tiled_cost(const Product& p, int bm, int bn, double fixed, double alone, double each) {
+//   4096 x 4096 x 4096   73.8  84.5 103.4 121.6     1024 x 8192 x 4096  53.0 39.5 52.8 53.6
+//   2048 x 2048 x 2048   29.2  15.8  14.0  16.9     32000 x 240 x 1600  27.9 23.5 25.9 27.6
+//   512 x 4096 x 4096    47.4  22.7  20.1  16.8     16000 x 240 x 1600  25.6 14.7 13.7 15.0
+//   256 x 4096 x 4096    46.6  20.8  14.1  11.1     4000 x 240 x 1600   24.7 12.1  8.5  6.9
+//   8192 x 2048 x 512    17.6  20.2  20.6  23.3     32000 x 512 x 512   17.8 22.3 21.2 24.1
+//   262144 x 1024 x 256   205   245   249   291     131072 x 1600 x 240  163  182  183  215
+double tiled_cost(const Product& p, int bm, int bn, double fixed, double alone, double each, double stores) {
   const int64_t tiles = most_tiles(p, bm) * ((p.n + bn - 1) / bn);
   if (tiles >= 1 << 22) fixed += 1e30 / bm;  // more threads than a launch has: the largest tile, if any
-  const double cu = each * (double)((tiles + 255) / 256);
-  return fixed + p.ld / 128 * (alone > cu ? alone : cu);
+  const double turns = (double)((tiles + 255) / 256), cu = each * turns;
+  return fixed + p.ld / 128 * (alone > cu ? alone : cu) + stores * turns;
 }
 
 template <typename TY>
 void launch_product(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
   if (few_rows(p)) return launch_few(s, p, p.qx, 0, y, ldy);
-  const double big = tiled_cost(p, 256, 256, 8.0, 1.35, 1.9), mid = tiled_cost(p, 128, 128, 5.0, 0.7, 0.64),
-               low = tiled_cost(p, 128, 64, 4.0, 0.5, 0.35), small = tiled_cost(p, 64, 64, 3.3, 0.25, 0.22);
+  const double big = tiled_cost(p, 256, 256, 8.0, 1.35, 1.9, 4.0), mid = tiled_cost(p, 128, 128, 5.0, 0.7, 0.64, 1.4),
+               low = tiled_cost(p, 128, 64, 4.0, 0.5, 0.35, 0.95), small = tiled_cost(p, 64, 64, 3.3, 0.25, 0.22, 0.5);
   if (big <= mid && big <= low && big <= small) return launch_tiled<TY, 256, 256, 2, 4>(s, p, y, ldy);
   if (mid <= low && mid <= small) return launch_tiled<TY, 128, 128, 2, 2>(s, p, y, ldy);
   if (low <= small) return launch_tiled<TY, 128, 64, 2, 2>(s, p, y, ldy);
