@@ -10,6 +10,7 @@ from . import binding as B
 
 _lib, _elem_of = B._lib, B.elem_of
 _raw_stream = torch._C._cuda_getCurrentRawStream   # hipStream_t of a device's current stream
+_current_device = torch._C._cuda_getDevice
 
 
 def _check(status, where):
@@ -43,6 +44,17 @@ def _on(x, device, name):
         raise ValueError(f"{name} is on {x.device}, the others are on cuda:{device}")
 
 
+def _elsewhere(device, stream):
+    """What a call on tensors of `device` has to enter first: that stream, or the
+    device if another is current (the library launches on the current one); None
+    if it can go ahead."""
+    if stream is not None:
+        if stream.device.index != device:
+            raise ValueError(f"stream is on {stream.device}, the tensors are on cuda:{device}")
+        return torch.cuda.stream(stream)               # makes the device current too
+    return None if _current_device() == device else torch.cuda.device(device)
+
+
 class Route:
     """Plan that sends each token's row to the experts it chooses and back.
 
@@ -54,17 +66,19 @@ class Route:
              empty rows at the end
     pos      int32 [tokens, topk]: row of each choice, -1 if it is dropped
 
-    stream: a torch stream that the call runs on, and for which its outputs are
-    allocated (default: the current one)."""
+    A call runs on the GPU of its tensors, whichever is current.
+    stream: a torch stream of that GPU that the call runs on, and for which its
+    outputs are allocated (default: the current one)."""
 
     def __init__(self, expert, nexpert, stream=None):
-        if stream is not None:
-            with torch.cuda.stream(stream):
-                return Route.__init__(self, expert, nexpert)
         if expert.dtype != torch.int32 or expert.dim() not in (1, 2) or not expert.is_contiguous():
             raise ValueError("expert must be contiguous int32 [tokens, topk] or [tokens]")
         _on(expert, None, "expert")
         self._device = dev = expert.get_device()
+        at = _elsewhere(dev, stream)
+        if at is not None:
+            with at:
+                return Route.__init__(self, expert, nexpert)
         self.ntok, self.topk = expert.shape if expert.dim() == 2 else (expert.shape[0], 1)
         self.nexpert = int(nexpert)
         m, head = self.ntok * self.topk, max(self.nexpert, 0) + 1
@@ -74,9 +88,9 @@ class Route:
         ws = expert.new_empty((nb + 3) // 4)
         self.offsets, self.rows, pos = buf.split_with_sizes((head, m, m))
         self.pos = pos.view(self.ntok, self.topk)
-        at = buf.data_ptr()
+        first = buf.data_ptr()
         _check(_lib.dpc_route_plan(_raw_stream(dev), self.ntok, self.topk, self.nexpert, expert.data_ptr(),
-                                   ws.data_ptr(), nb, at, at + 4 * head, at + 4 * (head + m)), "dpc_route_plan")
+                                   ws.data_ptr(), nb, first, first + 4 * head, first + 4 * (head + m)), "dpc_route_plan")
 
     @classmethod
     def from_plan(cls, offsets, rows, pos):
@@ -107,8 +121,9 @@ class Route:
     def gather(self, x, weight=None, out=None, stream=None):
         """[tokens * topk, width]: each row the token's row (times its weight),
         zeros in the empty rows.  With weights, the gradient of combine()."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
+        at = _elsewhere(self._device, stream)
+        if at is not None:
+            with at:
                 return self.gather(x, weight, out)
         dev, m = self._device, self.ntok * self.topk
         ldx, width = _rows(x, "x", self.ntok, None, None, dev), x.shape[1]
@@ -124,8 +139,9 @@ class Route:
     def combine(self, x, weight=None, out=None, stream=None):
         """[tokens, width]: the sum of each token's rows (times their weights);
         without weights, the gradient of gather()."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
+        at = _elsewhere(self._device, stream)
+        if at is not None:
+            with at:
                 return self.combine(x, weight, out)
         dev = self._device
         ldx, width = _rows(x, "rows", self.ntok * self.topk, None, None, dev), x.shape[1]
@@ -141,8 +157,9 @@ class Route:
     def combine_backward(self, x, dy, weight=None, need_rows=True, stream=None):
         """Gradient of combine(x, weight) from dE/dy: (dE/dx, dE/dweight); the
         second is None without weights, the first with need_rows=False."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
+        at = _elsewhere(self._device, stream)
+        if at is not None:
+            with at:
                 return self.combine_backward(x, dy, weight, need_rows)
         dev, m = self._device, self.ntok * self.topk
         ldx, width = _rows(x, "rows", m, None, None, dev), x.shape[1]
@@ -188,13 +205,14 @@ class Int8Linear:
     def from_weight(cls, weight, bias=None, stream=None):
         """Codes the rows (output channels) of weight [experts, outer, inner] or
         [outer, inner]; bias of any floating type."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
-                return cls.from_weight(weight, bias)
         w = weight[None] if weight.dim() == 2 else weight
         if w.dim() != 3:
             raise ValueError("weight must be [experts, outer, inner] or [outer, inner]")
         _on(w, None, "weight")
+        at = _elsewhere(w.get_device(), stream)
+        if at is not None:
+            with at:
+                return cls.from_weight(weight, bias)
         g, n, k = w.shape
         w = w.contiguous()
         codes = torch.empty((g, n, B.i8_ld(k)), dtype=torch.int8, device=w.device)
@@ -210,8 +228,9 @@ class Int8Linear:
         tokens and y its rows (each from its expert's layer); with offsets
         (int32 [experts + 1]), the rows of x are sorted by expert already.
         dtype: type of y (default: that of x)."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
+        at = _elsewhere(self._device, stream)
+        if at is not None:
+            with at:
                 return self(x, route, offsets, dtype, out)
         dev = self._device
         ldx = _rows(x, "x", None if route is None else route.ntok, self.inner, None, dev)
