@@ -505,11 +505,25 @@ def _wdtype(elem):
     return torch.float64 if int(elem) == DPC_ELEM_F64 else torch.float32
 
 
+INT_MAX = 2 ** 31 - 1
+
+
+def _sizes(where, *sizes):
+    """Refuses sizes that are no C int: ctypes would drop their high bits, and the
+    library would see a small size that passes its checks."""
+    for v in sizes:
+        if not -INT_MAX <= int(v) <= INT_MAX:
+            raise DpcError(DPC_ENOTSUP if v > 0 else DPC_EINVAL, where)
+
+
 def dpc_route_workspace_bytes(ntok, topk, nexpert):
+    if max(ntok, topk, nexpert) > INT_MAX or min(ntok, topk, nexpert) < 0:
+        return 0
     return int(_lib.dpc_route_workspace_bytes(int(ntok), int(topk), int(nexpert)))
 
 
 def dpc_route_plan(stream, ntok, topk, nexpert, expert, workspace, workspace_bytes, offsets, rows, pos):
+    _sizes("dpc_route_plan", ntok, topk, nexpert)
     m, i32 = int(ntok) * int(topk), torch.int32
     args = (_flat_ptr(expert, m, i32, "expert"), _flat_ptr(workspace, int(workspace_bytes), torch.uint8, "workspace"),
             int(workspace_bytes), _flat_ptr(offsets, int(nexpert) + 1, i32, "offsets"), _flat_ptr(rows, m, i32, "rows"),
@@ -519,6 +533,7 @@ def dpc_route_plan(stream, ntok, topk, nexpert, expert, workspace, workspace_byt
 
 
 def dpc_route_gather(stream, elem, ntok, topk, width, x, ldx, weight, rows, pos, y, ldy):
+    _sizes("dpc_route_gather", ntok, topk, width)
     m, dt = int(ntok) * int(topk), _elem_dtype(elem, "dpc_route_gather")
     args = (_rows_ptr(x, ntok, width, ldx, dt, "x"), int(ldx), _flat_ptr(weight, m, _wdtype(elem), "weight"),
             _flat_ptr(rows, m, torch.int32, "rows"), _flat_ptr(pos, m, torch.int32, "pos"),
@@ -529,6 +544,7 @@ def dpc_route_gather(stream, elem, ntok, topk, width, x, ldx, weight, rows, pos,
 
 
 def dpc_route_combine(stream, elem, ntok, topk, width, x, ldx, weight, pos, y, ldy):
+    _sizes("dpc_route_combine", ntok, topk, width)
     m, dt = int(ntok) * int(topk), _elem_dtype(elem, "dpc_route_combine")
     args = (_rows_ptr(x, m, width, ldx, dt, "x"), int(ldx), _flat_ptr(weight, m, _wdtype(elem), "weight"),
             _flat_ptr(pos, m, torch.int32, "pos"), _rows_ptr(y, ntok, width, ldy, dt, "y"), int(ldy))
@@ -538,6 +554,7 @@ def dpc_route_combine(stream, elem, ntok, topk, width, x, ldx, weight, pos, y, l
 
 
 def dpc_route_combine_bwd(stream, elem, ntok, topk, width, x, ldx, weight, rows, pos, dy, lddy, dx, lddx, dweight):
+    _sizes("dpc_route_combine_bwd", ntok, topk, width)
     m, dt = int(ntok) * int(topk), _elem_dtype(elem, "dpc_route_combine_bwd")
     wt, i32 = _wdtype(elem), torch.int32
     args = (_rows_ptr(x, m, width, ldx, dt, "x"), int(ldx), _flat_ptr(weight, m, wt, "weight"),
@@ -549,6 +566,7 @@ def dpc_route_combine_bwd(stream, elem, ntok, topk, width, x, ldx, weight, rows,
 
 
 def dpc_quant_rows(stream, elem, nrows, ncols, x, ldx, q, scale):
+    _sizes("dpc_quant_rows", nrows, ncols)
     dt = _elem_dtype(elem, "dpc_quant_rows")
     args = (_rows_ptr(x, nrows, ncols, ldx, dt, "x"), int(ldx),
             _flat_ptr(q, int(nrows) * i8_ld(ncols), torch.int8, "q"),
@@ -558,6 +576,7 @@ def dpc_quant_rows(stream, elem, nrows, ncols, x, ldx, q, scale):
 
 
 def _layer_args(elem_y, ntok, topk, n, k, ngroup, rows, offsets, qw, sw, bias, y, ldy, where):
+    _sizes(where, ntok, topk, n, k, ngroup)
     m, f32 = int(ntok) * int(topk), torch.float32
     head = (_flat_ptr(rows, m, torch.int32, "rows"), _flat_ptr(offsets, int(ngroup) + 1, torch.int32, "offsets"),
             _flat_ptr(qw, int(ngroup) * int(n) * i8_ld(k), torch.int8, "qw"),
@@ -574,6 +593,8 @@ def dpc_matmul_i8(stream, elem_y, ntok, topk, n, k, ngroup, qx, sx, rows, offset
 
 
 def dpc_linear_i8_workspace_bytes(ntok, k):
+    if max(ntok, k) > INT_MAX or min(ntok, k) < 0:
+        return 0
     return int(_lib.dpc_linear_i8_workspace_bytes(int(ntok), int(k)))
 
 

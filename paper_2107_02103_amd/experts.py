@@ -18,6 +18,12 @@ def _check(status, where):
         raise B.DpcError(status, where)
 
 
+def _sizes(where, most):
+    """Refuses a call whose largest size is no C int (ctypes would drop its high bits)."""
+    if most > B.INT_MAX:
+        raise B.DpcError(B.DPC_ENOTSUP, where)
+
+
 def _rows(x, name, n=None, width=None, dtype=None, device=None):
     """Checks a tensor of rows (unit stride inside a row, rows apart by any
     stride that does not make them overlap); returns its row stride."""
@@ -82,6 +88,7 @@ class Route:
         self.ntok, self.topk = expert.shape if expert.dim() == 2 else (expert.shape[0], 1)
         self.nexpert = int(nexpert)
         m, head = self.ntok * self.topk, max(self.nexpert, 0) + 1
+        _sizes("dpc_route_plan", max(m, abs(self.nexpert)))
         nb = _lib.dpc_route_workspace_bytes(self.ntok, self.topk, self.nexpert)
         # the three of the plan in one allocation
         buf = expert.new_empty(head + 2 * m)
@@ -106,6 +113,7 @@ class Route:
         r.offsets, r.rows, r.pos = offsets, rows, pos
         r.ntok, r.topk = pos.shape
         r.nexpert = len(offsets) - 1
+        _sizes("dpc_route_plan", max(r.ntok, r.topk, r.nexpert))
         return r
 
     def _weight(self, weight, x):
@@ -127,6 +135,7 @@ class Route:
                 return self.gather(x, weight, out)
         dev, m = self._device, self.ntok * self.topk
         ldx, width = _rows(x, "x", self.ntok, None, None, dev), x.shape[1]
+        _sizes("dpc_route_gather", width)
         if out is None:
             out, ldy = x.new_empty((m, width)), width or 1
         else:
@@ -145,6 +154,7 @@ class Route:
                 return self.combine(x, weight, out)
         dev = self._device
         ldx, width = _rows(x, "rows", self.ntok * self.topk, None, None, dev), x.shape[1]
+        _sizes("dpc_route_combine", width)
         if out is None:
             out, ldy = x.new_empty((self.ntok, width)), width or 1
         else:
@@ -163,6 +173,7 @@ class Route:
                 return self.combine_backward(x, dy, weight, need_rows)
         dev, m = self._device, self.ntok * self.topk
         ldx, width = _rows(x, "rows", m, None, None, dev), x.shape[1]
+        _sizes("dpc_route_combine_bwd", width)
         lddy = _rows(dy, "dy", self.ntok, width, x.dtype, dev)
         w = self._weight(weight, x)
         if weight is None and not need_rows:
@@ -193,6 +204,7 @@ class Int8Linear:
         self._device = codes.get_device()
         _on(codes, None, "codes")
         self.experts, self.outer = shape[:2]
+        _sizes("dpc_linear_i8", max(self.inner, self.experts, self.outer))
         for name, t in (("scales", scales), ("bias", bias)):
             if t is None:
                 continue
@@ -214,6 +226,7 @@ class Int8Linear:
             with at:
                 return cls.from_weight(weight, bias)
         g, n, k = w.shape
+        _sizes("dpc_quant_rows", max(g * n, k))
         w = w.contiguous()
         codes = torch.empty((g, n, B.i8_ld(k)), dtype=torch.int8, device=w.device)
         scales = torch.empty((g, n), dtype=torch.float32, device=w.device)
@@ -235,6 +248,7 @@ class Int8Linear:
         dev = self._device
         ldx = _rows(x, "x", None if route is None else route.ntok, self.inner, None, dev)
         ntok, topk, rows = x.shape[0], 1, None
+        _sizes("dpc_linear_i8", ntok)
         if route is not None:
             if offsets is not None:
                 raise ValueError("give a route or offsets, not both")
