@@ -378,8 +378,9 @@ int dpc_route_plan(void* stream, int ntok, int topk, int nexpert, const int* exp
  *   rows, pos  the plan
  *   y       device out [nslot] rows, ldy elements apart
  * Products are rounded once from float64 (DPC_ELEM_F64) or float32.  Rows
- * need the alignment of their elements alone.  Requires width >= 1, ldx and
- * ldy >= width.  Inputs and outputs must not overlap.                       */
+ * need the alignment of their elements alone.  Requires 1 <= width <= 2^31 -
+ * 128 (DPC_ENOTSUP above), ldx and ldy >= width.  Inputs and outputs must not
+ * overlap.                                                                  */
 int dpc_route_gather(void* stream, dpc_elem elem, int ntok, int topk, int width, const void* x,
                      int64_t ldx, const void* weight, const int* rows, const int* pos, void* y,
                      int64_t ldy);

@@ -30,6 +30,7 @@
 namespace {
 
 constexpr int64_t kMaxSlots = (int64_t)1 << 30;
+constexpr int kMaxWidth = INT32_MAX - 127;  // a lane's next element (64 on) and a width rounded up to chunks are ints
 
 // ---------------------------------------------------------------------------
 // plan
@@ -439,7 +440,7 @@ unsigned grid_for(int64_t items, int lanes_log2) {
 // DPC_OK and the shape of a call on rows, or why it is refused
 int row_shape(dpc_elem elem, int ntok, int topk, int width, Shape* sh) {
   if (!elem_ok(elem) || ntok < 0 || topk < 1 || width < 1) return DPC_EINVAL;
-  if (topk > DPC_MAX_TOPK || (int64_t)ntok * topk > kMaxSlots) return DPC_ENOTSUP;
+  if (topk > DPC_MAX_TOPK || (int64_t)ntok * topk > kMaxSlots || width > kMaxWidth) return DPC_ENOTSUP;
   *sh = Shape{(int64_t)ntok * topk, ntok, topk, width, log2_lanes(width, elem_size(elem))};
   return DPC_OK;
 }
