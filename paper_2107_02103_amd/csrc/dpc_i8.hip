@@ -899,11 +899,24 @@ __global__ __launch_bounds__(512, 4) void coded_product_kernel(Product p, dpc_el
   }
 }
 
-// Whether the rows of the layer are few enough to be held: a chunk at least, and
-// the codes of 32 rows twice in LDS.
+// Whether the rows of the layer are short enough to be held (a chunk at least, and
+// the codes of 32 rows twice in LDS), and one kernel faster than two.  Both, us,
+// 240 channels, one kernel and two:
+//   float32, 1,600 columns     512 rows 13.4 13.8, 2,048 13.9 15.0, 8,192 17.4 24.9, 262,144 462 611
+//   bfloat16, 1,600 columns    256 rows 13.7 13.3, 2,048 14.0 14.6, 8,192 15.5 22.9, 262,144 337 448
+//   float64, 1,024 columns     512 rows 11.6 12.3, 2,048 12.9 13.5, 8,192 20.0 25.8, 262,144 512 676
+//   float64, 1,600 columns     512 rows 18.8 13.7, 8,192 34.6 34.9, 16,000 60.4 57.5, 24,000 91.6 91.4,
+//                              32,000 116 123, 524,288 1,768 1,856 (27 registers of its kernel spill)
+//   bfloat16, 240 columns      8,192 rows 8.6 11.3, 32,000 18.9 21.4, 50,000 30.0 27.1, 262,144 129 101
+//   float32, 128 columns       8,192 rows 8.8 11.3, 32,000 17.8 18.8, 50,000 28.3 24.3, 262,144 122 111
+//   float32, 129 columns       8,192 rows 9.1 12.5, 32,000 21.7 27.3, 50,000 35.4 36.9, 262,144 166 188
+// Up to 32 chunks leave half of a wavefront without one while it codes.
 template <typename TX>
 bool coded_fits(const Product& p) {
-  return p.k >= Chunk<TX>::kElems && p.ld <= kCodedLd;
+  const int chunks = p.ld / Chunk<TX>::kElems;
+  if (p.k < Chunk<TX>::kElems || p.ld > kCodedLd) return false;
+  if (chunks <= 32) return p.m <= 32768;
+  return chunks <= 64 * 8 || p.m >= 24000;
 }
 
 template <typename TX, int TURNS = 1>
@@ -931,11 +944,12 @@ void few_by_type(hipStream_t s, const Product& p, dpc_elem elem_y, const TX* x, 
 // The layer in one kernel, if it is one for that: true and its status.
 bool coded_product(hipStream_t s, dpc_elem elem_x, dpc_elem elem_y, const Product& p, const void* x, int64_t ldx, void* y,
                    int64_t ldy, int* status) {
-  // both sides, us (float32 rows of 1,600; 240 channels): 2,048 rows 13.9 here
-  // and 16.0 in two kernels, 8,192 18.1 and 26.2, 262,144 500 and 581; with 512
-  // channels the products take longer here than the codes' way through memory
-  // (2,048 rows 21.5 and 16.4, 32,000 99 and 92, 262,144 742 and 730).  Rows
-  // that go to several experts would be coded once for each.
+  // Up to 256 channels, which a workgroup makes in one turn (coded_fits has both
+  // sides' times).  With 320 and 512 channels of float32 rows of 1,600 this kernel
+  // takes 16.6 and 21.1 us where two take 15.6 and 15.8 at 2,048 rows, 72 and 88
+  // where they take 89 and 97 at 32,000, of bfloat16 rows of 240 157 and 183 where
+  // they take 128 and 139 at 262,144.  Rows that go to several experts would be
+  // coded once for each.
   // Few rows in all, short ones: every workgroup codes them again, one row in
   // each wavefront, which costs less than a launch (one row of 1,600 to 240
   // channels 5.4 us and 7.2 in two kernels, 8 rows 6.2 and 7.6; but 16 rows

@@ -1,0 +1,46 @@
+"""Layers of up to 256 channels where one kernel gives way to two: short rows past
+32,768, and float64 rows of more than 1,024 elements up to 24,000.  The result
+is the same on both sides: the sums are exact, and the rest is one rounding."""
+import numpy as np
+import pytest
+
+import oracle.experts as ox
+from tests.test_gpu_i8 import TYPES, _check, _groups, _layer, _padded
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def _both_sides(t, k, n, few, many, experts):
+    """Rows of a layer for `many` rows and for `few` of the same ones, against the plain product."""
+    import paper_2107_02103_amd as P
+    rng = np.random.default_rng(k + n)
+    x = torch.from_numpy(rng.standard_normal((many, k)) * np.exp(rng.standard_normal((many, 1)))).to(TYPES[t]).cuda()
+    x[5] = 0
+    x[many - 2, k - 1] = float("nan")
+    x[many - 1, 0] = float("-inf")
+    qw, sw, b = _layer(rng, experts, n, k)
+    lin = P.Int8Linear(_padded(qw, P.i8_ld(k)), torch.from_numpy(sw).cuda(), k, torch.from_numpy(b).cuda())
+    qx, sx = ox.codes(x.cpu().double().numpy())
+    got = {}
+    for rows in (slice(many - few, many), slice(0, many)):
+        m = rows.stop - rows.start
+        off = np.linspace(0, m - 9, experts + 1).astype(np.int64) if experts > 1 else np.array([0, m])
+        want, mag = ox.product(qx[rows], sx[rows], qw, sw, b, _groups(off, m, experts))
+        y = lin(x[rows], offsets=torch.from_numpy(off.astype(np.int32)).cuda())
+        _check(y, want, mag, t)
+        got[m] = y
+    if experts == 1:
+        assert torch.equal(torch.nan_to_num(got[many][-few:], nan=1.25), torch.nan_to_num(got[few], nan=1.25))
+
+
+@pytest.mark.parametrize("experts", [1, 3])
+@pytest.mark.parametrize("t,k", [("bf16", 240), ("f16", 7 * 8 + 3), ("bf16", 256), ("f32", 128), ("f32", 5)])
+def test_short_rows(t, k, experts):
+    _both_sides(t, k, 40, 32768, 32769, experts)
+
+
+@pytest.mark.parametrize("experts", [1, 3])
+@pytest.mark.parametrize("k", [1025, 1601, 2048])
+def test_long_rows_of_64_bits(k, experts):
+    _both_sides("f64", k, 24, 23999, 24000, experts)
