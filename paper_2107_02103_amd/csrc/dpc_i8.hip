@@ -322,8 +322,8 @@ __device__ __forceinline__ v4i to_rows(v4i w) {
 
 // Few rows: 16 rows times 16 channels of y for each `share` wavefronts of a
 // workgroup of 8, which take the steps of K in turn and whose sums are added in
-// LDS.  W is read once, 8 KiB of it under way in every wavefront: bound by that
-// read, or for short rows by latency.  TX is the type of rows that the workgroup
+// LDS.  W is read once for each 16 rows of an expert, 8 KiB of it under way in
+// every wavefront: bound by that read, or for short rows by latency.  TX is the type of rows that the workgroup
 // codes itself (into LDS), or int8_t for rows that are codes already.
 constexpr int kFewWaves = 8, kFewAhead = 4;
 
@@ -437,9 +437,22 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_product_kernel(Product p, 
   }
 }
 
-// Whether at most 16 rows share an expert's weights, on average.
+// Whether few enough rows share an expert's weights for tiles of 16 rows: at most
+// 16 for one layer; for experts, whose rows the host does not know one by one, by
+// the rows in all and their average.  Device times, us, few rows and the kernels
+// that take over, even choice and (in brackets) a share of 1 / e^2 for expert e:
+//   bfloat16, 4,096 x 4,096      64 experts, 4 rows each 209 211 (78 78), 8 223 217 (144 143), 16 277 223
+//                                (209 154), 64 552 317 (521 316); 256 experts, 8 rows 799 837 (371 275);
+//                                3 experts, 48 rows in all 24.8 26.5, 64 24.5 26.6, 128 35.6 26.9
+//   bfloat16, 1,024 x 1,024      256 experts, 4 rows 53 68 (26 21), 8 60 75 (36 28), 16 73 78 (53 42)
+//   float32, 1,600 to 240        64 experts, 8 rows 14.2 16.9 (12.0 16.0), 16 19.5 17.3 (17.1 16.2), 64 35.9 20.6;
+//                                256 experts, 2 rows 25.7 22.7, 8 32.7 25.1 (24.4 18.7), 16 38 26 (31 20)
+// A busy expert's W is read again for each of its 16-row tiles: with few rows on
+// average and most of them on one of many experts that still costs up to a half.
 inline bool few_rows(const Product& p) {
-  return (p.offsets ? ((int64_t)p.m + p.ngroup - 1) / p.ngroup : p.m) <= 16;
+  if (!p.offsets) return p.m <= 16;
+  if (p.n <= 256) return p.m <= 512 && p.m <= 16 * p.ngroup;
+  return p.m <= 64 || p.m <= 8 * p.ngroup;
 }
 
 template <typename TX, typename TY>
@@ -900,16 +913,16 @@ __global__ __launch_bounds__(512, 4) void coded_product_kernel(Product p, dpc_el
 }
 
 // Whether the rows of the layer are short enough to be held (a chunk at least, and
-// the codes of 32 rows twice in LDS), and one kernel faster than two.  Both, us,
-// 240 channels, one kernel and two:
-//   float32, 1,600 columns     512 rows 13.4 13.8, 2,048 13.9 15.0, 8,192 17.4 24.9, 262,144 462 611
-//   bfloat16, 1,600 columns    256 rows 13.7 13.3, 2,048 14.0 14.6, 8,192 15.5 22.9, 262,144 337 448
-//   float64, 1,024 columns     512 rows 11.6 12.3, 2,048 12.9 13.5, 8,192 20.0 25.8, 262,144 512 676
-//   float64, 1,600 columns     512 rows 18.8 13.7, 8,192 34.6 34.9, 16,000 60.4 57.5, 24,000 91.6 91.4,
-//                              32,000 116 123, 524,288 1,768 1,856 (27 registers of its kernel spill)
-//   bfloat16, 240 columns      8,192 rows 8.6 11.3, 32,000 18.9 21.4, 50,000 30.0 27.1, 262,144 129 101
-//   float32, 128 columns       8,192 rows 8.8 11.3, 32,000 17.8 18.8, 50,000 28.3 24.3, 262,144 122 111
-//   float32, 129 columns       8,192 rows 9.1 12.5, 32,000 21.7 27.3, 50,000 35.4 36.9, 262,144 166 188
+// the codes of 32 rows twice in LDS), and one kernel faster than two.  Device
+// times, us, 240 channels, one kernel and two:
+//   float32, 1,600 columns     512 rows 13.4 13.6, 2,048 14.1 15.2, 8,192 17.6 25.3, 262,144 468 616
+//   bfloat16, 1,600 columns    256 rows 13.7 12.9, 2,048 14.3 15.2, 8,192 16.0 23.0, 262,144 337 444
+//   float64, 1,024 columns     512 rows 11.5 11.8, 2,048 12.9 13.3, 8,192 20.1 26.1, 262,144 512 675
+//   float64, 1,600 columns     512 rows 20.2 13.7, 8,192 35.0 35.2, 16,000 61.1 58.1, 24,000 90.0 91.5,
+//                              32,000 116 122, 524,288 1,771 1,855 (27 registers of its kernel spill)
+//   bfloat16, 240 columns      512 rows 6.8 7.5, 8,192 7.7 9.4, 32,000 18.9 20.6, 50,000 33.0 29.7, 262,144 131 103
+//   float32, 128 columns       512 rows 5.6 6.6, 8,192 6.9 8.5, 32,000 17.6 18.8, 50,000 30.8 26.7, 262,144 126 114
+//   float32, 129 columns       512 rows 6.5 7.2, 8,192 7.9 11.1, 32,000 21.5 26.4, 50,000 38.3 40.0, 262,144 170 192
 // Up to 32 chunks leave half of a wavefront without one while it codes.
 template <typename TX>
 bool coded_fits(const Product& p) {
@@ -946,9 +959,9 @@ bool coded_product(hipStream_t s, dpc_elem elem_x, dpc_elem elem_y, const Produc
                    int64_t ldy, int* status) {
   // Up to 256 channels, which a workgroup makes in one turn (coded_fits has both
   // sides' times).  With 320 and 512 channels of float32 rows of 1,600 this kernel
-  // takes 16.6 and 21.1 us where two take 15.6 and 15.8 at 2,048 rows, 72 and 88
-  // where they take 89 and 97 at 32,000, of bfloat16 rows of 240 157 and 183 where
-  // they take 128 and 139 at 262,144.  Rows that go to several experts would be
+  // takes 16.6 and 20.8 us where two take 15.5 and 16.0 at 2,048 rows, 73 and 91
+  // where they take 90 and 97 at 32,000; with 320 of bfloat16 rows of 240 161 where
+  // they take 129 at 262,144.  Rows that go to several experts would be
   // coded once for each.
   // Few rows in all, short ones: every workgroup codes them again, one row in
   // each wavefront, which costs less than a launch (one row of 1,600 to 240

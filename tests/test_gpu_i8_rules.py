@@ -1,6 +1,8 @@
-"""Layers of up to 256 channels where one kernel gives way to two: short rows past
-32,768, and float64 rows of more than 1,024 elements up to 24,000.  The result
-is the same on both sides: the sums are exact, and the rest is one rounding."""
+"""The sizes at which a layer's kernels change.  Layers of up to 256 channels go
+from one kernel to two: short rows past 32,768, and float64 rows of more than
+1,024 elements below 24,000.  Experts with few rows each go from tiles of 16
+rows to larger ones.  The result is the same on both sides: the sums are exact,
+and the rest is one rounding."""
 import numpy as np
 import pytest
 
@@ -44,3 +46,27 @@ def test_short_rows(t, k, experts):
 @pytest.mark.parametrize("k", [1025, 1601, 2048])
 def test_long_rows_of_64_bits(k, experts):
     _both_sides("f64", k, 24, 23999, 24000, experts)
+
+
+@pytest.mark.parametrize("E,n,k,sizes", [(3, 300, 520, (64, 65)), (16, 300, 520, (128, 129)), (40, 240, 1600, (512, 513)),
+                                         (20, 130, 200, (320, 321)), (40, 256, 2050, (512, 513))])
+@pytest.mark.parametrize("topk", [1, 2])
+def test_few_rows_of_experts(E, n, k, sizes, topk):
+    # even experts, and most rows on one of them; dropped choices and experts without any
+    import paper_2107_02103_amd as P
+    rng = np.random.default_rng(E + n)
+    qw, sw, b = _layer(rng, E, n, k)
+    lin = P.Int8Linear(_padded(qw, P.i8_ld(k)), torch.from_numpy(sw).cuda(), k, torch.from_numpy(b).cuda())
+    for m in sizes:
+        ntok = -(-m // topk)
+        for share in (0.0, 0.9):
+            e = rng.integers(-1, E, (ntok, topk))
+            e[rng.random((ntok, topk)) < share] = E // 2
+            off, rows, _ = ox.plan(e, E)
+            r = P.Route(torch.from_numpy(e.astype(np.int32)).cuda(), E)
+            x = torch.from_numpy(rng.standard_normal((ntok, k)).astype(np.float32)).cuda()
+            x[ntok // 2] = float("nan")
+            qx, sx = ox.codes(x.cpu().numpy())
+            tok = np.maximum(rows, 0) // topk
+            want, mag = ox.product(qx[tok], sx[tok], qw, sw, b, _groups(off, ntok * topk, E))
+            _check(lin(x, route=r), want, mag, "f32")
