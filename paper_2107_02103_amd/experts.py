@@ -8,7 +8,7 @@ import torch
 
 from . import binding as B
 
-_lib, _elem_of = B._lib, B.elem_of
+_lib, _elem_of, _MOST = B._lib, B.elem_of, B.INT_MAX
 _raw_stream = torch._C._cuda_getCurrentRawStream   # hipStream_t of a device's current stream
 _current_device = torch._C._cuda_getDevice
 
@@ -18,10 +18,9 @@ def _check(status, where):
         raise B.DpcError(status, where)
 
 
-def _sizes(where, most):
-    """Refuses a call whose largest size is no C int (ctypes would drop its high bits)."""
-    if most > B.INT_MAX:
-        raise B.DpcError(B.DPC_ENOTSUP, where)
+def _too_large(where):
+    """Refuses a call with a size that is no C int (ctypes would drop its high bits)."""
+    raise B.DpcError(B.DPC_ENOTSUP, where)
 
 
 def _rows(x, name, n=None, width=None, dtype=None, device=None):
@@ -50,15 +49,14 @@ def _on(x, device, name):
         raise ValueError(f"{name} is on {x.device}, the others are on cuda:{device}")
 
 
-def _elsewhere(device, stream):
-    """What a call on tensors of `device` has to enter first: that stream, or the
-    device if another is current (the library launches on the current one); None
-    if it can go ahead."""
-    if stream is not None:
-        if stream.device.index != device:
-            raise ValueError(f"stream is on {stream.device}, the tensors are on cuda:{device}")
-        return torch.cuda.stream(stream)               # makes the device current too
-    return None if _current_device() == device else torch.cuda.device(device)
+def _enter(device, stream):
+    """Context for a call on tensors of `device`: the stream it is to run on, or
+    that device where another is current (the library launches on the current one)."""
+    if stream is None:
+        return torch.cuda.device(device)
+    if stream.device.index != device:
+        raise ValueError(f"stream is on {stream.device}, the tensors are on cuda:{device}")
+    return torch.cuda.stream(stream)                   # makes the device current too
 
 
 class Route:
@@ -81,14 +79,14 @@ class Route:
             raise ValueError("expert must be contiguous int32 [tokens, topk] or [tokens]")
         _on(expert, None, "expert")
         self._device = dev = expert.get_device()
-        at = _elsewhere(dev, stream)
-        if at is not None:
-            with at:
+        if stream is not None or _current_device() != dev:
+            with _enter(dev, stream):
                 return Route.__init__(self, expert, nexpert)
         self.ntok, self.topk = expert.shape if expert.dim() == 2 else (expert.shape[0], 1)
         self.nexpert = int(nexpert)
         m, head = self.ntok * self.topk, max(self.nexpert, 0) + 1
-        _sizes("dpc_route_plan", max(m, abs(self.nexpert)))
+        if m > _MOST or abs(self.nexpert) > _MOST:
+            _too_large("dpc_route_plan")
         nb = _lib.dpc_route_workspace_bytes(self.ntok, self.topk, self.nexpert)
         # the three of the plan in one allocation
         buf = expert.new_empty(head + 2 * m)
@@ -113,7 +111,8 @@ class Route:
         r.offsets, r.rows, r.pos = offsets, rows, pos
         r.ntok, r.topk = pos.shape
         r.nexpert = len(offsets) - 1
-        _sizes("dpc_route_plan", max(r.ntok, r.topk, r.nexpert))
+        if r.ntok > _MOST or r.topk > _MOST or r.nexpert > _MOST:
+            _too_large("dpc_route_plan")
         return r
 
     def _weight(self, weight, x):
@@ -129,13 +128,13 @@ class Route:
     def gather(self, x, weight=None, out=None, stream=None):
         """[tokens * topk, width]: each row the token's row (times its weight),
         zeros in the empty rows.  With weights, the gradient of combine()."""
-        at = _elsewhere(self._device, stream)
-        if at is not None:
-            with at:
+        if stream is not None or _current_device() != self._device:
+            with _enter(self._device, stream):
                 return self.gather(x, weight, out)
         dev, m = self._device, self.ntok * self.topk
         ldx, width = _rows(x, "x", self.ntok, None, None, dev), x.shape[1]
-        _sizes("dpc_route_gather", width)
+        if width > _MOST:
+            _too_large("dpc_route_gather")
         if out is None:
             out, ldy = x.new_empty((m, width)), width or 1
         else:
@@ -148,13 +147,13 @@ class Route:
     def combine(self, x, weight=None, out=None, stream=None):
         """[tokens, width]: the sum of each token's rows (times their weights);
         without weights, the gradient of gather()."""
-        at = _elsewhere(self._device, stream)
-        if at is not None:
-            with at:
+        if stream is not None or _current_device() != self._device:
+            with _enter(self._device, stream):
                 return self.combine(x, weight, out)
         dev = self._device
         ldx, width = _rows(x, "rows", self.ntok * self.topk, None, None, dev), x.shape[1]
-        _sizes("dpc_route_combine", width)
+        if width > _MOST:
+            _too_large("dpc_route_combine")
         if out is None:
             out, ldy = x.new_empty((self.ntok, width)), width or 1
         else:
@@ -167,13 +166,13 @@ class Route:
     def combine_backward(self, x, dy, weight=None, need_rows=True, stream=None):
         """Gradient of combine(x, weight) from dE/dy: (dE/dx, dE/dweight); the
         second is None without weights, the first with need_rows=False."""
-        at = _elsewhere(self._device, stream)
-        if at is not None:
-            with at:
+        if stream is not None or _current_device() != self._device:
+            with _enter(self._device, stream):
                 return self.combine_backward(x, dy, weight, need_rows)
         dev, m = self._device, self.ntok * self.topk
         ldx, width = _rows(x, "rows", m, None, None, dev), x.shape[1]
-        _sizes("dpc_route_combine_bwd", width)
+        if width > _MOST:
+            _too_large("dpc_route_combine_bwd")
         lddy = _rows(dy, "dy", self.ntok, width, x.dtype, dev)
         w = self._weight(weight, x)
         if weight is None and not need_rows:
@@ -204,7 +203,8 @@ class Int8Linear:
         self._device = codes.get_device()
         _on(codes, None, "codes")
         self.experts, self.outer = shape[:2]
-        _sizes("dpc_linear_i8", max(self.inner, self.experts, self.outer))
+        if self.inner > _MOST or self.experts > _MOST or self.outer > _MOST:
+            _too_large("dpc_linear_i8")
         for name, t in (("scales", scales), ("bias", bias)):
             if t is None:
                 continue
@@ -221,12 +221,12 @@ class Int8Linear:
         if w.dim() != 3:
             raise ValueError("weight must be [experts, outer, inner] or [outer, inner]")
         _on(w, None, "weight")
-        at = _elsewhere(w.get_device(), stream)
-        if at is not None:
-            with at:
+        if stream is not None or _current_device() != w.get_device():
+            with _enter(w.get_device(), stream):
                 return cls.from_weight(weight, bias)
         g, n, k = w.shape
-        _sizes("dpc_quant_rows", max(g * n, k))
+        if g * n > _MOST or k > _MOST:
+            _too_large("dpc_quant_rows")
         w = w.contiguous()
         codes = torch.empty((g, n, B.i8_ld(k)), dtype=torch.int8, device=w.device)
         scales = torch.empty((g, n), dtype=torch.float32, device=w.device)
@@ -241,14 +241,14 @@ class Int8Linear:
         tokens and y its rows (each from its expert's layer); with offsets
         (int32 [experts + 1]), the rows of x are sorted by expert already.
         dtype: type of y (default: that of x)."""
-        at = _elsewhere(self._device, stream)
-        if at is not None:
-            with at:
+        if stream is not None or _current_device() != self._device:
+            with _enter(self._device, stream):
                 return self(x, route, offsets, dtype, out)
         dev = self._device
         ldx = _rows(x, "x", None if route is None else route.ntok, self.inner, None, dev)
         ntok, topk, rows = x.shape[0], 1, None
-        _sizes("dpc_linear_i8", ntok)
+        if ntok > _MOST:
+            _too_large("dpc_linear_i8")
         if route is not None:
             if offsets is not None:
                 raise ValueError("give a route or offsets, not both")
