@@ -16,6 +16,7 @@
 
 #include "dpc.h"
 #include "dpc_elem.h"
+#include "dpc_i8_tiles.h"
 #include "dpc_internal.h"
 
 namespace {
@@ -284,11 +285,10 @@ __device__ __forceinline__ int count_tiles(const Product& p, int size) {
 
 // Tiles of `size` rows that find_tile can be asked for.
 inline int64_t most_tiles(const Product& p, int size) {
-  if (!p.offsets) return ((int64_t)p.m + size - 1) / size;
-  // every group and the empty rows may end in a tile of their own
-  const int64_t t = (int64_t)p.m / size + p.ngroup + 1;
-  return t < p.m ? t : p.m;
+  return i8_most_tiles(p.m, p.ngroup, p.offsets != nullptr, size);
 }
+
+inline bool few_rows(const Product& p) { return i8_few_rows(p.m, p.n, p.ngroup, p.offsets != nullptr); }
 
 // token of row r, or -1
 __device__ __forceinline__ int token_of(const Product& p, int r) {
@@ -435,24 +435,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_product_kernel(Product p, 
     }
     y[(int64_t)r * ldy + c] = out;
   }
-}
-
-// Whether few enough rows share an expert's weights for tiles of 16 rows: at most
-// 16 for one layer; for experts, whose rows the host does not know one by one, by
-// the rows in all and their average.  Device times, us, few rows and the kernels
-// that take over, even choice and (in brackets) a share of 1 / e^2 for expert e:
-//   bfloat16, 4,096 x 4,096      64 experts, 4 rows each 209 211 (78 78), 8 223 217 (144 143), 16 277 223
-//                                (209 154), 64 552 317 (521 316); 256 experts, 8 rows 799 837 (371 275);
-//                                3 experts, 48 rows in all 24.8 26.5, 64 24.5 26.6, 128 35.6 26.9
-//   bfloat16, 1,024 x 1,024      256 experts, 4 rows 53 68 (26 21), 8 60 75 (36 28), 16 73 78 (53 42)
-//   float32, 1,600 to 240        64 experts, 8 rows 14.2 16.9 (12.0 16.0), 16 19.5 17.3 (17.1 16.2), 64 35.9 20.6;
-//                                256 experts, 2 rows 25.7 22.7, 8 32.7 25.1 (24.4 18.7), 16 38 26 (31 20)
-// A busy expert's W is read again for each of its 16-row tiles: with few rows on
-// average and most of them on one of many experts that still costs up to a half.
-inline bool few_rows(const Product& p) {
-  if (!p.offsets) return p.m <= 16;
-  if (p.n <= 256) return p.m <= 512 && p.m <= 16 * p.ngroup;
-  return p.m <= 64 || p.m <= 8 * p.ngroup;
 }
 
 template <typename TX, typename TY>
@@ -694,32 +676,15 @@ void launch_tiled(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
                      y, ldy);
 }
 
-// Time of the tiled product: a fixed part, for each step of K the larger of one
-// tile's time alone and the time of the tiles of a CU one after the other, and
-// each tile's start and stores.
-// Measured on 256 CUs (us, bf16 results; 256x256, 128x128, 128x64, 64x64 tiles):
-//   4096 x 4096 x 4096   73.8  84.5 103.4 121.6     1024 x 8192 x 4096  53.0 39.5 52.8 53.6
-//   2048 x 2048 x 2048   29.2  15.8  14.0  16.9     32000 x 240 x 1600  27.9 23.5 25.9 27.6
-//   512 x 4096 x 4096    47.4  22.7  20.1  16.8     16000 x 240 x 1600  25.6 14.7 13.7 15.0
-//   256 x 4096 x 4096    46.6  20.8  14.1  11.1     4000 x 240 x 1600   24.7 12.1  8.5  6.9
-//   8192 x 2048 x 512    17.6  20.2  20.6  23.3     32000 x 512 x 512   17.8 22.3 21.2 24.1
-//   262144 x 1024 x 256   205   245   249   291     131072 x 1600 x 240  163  182  183  215
-double tiled_cost(const Product& p, int bm, int bn, double fixed, double alone, double each, double stores) {
-  const int64_t tiles = most_tiles(p, bm) * ((p.n + bn - 1) / bn);
-  if (tiles >= 1 << 22) fixed += 1e30 / bm;  // more threads than a launch has: the largest tile, if any
-  const double turns = (double)((tiles + 255) / 256), cu = each * turns;
-  return fixed + p.ld / 128 * (alone > cu ? alone : cu) + stores * turns;
-}
-
 template <typename TY>
 void launch_product(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
   if (few_rows(p)) return launch_few(s, p, p.qx, 0, y, ldy);
-  const double big = tiled_cost(p, 256, 256, 8.0, 1.35, 1.9, 4.0), mid = tiled_cost(p, 128, 128, 5.0, 0.7, 0.64, 1.4),
-               low = tiled_cost(p, 128, 64, 4.0, 0.5, 0.35, 0.95), small = tiled_cost(p, 64, 64, 3.3, 0.25, 0.22, 0.5);
-  if (big <= mid && big <= low && big <= small) return launch_tiled<TY, 256, 256, 2, 4>(s, p, y, ldy);
-  if (mid <= low && mid <= small) return launch_tiled<TY, 128, 128, 2, 2>(s, p, y, ldy);
-  if (low <= small) return launch_tiled<TY, 128, 64, 2, 2>(s, p, y, ldy);
-  return launch_tiled<TY, 64, 64, 2, 2>(s, p, y, ldy);
+  switch (i8_tile(p.m, p.n, p.ld, p.ngroup, p.offsets != nullptr)) {
+    case 0: return launch_tiled<TY, 256, 256, 2, 4>(s, p, y, ldy);
+    case 1: return launch_tiled<TY, 128, 128, 2, 2>(s, p, y, ldy);
+    case 2: return launch_tiled<TY, 128, 64, 2, 2>(s, p, y, ldy);
+    default: return launch_tiled<TY, 64, 64, 2, 2>(s, p, y, ldy);
+  }
 }
 
 int product(hipStream_t s, dpc_elem elem_y, const Product& p, void* y, int64_t ldy) {
@@ -763,7 +728,7 @@ __device__ __forceinline__ void put_row(TY* y, int c, int n, const v4i (&acc)[2]
 // leaves L2 to W (1.90 -> 1.87 ms).  Tried without gain: 16 wavefronts (2.7 ms,
 // spills), three workgroups (3.2 ms, spills), W asked for before the codes are
 // done, swizzled lanes for to_rows (its bank conflicts cost nothing).
-constexpr int kCodedRows = 32, kCodedLd = 2048;
+constexpr int kCodedRows = 32, kCodedLd = kI8OneKernelLd;
 
 template <typename TX, int TURNS>
 __global__ __launch_bounds__(512, 4) void coded_product_kernel(Product p, dpc_elem elem_y, const TX* __restrict__ x,
@@ -912,26 +877,6 @@ __global__ __launch_bounds__(512, 4) void coded_product_kernel(Product p, dpc_el
   }
 }
 
-// Whether the rows of the layer are short enough to be held (a chunk at least, and
-// the codes of 32 rows twice in LDS), and one kernel faster than two.  Device
-// times, us, 240 channels, one kernel and two:
-//   float32, 1,600 columns     512 rows 13.4 13.6, 2,048 14.1 15.2, 8,192 17.6 25.3, 262,144 468 616
-//   bfloat16, 1,600 columns    256 rows 13.7 12.9, 2,048 14.3 15.2, 8,192 16.0 23.0, 262,144 337 444
-//   float64, 1,024 columns     512 rows 11.5 11.8, 2,048 12.9 13.3, 8,192 20.1 26.1, 262,144 512 675
-//   float64, 1,600 columns     512 rows 20.2 13.7, 8,192 35.0 35.2, 16,000 61.1 58.1, 24,000 90.0 91.5,
-//                              32,000 116 122, 524,288 1,771 1,855 (27 registers of its kernel spill)
-//   bfloat16, 240 columns      512 rows 6.8 7.5, 8,192 7.7 9.4, 32,000 18.9 20.6, 50,000 33.0 29.7, 262,144 131 103
-//   float32, 128 columns       512 rows 5.6 6.6, 8,192 6.9 8.5, 32,000 17.6 18.8, 50,000 30.8 26.7, 262,144 126 114
-//   float32, 129 columns       512 rows 6.5 7.2, 8,192 7.9 11.1, 32,000 21.5 26.4, 50,000 38.3 40.0, 262,144 170 192
-// Up to 32 chunks leave half of a wavefront without one while it codes.
-template <typename TX>
-bool coded_fits(const Product& p) {
-  const int chunks = p.ld / Chunk<TX>::kElems;
-  if (p.k < Chunk<TX>::kElems || p.ld > kCodedLd) return false;
-  if (chunks <= 32) return p.m <= 32768;
-  return chunks <= 64 * 8 || p.m >= 24000;
-}
-
 template <typename TX, int TURNS = 1>
 void launch_coded(hipStream_t s, const Product& p, dpc_elem elem_y, const TX* x, int64_t ldx, void* y, int64_t ldy) {
   constexpr int kTurn = 64 * Chunk<TX>::kElems;
@@ -957,7 +902,7 @@ void few_by_type(hipStream_t s, const Product& p, dpc_elem elem_y, const TX* x, 
 // The layer in one kernel, if it is one for that: true and its status.
 bool coded_product(hipStream_t s, dpc_elem elem_x, dpc_elem elem_y, const Product& p, const void* x, int64_t ldx, void* y,
                    int64_t ldy, int* status) {
-  // Up to 256 channels, which a workgroup makes in one turn (coded_fits has both
+  // Up to 256 channels, which a workgroup makes in one turn (i8_one_kernel has both
   // sides' times).  With 320 and 512 channels of float32 rows of 1,600 this kernel
   // takes 16.6 and 20.8 us where two take 15.5 and 16.0 at 2,048 rows, 73 and 91
   // where they take 90 and 97 at 32,000; with 320 of bfloat16 rows of 240 161 where
@@ -974,7 +919,8 @@ bool coded_product(hipStream_t s, dpc_elem elem_x, dpc_elem elem_y, const Produc
     if (few) {
       few_by_type(s, p, elem_y, px, ldx, y, ldy);
     } else {
-      if (!coded_fits<std::remove_const_t<std::remove_pointer_t<decltype(px)>>>(p)) return false;
+      if (!i8_one_kernel(p.m, p.k, p.ld, Chunk<std::remove_const_t<std::remove_pointer_t<decltype(px)>>>::kElems))
+        return false;
       launch_coded(s, p, elem_y, px, ldx, y, ldy);
     }
     *status = dpc_internal_launch_status();

@@ -36,20 +36,21 @@ def _both_sides(t, k, n, few, many, experts):
         assert torch.equal(torch.nan_to_num(got[many][-few:], nan=1.25), torch.nan_to_num(got[few], nan=1.25))
 
 
-@pytest.mark.parametrize("experts", [1, 3])
-@pytest.mark.parametrize("t,k", [("bf16", 240), ("f16", 7 * 8 + 3), ("bf16", 256), ("f32", 128), ("f32", 5)])
-def test_short_rows(t, k, experts):
-    _both_sides(t, k, 40, 32768, 32769, experts)
+# type, columns, rows on both sides
+ONE_KERNEL = ([(t, k, 32768, 32769) for t, k in (("bf16", 240), ("f16", 59), ("bf16", 256), ("f32", 128), ("f32", 5))] +
+              [("f64", k, 23999, 24000) for k in (1025, 1601, 2048)])
+# experts, channels, columns, rows on both sides
+FEW_ROWS = [(3, 300, 520, (64, 65)), (16, 300, 520, (128, 129)), (40, 240, 1600, (512, 513)), (20, 130, 200, (320, 321)),
+            (40, 256, 2050, (512, 513))]
 
 
 @pytest.mark.parametrize("experts", [1, 3])
-@pytest.mark.parametrize("k", [1025, 1601, 2048])
-def test_long_rows_of_64_bits(k, experts):
-    _both_sides("f64", k, 24, 23999, 24000, experts)
+@pytest.mark.parametrize("t,k,few,many", ONE_KERNEL)
+def test_one_kernel_or_two(t, k, few, many, experts):
+    _both_sides(t, k, 40 if t != "f64" else 24, few, many, experts)
 
 
-@pytest.mark.parametrize("E,n,k,sizes", [(3, 300, 520, (64, 65)), (16, 300, 520, (128, 129)), (40, 240, 1600, (512, 513)),
-                                         (20, 130, 200, (320, 321)), (40, 256, 2050, (512, 513))])
+@pytest.mark.parametrize("E,n,k,sizes", FEW_ROWS)
 @pytest.mark.parametrize("topk", [1, 2])
 def test_few_rows_of_experts(E, n, k, sizes, topk):
     # even experts, and most rows on one of them; dropped choices and experts without any
