@@ -10,7 +10,10 @@ free-energy calculations; dE/dw_ij is what such a calculation integrates.
 float64: rows sorted by species, each species' rows through
 dpc_fitting_fwd_bwd.  8 bits: every layer one call for all species, forward
 and for the gradient, whose errors (about 1% of a product) suit searches and
-members of an ensemble rather than dynamics."""
+members of an ensemble rather than dynamics: forces within 1 to 2% of their norm
+where the nets expect descriptors of the size they have (as trained ones do, and
+as the first layer is divided here).  Behind saturated layers they are wrong: with
+random nets on the descriptors as they come the error is as large as the forces."""
 import argparse
 import os
 import sys

@@ -410,7 +410,11 @@ int dpc_route_combine_bwd(void* stream, dpc_elem elem, int ntok, int topk, int w
 /* ---- Layers in 8-bit integers -------------------------------------------
  * y = x W^T + b with x and W held as 8-bit codes: every row of x (an atom) and
  * every row of W (an output channel) has a scale of its own.  A matrix of
- * codes is int8 [rows][DPC_I8_LD(cols)], the columns past `cols` zero.      */
+ * codes is int8 [rows][DPC_I8_LD(cols)], the columns past `cols` zero.
+ * A code is off by up to half a step, 1/254 of its row's largest magnitude: a
+ * product of normally distributed rows is off by about 1% of the norm.  What
+ * follows the layer may need more: behind tanh of large arguments the gradient
+ * lives in the few that are small, which such an error changes altogether.  */
 #define DPC_I8_LD(cols) (((cols) + 127) / 128 * 128)
 #define DPC_MAX_I8_COLS 131071 /* sums of that many products fit 32 bits */
 

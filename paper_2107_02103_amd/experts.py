@@ -1,6 +1,9 @@
 """Convenience objects of the routing and 8-bit calls: they check arguments and
 allocate outputs as torch tensors.  All arithmetic happens in libdpc.
 
+No call is recorded for torch's autograd: the outputs of tensors that require a
+gradient do not.  Gradients are calls of their own, named at each method.
+
 A call with few rows is over in microseconds, so these methods check what they
 are given once and call the library by address, without the checks of the
 binding's functions of the same names."""
@@ -188,6 +191,11 @@ class Route:
 
 class Int8Linear:
     """A layer y = x W^T + b on 8-bit codes, or one layer for each expert.
+
+    Each product is off by about 1% of its norm.  Whether that will do is up to
+    what follows: where tanh is saturated (pre-activations far above 1) forces
+    taken through these layers can be wrong altogether.  A layer of the codes of
+    W^T approximates the gradient in x; it is not the derivative of y.
 
     codes   int8 [experts, outer, i8_ld(inner)] (or [outer, ...] for one layer)
     scales  float32 [experts, outer];  bias float32 [experts, outer] or None"""
