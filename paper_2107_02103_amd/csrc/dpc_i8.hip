@@ -8,7 +8,9 @@
 // Product: y[r][c] = (sum_i qx[t][i] qw[g][c][i]) sx[t] sw[g][c] + bias[g][c].
 // The sum over i is exact in 32-bit integers, so its order is free.  On the
 // matrix cores W's rows are the rows and x's rows the columns of a tile: a
-// lane of the result then holds four consecutive channels of one row of y.
+// lane of a result holds four channels of one row of y.  Which rows of W make
+// a tile is free, so larger tiles are dealt rows that end as runs of 16 bytes
+// of y in a lane (channel_of).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -88,6 +90,9 @@ __device__ __forceinline__ void scale_of(unsigned top, float* scale, float* inve
 // 262,144 float32 rows of 240 118 and 102; a workgroup: 262,144 float64 rows of
 // 1,600 708 and 926, 32,768 float32 rows of 4,096 124 and 135, 32,768 bfloat16
 // rows of 8,192 154 and 161.
+// Rows longer than a workgroup holds (8,192 of float32) are read element by
+// element, twice: 16,384 float32 rows of 16,384 467 us (2.9 TB/s), 16,384 float64
+// rows of 8,192 361 (3.4), 16,384 bfloat16 rows of 32,768 1,007 (1.6).
 template <typename T, int LANES, bool HELD>
 __global__ __launch_bounds__(256) void quant_kernel(int nrows, int ncols, const T* __restrict__ x, int64_t ldx,
                                                     int8_t* __restrict__ q, float* __restrict__ scale) {
@@ -724,7 +729,9 @@ __device__ __forceinline__ void put_row(TY* y, int c, int n, const v4i (&acc)[2]
 //
 // Bound by the read of x: 1,048,576 float32 rows of 1,600 to 240 channels (7.7
 // GB) in 1.83 to 1.87 ms, 1.67 without the products, which two workgroups of a
-// CU do not hide entirely; 32,000 rows in 64 us.  Reading x past the caches
+// CU do not hide entirely; 32,000 rows in 64 us.  float64 rows of 1,025 to 2,048
+// take 16 turns, two rows of which do not fit (128 registers, 27 in scratch memory):
+// 1,048,576 of 1,600 in 3.49 ms (15.4 GB: 4.4 TB/s).  Reading x past the caches
 // leaves L2 to W (1.90 -> 1.87 ms).  Tried without gain: 16 wavefronts (2.7 ms,
 // spills), three workgroups (3.2 ms, spills), W asked for before the codes are
 // done, swizzled lanes for to_rows (its bank conflicts cost nothing).
@@ -909,9 +916,12 @@ bool coded_product(hipStream_t s, dpc_elem elem_x, dpc_elem elem_y, const Produc
   // they take 129 at 262,144.  Rows that go to several experts would be
   // coded once for each.
   // Few rows in all, short ones: every workgroup codes them again, one row in
-  // each wavefront, which costs less than a launch (one row of 1,600 to 240
-  // channels 5.4 us and 7.2 in two kernels, 8 rows 6.2 and 7.6; but 16 rows
-  // 9.2 and 7.9, one row of 4,096 to 4,096 channels 9.7 and 8.0).
+  // each wavefront, which costs less than a launch (device times: one float32 row
+  // of 1,600 to 240 channels 5.6 us and 6.9 in two kernels, 8 rows 6.6 and 7.5; but
+  // 16 rows 9.8 and 7.7, one bfloat16 row of 4,096 to 4,096 channels 9.2 and 9.0, 8
+  // rows 12.9 and 11.0).  Coding float64 rows takes longer than a launch of its own
+  // on the device (one row 7.7 and 6.5, 8 rows 9.2 and 6.8) but not with the
+  // host's part of it (9.6 and 12.3).
   const bool few = p.m <= kFewWaves && p.ld <= 2048;
   if (!few && (p.topk != 1 || p.n > 256 || few_rows(p))) return false;
   (void)hipGetLastError();  // report only what this launch raises

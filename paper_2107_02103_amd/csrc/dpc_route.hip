@@ -16,9 +16,10 @@
 // cut into 16-byte chunks, and the lanes of a wavefront take the chunks of one
 // row, or of several rows if a row has fewer than 33.  The last chunk of a row
 // whose width is no multiple of a chunk overlaps the one before it, so that
-// odd widths run at the same loads.  65,536 tokens of 8 KiB to 4 experts each:
-// gather 522 us (2.7 GB: 5.1 TB/s), combine 460 (2.7 GB: 5.8), gradient 914 (4.8
-// GB: 5.3); a copy of 2 GiB runs at 4.9 TB/s.
+// odd widths run at the same loads.  65,536 tokens of 8 KiB to 4 experts each,
+// 11% of the choices dropped: gather 524 us (2.7 GB by counters: 5.1 TB/s),
+// combine 459 (2.5 GB: 5.4), gradient 917 (4.6 GB: 5.0); a copy of 2 GiB runs at
+// 4.9 TB/s.  float64: 262,144 rows of 1,600 1,268, 1,240 and 1,896 us (5.3, 5.4, 5.3).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
