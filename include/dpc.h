@@ -347,7 +347,7 @@ int dpc_fitting_fwd_bwd(void* stream, void* blas, int nloc, const dpc_fitting_ne
  * nslot = ntok * topk rows are laid out; the first offsets[nexpert] of them
  * are the kept slots sorted by expert (ties by slot), the rest is empty.   */
 
-/* Types of the elements of rows (the routing and 8-bit calls). */
+/* Types of the elements of rows (the routing calls and those behind them). */
 typedef enum { DPC_ELEM_F64 = 0, DPC_ELEM_F32 = 1, DPC_ELEM_F16 = 2, DPC_ELEM_BF16 = 3 } dpc_elem;
 
 #define DPC_MAX_EXPERTS 1024
@@ -467,6 +467,143 @@ int dpc_linear_i8(void* stream, dpc_elem elem_x, dpc_elem elem_y, int ntok, int 
                   int ngroup, const void* x, int64_t ldx, const int* rows, const int* offsets,
                   const int8_t* qw, const float* sw, const float* bias, void* workspace,
                   size_t workspace_bytes, void* y, int64_t ldy);
+
+/* ---- Choice of experts ---------------------------------------------------
+ * From the scores of a token for each expert to the experts that it is sent to
+ * and their weights: the inputs of dpc_route_plan and dpc_route_combine.
+ *   s_e = exp(z_e) / sum exp(z), or 1 / (1 + exp(-z_e));  c_e = s_e + bias_e
+ * An expert with z_e = -infinity is closed: its s_e is 0, it is never chosen and
+ * does not count in its group.  The experts stand in `groups` groups of equal
+ * size; the value of a group is the sum of its `best` (1 or 2) largest c, and the
+ * `keep` groups of largest value stay (a group with no open expert never does).
+ * Of these groups' open experts the topk of largest c are chosen, the largest
+ * first.  Ties go to the lower group and the lower expert.  A bias of -infinity
+ * closes its expert for all tokens (its s_e keeps its share).  The weights are
+ *   w_j = scale * s_j,  or (renorm)  scale * s_j / sum_j s_j   (0 if the sum is 0)
+ * s, c, groups' values and sums are float64, whatever the type of z, rounded
+ * once to the weights' type: equal choices on every card and in every order.
+ * Slots without an open expert get expert -1 (which dpc_route_plan drops) and
+ * weight 0.  A token with a NaN among its z or c (or, in a softmax, z = +infinity)
+ * gets the experts 0 .. topk - 1 and weights NaN.                            */
+typedef enum { DPC_SCORE_SOFTMAX = 0, DPC_SCORE_SIGMOID = 1 } dpc_score;
+typedef struct {
+  int nexpert, topk;
+  int score;               /* a dpc_score */
+  int groups, keep, best;  /* 1, 1, 1: no groups */
+  int renorm;              /* not 0: weights of a token sum to scale */
+  double scale;
+} dpc_gate_spec;
+
+#define DPC_MAX_GATE_GROUPS 64
+
+/*   logits  device [ntok] rows of nexpert elements, ldl elements apart
+ *   bias    device float32 [nexpert] or NULL
+ *   expert  device out int32 [ntok][topk]
+ *   weight  device out [ntok][topk], float64 for DPC_ELEM_F64, else float32
+ * Requires nexpert <= DPC_MAX_EXPERTS, topk <= DPC_MAX_TOPK, groups <=
+ * DPC_MAX_GATE_GROUPS, ntok * topk <= 2^30 (DPC_ENOTSUP above); groups divides
+ * nexpert, keep <= groups, topk <= keep * nexpert / groups, finite scale.
+ * `spec` is host memory, read during the call.                               */
+int dpc_gate(void* stream, dpc_elem elem, const dpc_gate_spec* spec, int ntok, const void* logits,
+             int64_t ldl, const float* bias, int* expert, void* weight);
+
+/* Gradient of the weights in the logits, from dE/dweight at the experts that
+ * were chosen (the choice itself has none, nor has the bias):
+ *   S = sum_j s_j,  ds_j = scale dw_j  or (renorm)  scale / S (dw_j - sum_i dw_i s_i / S)
+ *   softmax  dz_e = s_e (ds_e - sum_j ds_j s_j),   sigmoid  dz_e = ds_e s_e (1 - s_e)
+ * with ds_e summed over the slots that hold e; 0 for closed experts, and
+ * everywhere where S is 0.  Slots whose expert is outside [0, nexpert), and what
+ * dweight holds there, do not count.  Arithmetic is float32 (float64 for
+ * DPC_ELEM_F64), rounded once; sums have a fixed order.
+ *   dlogits  device out [ntok] rows, lddl elements apart, of logits' type
+ * groups, keep and best are checked and not used.  Other arguments as above. */
+int dpc_gate_bwd(void* stream, dpc_elem elem, const dpc_gate_spec* spec, int ntok, const void* logits,
+                 int64_t ldl, const int* expert, const void* dweight, void* dlogits, int64_t lddl);
+
+/* ---- Vectors of ids ------------------------------------------------------
+ * y[t] = scale * table[ids[t]]; zeros where ids[t] is outside [0, nid) (atoms
+ * that pad a batch).  The product is rounded once from float64 (DPC_ELEM_F64) or
+ * float32, scale rounded to that type before.
+ *   ids    device int32 [ntok]
+ *   table  device [nid] rows of `width` elements, ldt elements apart
+ *   y      device out [ntok] rows, ldy elements apart
+ * Rows need the alignment of their elements alone.  Requires 1 <= nid <= 2^30,
+ * ntok <= 2^30, 1 <= width <= 2^31 - 128 (DPC_ENOTSUP above).                */
+int dpc_embed(void* stream, dpc_elem elem, int ntok, int nid, int width, const int* ids,
+              const void* table, int64_t ldt, double scale, void* y, int64_t ldy);
+
+/* Gradient of dpc_embed in its table: tokens are sorted by id, then
+ *   dtable[v] = scale * sum over t with ids[t] = v of dy[t]
+ * (zeros for an id without tokens).  Runs of a few rows are summed in float32
+ * (float64 for DPC_ELEM_F64), longer ones joined in float64, in an order that
+ * depends on the sizes alone; rounded once.
+ *   dy       device [ntok] rows of `width` elements of type `elem`
+ *   dtable   device out [nid] rows of type elem_d: elem or DPC_ELEM_F32
+ *   workspace  device, 16-byte aligned, >= dpc_embed_bwd_workspace_bytes()
+ *            (0 for bad sizes); two calls that may run at once need one each
+ * Other arguments as dpc_embed.                                              */
+size_t dpc_embed_bwd_workspace_bytes(dpc_elem elem, int ntok, int nid, int width);
+int dpc_embed_bwd(void* stream, dpc_elem elem, dpc_elem elem_d, int ntok, int nid, int width, const int* ids,
+                  const void* dy, int64_t lddy, double scale, void* workspace, size_t workspace_bytes,
+                  void* dtable, int64_t lddt);
+
+/* ---- Layers in microscaled 4-bit floating point --------------------------
+ * As the layers in 8-bit integers, with x and W as 4-bit floating-point codes
+ * (E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) that share a power of two in
+ * blocks of 32 along a row.  Rows are padded with zeros to DPC_MX4_LD columns:
+ *   codes   uint8 [rows][DPC_MX4_LD(cols) / 2]: two columns in a byte, the even
+ *           one in the low half
+ *   scales  uint8 [DPC_MX4_LD(cols) / 256][rows][8]: byte E of a block stands for
+ *           2^(E - 127), 255 for NaN
+ * A code is off by up to a sixth of its block's largest magnitude where that is
+ * large and a quarter of itself elsewhere: a product of normally distributed rows
+ * is off by 13 to 17% of the norm.  That is for searches and for weights trained
+ * with it; forces of nets that were not are wrong.                           */
+#define DPC_MX4_LD(cols) (((cols) + 255) / 256 * 256)
+#define DPC_MAX_MX4_COLS (1 << 20)
+
+/* Codes of rows.  With x rounded to float32 and a the largest magnitude of a
+ * block, E - 125 = floor(log2 a), one more if a is 1.75 times that power of two or
+ * larger (so that a is below 7 scales), and the code is x / 2^(E - 127) to the
+ * nearest code (ties to the even one, 6 at most).  A block with a < 2^-100 gets
+ * E = 0 and codes of 0, one with an infinity or a NaN E = 255 and codes of 0.
+ *   x      device [ngroup * nrows] rows of `ncols` elements, ldx elements apart
+ *   q      device out codes [ngroup][nrows], 16-byte aligned
+ *   scale  device out scales, one array [.][nrows][8] for each group, 8-byte aligned
+ * Requires 1 <= ncols <= DPC_MAX_MX4_COLS, ngroup * nrows <= 2^30 (DPC_ENOTSUP
+ * above).                                                                    */
+int dpc_quant_mx4(void* stream, dpc_elem elem, int ngroup, int nrows, int ncols, const void* x, int64_t ldx,
+                  uint8_t* q, uint8_t* scale);
+
+/* The values that codes stand for, rounded to `elem` (float32, float64 and
+ * bfloat16 hold nearly all of them).  y: device out [ngroup * nrows] rows.   */
+int dpc_values_mx4(void* stream, dpc_elem elem, int ngroup, int nrows, int ncols, const uint8_t* q,
+                   const uint8_t* scale, void* y, int64_t ldy);
+
+/* Product of codes, for one layer or for the layer of each row's expert:
+ *   y[r][c] = sum_i xq[t][i] wq[g][c][i] + bias[g][c]
+ * of the values that the codes stand for, summed in float32 on the matrix cores
+ * in a fixed order, the bias added in float32, rounded to the type of y.  Rows,
+ * groups and empty rows as in dpc_matmul_i8.
+ *   qx, sx  device codes and scales of [ntok] rows (one group)
+ *   qw, sw  device codes and scales of [ngroup] groups of n rows
+ *   bias    device float32 [ngroup][n] or NULL
+ * qx and qw 16-byte, sx and sw 8-byte aligned.  Requires 1 <= n <= 2^24, 1 <= k
+ * <= DPC_MAX_MX4_COLS, ngroup <= DPC_MAX_EXPERTS, topk <= DPC_MAX_TOPK and
+ * ntok * topk <= 2^27 (DPC_ENOTSUP above).  Gradients: as in dpc_matmul_i8, the
+ * codes of W^T give an approximation, not the derivative.                    */
+int dpc_matmul_mx4(void* stream, dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup,
+                   const uint8_t* qx, const uint8_t* sx, const int* rows, const int* offsets,
+                   const uint8_t* qw, const uint8_t* sw, const float* bias, void* y, int64_t ldy);
+
+/* dpc_quant_mx4 of x [ntok][k] and dpc_matmul_mx4 in one call, with the same
+ * codes.  The workspace (device, 16-byte aligned) may hold the codes and scales
+ * of x in between.  dpc_linear_mx4_workspace_bytes is 0 for bad sizes.       */
+size_t dpc_linear_mx4_workspace_bytes(int ntok, int k);
+int dpc_linear_mx4(void* stream, dpc_elem elem_x, dpc_elem elem_y, int ntok, int topk, int n, int k,
+                   int ngroup, const void* x, int64_t ldx, const int* rows, const int* offsets,
+                   const uint8_t* qw, const uint8_t* sw, const float* bias, void* workspace,
+                   size_t workspace_bytes, void* y, int64_t ldy);
 
 #ifdef __cplusplus
 }

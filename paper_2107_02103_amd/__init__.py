@@ -15,17 +15,19 @@ _BINDING = ("DPC_F32", "DPC_F32_ACC64", "DPC_F64", "DPC_OK", "DPC_EINVAL", "DPC_
             "DPC_ELEM_F64", "DPC_ELEM_F32", "DPC_ELEM_F16", "DPC_ELEM_BF16", "DPC_MAX_EXPERTS", "DPC_MAX_TOPK",
             "DPC_MAX_I8_COLS", "dpc_route_workspace_bytes", "dpc_route_plan", "dpc_route_gather", "dpc_route_combine",
             "dpc_route_combine_bwd", "dpc_quant_rows", "dpc_matmul_i8", "dpc_linear_i8_workspace_bytes",
-            "dpc_linear_i8", "elem_of", "i8_ld")
+            "dpc_linear_i8", "elem_of", "i8_ld",
+            "DPC_SCORE_SOFTMAX", "DPC_SCORE_SIGMOID", "DPC_MAX_GATE_GROUPS", "DPC_MAX_MX4_COLS", "dpc_gate_spec", "dpc_gate",
+            "dpc_gate_bwd", "dpc_embed", "dpc_embed_bwd_workspace_bytes", "dpc_embed_bwd", "dpc_quant_mx4",
+            "dpc_values_mx4", "dpc_matmul_mx4", "dpc_linear_mx4_workspace_bytes", "dpc_linear_mx4", "mx4_ld")
+_OBJECTS = {"SeATab": "descriptor", "Route": "experts", "Int8Linear": "experts", "Gate": "gate", "Embedding": "gate",
+            "Mx4Rows": "mx4", "Mx4Linear": "mx4"}
 
 
 def __getattr__(name):
     if name in _BINDING:
         from . import binding
         return getattr(binding, name)
-    if name == "SeATab":
-        from .descriptor import SeATab
-        return SeATab
-    if name in ("Route", "Int8Linear"):
-        from . import experts
-        return getattr(experts, name)
+    if name in _OBJECTS:
+        from importlib import import_module
+        return getattr(import_module("." + _OBJECTS[name], __name__), name)
     raise AttributeError(name)

@@ -33,13 +33,17 @@ DPC_MAX_TYPES, DPC_MAX_M1 = 8, 256
 DPC_NLIST_NOALLOC_MAX_ATOMS = 524288
 DPC_ELEM_F64, DPC_ELEM_F32, DPC_ELEM_F16, DPC_ELEM_BF16 = 0, 1, 2, 3
 DPC_MAX_EXPERTS, DPC_MAX_TOPK, DPC_MAX_I8_COLS = 1024, 64, 131071
+DPC_SCORE_SOFTMAX, DPC_SCORE_SIGMOID = 0, 1
+DPC_MAX_GATE_GROUPS, DPC_MAX_MX4_COLS = 64, 1 << 20
 EXPORTED = ("dpc_strerror", "dpc_last_hip_error", "dpc_version", "dpc_table_layout", "dpc_build_table",
             "dpc_se_a_tab_fwd", "dpc_se_a_tab_bwd", "dpc_descriptor_bwd", "dpc_env_mat_a",
             "dpc_nlist_reverse", "dpc_force_a", "dpc_fitting_workspace_bytes", "dpc_fitting_fwd_bwd",
             "dpc_nlist_workspace_bytes", "dpc_nlist_build", "dpc_nlist_build_noalloc",
             "dpc_se_a_tab_bwd_from_dD", "dpc_route_workspace_bytes", "dpc_route_plan", "dpc_route_gather",
             "dpc_route_combine", "dpc_route_combine_bwd", "dpc_quant_rows", "dpc_matmul_i8",
-            "dpc_linear_i8_workspace_bytes", "dpc_linear_i8")
+            "dpc_linear_i8_workspace_bytes", "dpc_linear_i8", "dpc_gate", "dpc_gate_bwd", "dpc_embed",
+            "dpc_embed_bwd_workspace_bytes", "dpc_embed_bwd", "dpc_quant_mx4", "dpc_values_mx4", "dpc_matmul_mx4",
+            "dpc_linear_mx4_workspace_bytes", "dpc_linear_mx4")
 
 
 class dpc_range(C.Structure):
@@ -127,6 +131,34 @@ _lib.dpc_linear_i8_workspace_bytes.restype = _Z
 _lib.dpc_linear_i8_workspace_bytes.argtypes = [_I, _I]
 _lib.dpc_linear_i8.restype = _I
 _lib.dpc_linear_i8.argtypes = [_P, _I, _I, _I, _I, _I, _I, _I, _P, _L, _P, _P, _P, _P, _P, _P, _Z, _P, _L]
+
+
+class dpc_gate_spec(C.Structure):
+    _fields_ = [("nexpert", C.c_int), ("topk", C.c_int), ("score", C.c_int), ("groups", C.c_int), ("keep", C.c_int),
+                ("best", C.c_int), ("renorm", C.c_int), ("scale", C.c_double)]
+
+
+_D = C.c_double
+_lib.dpc_gate.restype = _I
+_lib.dpc_gate.argtypes = [_P, _I, C.POINTER(dpc_gate_spec), _I, _P, _L, _P, _P, _P]
+_lib.dpc_gate_bwd.restype = _I
+_lib.dpc_gate_bwd.argtypes = [_P, _I, C.POINTER(dpc_gate_spec), _I, _P, _L, _P, _P, _P, _L]
+_lib.dpc_embed.restype = _I
+_lib.dpc_embed.argtypes = [_P, _I, _I, _I, _I, _P, _P, _L, _D, _P, _L]
+_lib.dpc_embed_bwd_workspace_bytes.restype = _Z
+_lib.dpc_embed_bwd_workspace_bytes.argtypes = [_I, _I, _I, _I]
+_lib.dpc_embed_bwd.restype = _I
+_lib.dpc_embed_bwd.argtypes = [_P, _I, _I, _I, _I, _I, _P, _P, _L, _D, _P, _Z, _P, _L]
+_lib.dpc_quant_mx4.restype = _I
+_lib.dpc_quant_mx4.argtypes = [_P, _I, _I, _I, _I, _P, _L, _P, _P]
+_lib.dpc_values_mx4.restype = _I
+_lib.dpc_values_mx4.argtypes = [_P, _I, _I, _I, _I, _P, _P, _P, _L]
+_lib.dpc_matmul_mx4.restype = _I
+_lib.dpc_matmul_mx4.argtypes = [_P, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _L]
+_lib.dpc_linear_mx4_workspace_bytes.restype = _Z
+_lib.dpc_linear_mx4_workspace_bytes.argtypes = [_I, _I]
+_lib.dpc_linear_mx4.restype = _I
+_lib.dpc_linear_mx4.argtypes = [_P, _I, _I, _I, _I, _I, _I, _I, _P, _L, _P, _P, _P, _P, _P, _P, _Z, _P, _L]
 
 
 class DpcError(RuntimeError):
@@ -606,6 +638,114 @@ def dpc_linear_i8(stream, elem_x, elem_y, ntok, topk, n, k, ngroup, x, ldx, rows
     _same_device(stream, x=x, rows=rows, offsets=offsets, qw=qw, sw=sw, bias=bias, workspace=workspace, y=y)
     _check(_lib.dpc_linear_i8(_stream(stream), int(elem_x), int(elem_y), int(ntok), int(topk), int(n), int(k),
                               int(ngroup), px, int(ldx), *head, pw, int(workspace_bytes), *tail), "dpc_linear_i8")
+
+
+# ---- choice of experts, vectors of ids, layers in microscaled 4 bits ----
+def dpc_gate(stream, elem, spec, ntok, logits, ldl, bias, expert, weight):
+    """``spec``: a dpc_gate_spec."""
+    _sizes("dpc_gate", ntok)
+    m, dt = int(ntok) * spec.topk, _elem_dtype(elem, "dpc_gate")
+    args = (_rows_ptr(logits, ntok, spec.nexpert, ldl, dt, "logits"), int(ldl),
+            _flat_ptr(bias, spec.nexpert, torch.float32, "bias"), _flat_ptr(expert, m, torch.int32, "expert"),
+            _flat_ptr(weight, m, _wdtype(elem), "weight"))
+    _same_device(stream, logits=logits, bias=bias, expert=expert, weight=weight)
+    _check(_lib.dpc_gate(_stream(stream), int(elem), C.byref(spec), int(ntok), *args), "dpc_gate")
+
+
+def dpc_gate_bwd(stream, elem, spec, ntok, logits, ldl, expert, dweight, dlogits, lddl):
+    _sizes("dpc_gate_bwd", ntok)
+    m, dt = int(ntok) * spec.topk, _elem_dtype(elem, "dpc_gate_bwd")
+    args = (_rows_ptr(logits, ntok, spec.nexpert, ldl, dt, "logits"), int(ldl), _flat_ptr(expert, m, torch.int32, "expert"),
+            _flat_ptr(dweight, m, _wdtype(elem), "dweight"), _rows_ptr(dlogits, ntok, spec.nexpert, lddl, dt, "dlogits"),
+            int(lddl))
+    _same_device(stream, logits=logits, expert=expert, dweight=dweight, dlogits=dlogits)
+    _check(_lib.dpc_gate_bwd(_stream(stream), int(elem), C.byref(spec), int(ntok), *args), "dpc_gate_bwd")
+
+
+def dpc_embed(stream, elem, ntok, nid, width, ids, table, ldt, scale, y, ldy):
+    _sizes("dpc_embed", ntok, nid, width)
+    dt = _elem_dtype(elem, "dpc_embed")
+    args = (_flat_ptr(ids, int(ntok), torch.int32, "ids"), _rows_ptr(table, nid, width, ldt, dt, "table"), int(ldt),
+            float(scale), _rows_ptr(y, ntok, width, ldy, dt, "y"), int(ldy))
+    _same_device(stream, ids=ids, table=table, y=y)
+    _check(_lib.dpc_embed(_stream(stream), int(elem), int(ntok), int(nid), int(width), *args), "dpc_embed")
+
+
+def dpc_embed_bwd_workspace_bytes(elem, ntok, nid, width):
+    if max(ntok, nid, width) > INT_MAX or min(ntok, nid, width) < 0:
+        return 0
+    return int(_lib.dpc_embed_bwd_workspace_bytes(int(elem), int(ntok), int(nid), int(width)))
+
+
+def dpc_embed_bwd(stream, elem, elem_d, ntok, nid, width, ids, dy, lddy, scale, workspace, workspace_bytes, dtable, lddt):
+    _sizes("dpc_embed_bwd", ntok, nid, width)
+    dt, dd = _elem_dtype(elem, "dpc_embed_bwd"), _elem_dtype(elem_d, "dpc_embed_bwd")
+    args = (_flat_ptr(ids, int(ntok), torch.int32, "ids"), _rows_ptr(dy, ntok, width, lddy, dt, "dy"), int(lddy), float(scale),
+            _flat_ptr(workspace, int(workspace_bytes), torch.uint8, "workspace"), int(workspace_bytes),
+            _rows_ptr(dtable, nid, width, lddt, dd, "dtable"), int(lddt))
+    _same_device(stream, ids=ids, dy=dy, workspace=workspace, dtable=dtable)
+    _check(_lib.dpc_embed_bwd(_stream(stream), int(elem), int(elem_d), int(ntok), int(nid), int(width), *args),
+           "dpc_embed_bwd")
+
+
+def mx4_ld(cols):
+    """Columns that a row of 4-bit codes is padded to (DPC_MX4_LD in dpc.h); it has half as many bytes, and 8 scales
+    for every 256."""
+    return (int(cols) + 255) // 256 * 256
+
+
+def _mx4_rows(rows, cols, q, scale, qname, sname):
+    ld = mx4_ld(cols)
+    return (_flat_ptr(q, int(rows) * ld // 2, torch.uint8, qname), _flat_ptr(scale, int(rows) * ld // 32, torch.uint8, sname))
+
+
+def dpc_quant_mx4(stream, elem, ngroup, nrows, ncols, x, ldx, q, scale):
+    _sizes("dpc_quant_mx4", ngroup, nrows, ncols)
+    rows, dt = int(ngroup) * int(nrows), _elem_dtype(elem, "dpc_quant_mx4")
+    args = (_rows_ptr(x, rows, ncols, ldx, dt, "x"), int(ldx)) + _mx4_rows(rows, ncols, q, scale, "q", "scale")
+    _same_device(stream, x=x, q=q, scale=scale)
+    _check(_lib.dpc_quant_mx4(_stream(stream), int(elem), int(ngroup), int(nrows), int(ncols), *args), "dpc_quant_mx4")
+
+
+def dpc_values_mx4(stream, elem, ngroup, nrows, ncols, q, scale, y, ldy):
+    _sizes("dpc_values_mx4", ngroup, nrows, ncols)
+    rows, dt = int(ngroup) * int(nrows), _elem_dtype(elem, "dpc_values_mx4")
+    args = _mx4_rows(rows, ncols, q, scale, "q", "scale") + (_rows_ptr(y, rows, ncols, ldy, dt, "y"), int(ldy))
+    _same_device(stream, q=q, scale=scale, y=y)
+    _check(_lib.dpc_values_mx4(_stream(stream), int(elem), int(ngroup), int(nrows), int(ncols), *args), "dpc_values_mx4")
+
+
+def _mx4_layer_args(elem_y, ntok, topk, n, k, ngroup, rows, offsets, qw, sw, bias, y, ldy, where):
+    _sizes(where, ntok, topk, n, k, ngroup)
+    m = int(ntok) * int(topk)
+    head = (_flat_ptr(rows, m, torch.int32, "rows"), _flat_ptr(offsets, int(ngroup) + 1, torch.int32, "offsets"))
+    head += _mx4_rows(int(ngroup) * int(n), k, qw, sw, "qw", "sw")
+    head += (_flat_ptr(bias, int(ngroup) * int(n), torch.float32, "bias"),)
+    return head, (_rows_ptr(y, m, n, ldy, _elem_dtype(elem_y, where), "y"), int(ldy))
+
+
+def dpc_matmul_mx4(stream, elem_y, ntok, topk, n, k, ngroup, qx, sx, rows, offsets, qw, sw, bias, y, ldy):
+    head, tail = _mx4_layer_args(elem_y, ntok, topk, n, k, ngroup, rows, offsets, qw, sw, bias, y, ldy, "dpc_matmul_mx4")
+    px = _mx4_rows(ntok, k, qx, sx, "qx", "sx")
+    _same_device(stream, qx=qx, sx=sx, rows=rows, offsets=offsets, qw=qw, sw=sw, bias=bias, y=y)
+    _check(_lib.dpc_matmul_mx4(_stream(stream), int(elem_y), int(ntok), int(topk), int(n), int(k), int(ngroup), *px, *head,
+                               *tail), "dpc_matmul_mx4")
+
+
+def dpc_linear_mx4_workspace_bytes(ntok, k):
+    if max(ntok, k) > INT_MAX or min(ntok, k) < 0:
+        return 0
+    return int(_lib.dpc_linear_mx4_workspace_bytes(int(ntok), int(k)))
+
+
+def dpc_linear_mx4(stream, elem_x, elem_y, ntok, topk, n, k, ngroup, x, ldx, rows, offsets, qw, sw, bias, workspace,
+                   workspace_bytes, y, ldy):
+    head, tail = _mx4_layer_args(elem_y, ntok, topk, n, k, ngroup, rows, offsets, qw, sw, bias, y, ldy, "dpc_linear_mx4")
+    px = _rows_ptr(x, ntok, k, ldx, _elem_dtype(elem_x, "dpc_linear_mx4"), "x")
+    pw = _flat_ptr(workspace, int(workspace_bytes), torch.uint8, "workspace")
+    _same_device(stream, x=x, rows=rows, offsets=offsets, qw=qw, sw=sw, bias=bias, workspace=workspace, y=y)
+    _check(_lib.dpc_linear_mx4(_stream(stream), int(elem_x), int(elem_y), int(ntok), int(topk), int(n), int(k), int(ngroup),
+                               px, int(ldx), *head, pw, int(workspace_bytes), *tail), "dpc_linear_mx4")
 
 
 class RocblasHandle:

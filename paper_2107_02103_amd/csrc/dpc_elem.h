@@ -40,6 +40,16 @@ struct Chunk {
   typedef unsigned u4 __attribute__((ext_vector_type(4), aligned(2)));  // of its elements, at least
 };
 
+// weight times an element: a product in the type of sums, rounded to it before it
+// is rounded to the element's type (one fused multiply would round once, and
+// differ from what a caller gets from the two operations)
+template <typename T>
+__device__ __forceinline__ T times(typename ElemAcc<T>::type w, T v) {
+  typename ElemAcc<T>::type p = w * (typename ElemAcc<T>::type)v;
+  if constexpr (sizeof(T) == 2) asm("" : "+v"(p));  // the product is a value of its own
+  return (T)p;
+}
+
 inline size_t elem_size(dpc_elem e) { return e == DPC_ELEM_F64 ? 8 : e == DPC_ELEM_F32 ? 4 : 2; }
 inline bool elem_ok(dpc_elem e) {
   return e == DPC_ELEM_F64 || e == DPC_ELEM_F32 || e == DPC_ELEM_F16 || e == DPC_ELEM_BF16;

@@ -1,0 +1,352 @@
+// Layers in microscaled 4-bit floating point (dpc_quant_mx4, dpc_values_mx4,
+// dpc_matmul_mx4, dpc_linear_mx4).
+//
+// Codes: a block of 32 elements is held by 4 lanes, 8 in each; its scale follows
+// from its own largest magnitude, so that a row is read once, in any order.
+//
+// Product: y[r][c] = sum_i xq[t][i] wq[g][c][i] + bias[g][c] on the matrix cores,
+// which take 128 columns of codes and the scales of their 4 blocks at a time.  A
+// step is 256 columns, 128 bytes of codes and 8 of scales of a row.  Which block
+// stands in which lane of a product is free as long as both sides agree: quarter q
+// of the lanes takes blocks 2 q and 2 q + 1 of the step in its two products, whose
+// scales are neighbouring bytes.  W's rows are the rows and x's rows the columns of
+// a tile: a lane of a result holds four channels of one row of y.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "dpc.h"
+#include "dpc_elem.h"
+#include "dpc_groups.h"
+#include "dpc_internal.h"
+
+namespace {
+
+constexpr int64_t kMaxRows = (int64_t)1 << 30;      // rows of codes
+constexpr int64_t kMaxProduct = (int64_t)1 << 27;   // rows of a product (a launch has under 2^32 threads)
+constexpr int kMaxChannels = 1 << 24;
+constexpr int kBlock = 256;
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+
+// ---------------------------------------------------------------------------
+// codes
+// ---------------------------------------------------------------------------
+// The scale byte of a block whose largest magnitude (as float32) is a, and the
+// scale as a number, 0 where the codes are 0.
+__device__ __forceinline__ unsigned scale_byte(float a, float* scale) {
+  const unsigned bits = __float_as_uint(a);
+  unsigned e = ((bits + (1u << 21)) >> 23) - 2;  // rounded up from 1.75 on
+  const bool finite = bits < 0x7f800000u, live = finite && a >= 0x1p-100f;
+  *scale = live ? __uint_as_float(e << 23) : 0.0f;
+  return live ? e : finite ? 0u : 255u;
+}
+
+// The largest of magnitudes, NaN if one is.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// The same over the 4 lanes of a block.
+__device__ __forceinline__ float block_max(float a) {
+  a = larger(a, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(a), 0xb1, 0xf, 0xf, false)));  // lanes 1 0 3 2
+  return larger(a, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(a), 0x4e, 0xf, 0xf, false)));  // 2 3 0 1
+}
+
+// 8 elements to 8 codes.
+__device__ __forceinline__ unsigned codes_of(const float (&v)[8], float scale) {
+  unsigned q = 0;
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[0], v[1], scale, 0);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[2], v[3], scale, 1);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[4], v[5], scale, 2);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[6], v[7], scale, 3);
+  return scale > 0.0f ? q : 0u;
+}
+
+// 8 elements of a row of `ncols` from column c on, zeros past its end.
+template <typename T>
+__device__ __forceinline__ void take8(const T* px, int c, int ncols, float (&v)[8]) {
+  if (c + 8 <= ncols) {
+    T t[8];
+    __builtin_memcpy(t, px + c, sizeof(t));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i < ncols ? (float)px[c + i] : 0.0f;
+  }
+}
+
+constexpr int kQuantSteps = 4;  // steps of a row that 32 lanes take
+
+// 8 rows to a workgroup, kQuantSteps steps of each.  Rows go on in z: one
+// dimension of a launch has under 2^32 threads.
+constexpr int64_t kWide = 1 << 22;
+dim3 rows_grid(int64_t rows, int ncols) {
+  const int64_t blocks = (rows + kBlock / 32 - 1) / (kBlock / 32), wide = blocks < kWide ? blocks : kWide;
+  const int steps = DPC_MX4_LD(ncols) / 256;
+  return dim3((unsigned)wide, (unsigned)((steps + kQuantSteps - 1) / kQuantSteps), (unsigned)((blocks + wide - 1) / wide));
+}
+__device__ __forceinline__ int64_t row_of_lane() {
+  return (blockIdx.z * (int64_t)gridDim.x + blockIdx.x) * (kBlock / 32) + threadIdx.x / 32;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void quant_kernel(int64_t nrows_all, int nrows, int ncols, const T* __restrict__ x,
+                                                       int64_t ldx, uint8_t* __restrict__ q, uint8_t* __restrict__ scale) {
+  const int lane = threadIdx.x & 31, steps = DPC_MX4_LD(ncols) / 256;
+  const int64_t r = row_of_lane();
+  if (r >= nrows_all) return;
+  const int s0 = blockIdx.y * kQuantSteps;
+  const int64_t group = r / nrows, row = r - group * nrows;
+  const T* px = x + r * ldx;
+  float v[kQuantSteps][8];
+#pragma unroll
+  for (int k = 0; k < kQuantSteps; ++k) take8(px, (s0 + k) * 256 + lane * 8, ncols, v[k]);
+#pragma unroll
+  for (int k = 0; k < kQuantSteps; ++k) {
+    if (s0 + k >= steps) break;
+    float a = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a = larger(a, __builtin_fabsf(v[k][i]));
+    float factor;
+    const unsigned e = scale_byte(block_max(a), &factor);
+    *reinterpret_cast<unsigned*>(q + (r * steps + s0 + k) * 128 + lane * 4) = codes_of(v[k], factor);
+    if ((lane & 3) == 0) scale[((group * steps + s0 + k) * nrows + row) * 8 + (lane >> 2)] = (uint8_t)e;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void values_kernel(int64_t nrows_all, int nrows, int ncols, const uint8_t* __restrict__ q,
+                                                        const uint8_t* __restrict__ scale, T* __restrict__ y, int64_t ldy) {
+  const int lane = threadIdx.x & 31, steps = DPC_MX4_LD(ncols) / 256;
+  const int64_t r = row_of_lane();
+  if (r >= nrows_all) return;
+  const int s0 = blockIdx.y * kQuantSteps;
+  const int64_t group = r / nrows, row = r - group * nrows;
+  unsigned code[kQuantSteps], e[kQuantSteps];
+#pragma unroll
+  for (int k = 0; k < kQuantSteps; ++k) {
+    const int s = min(s0 + k, steps - 1);
+    code[k] = *reinterpret_cast<const unsigned*>(q + (r * steps + s) * 128 + lane * 4);
+    e[k] = scale[((group * steps + s) * nrows + row) * 8 + (lane >> 2)];
+  }
+#pragma unroll
+  for (int k = 0; k < kQuantSteps; ++k) {
+    const int c = (s0 + k) * 256 + lane * 8;
+    if (c >= ncols) break;
+    // 2^(E - 127): in float32 a number below the least normal one for E = 0
+    typename ElemAcc<T>::type f;
+    if constexpr (sizeof(T) == 8) f = __longlong_as_double(e[k] == 255 ? 0x7ff8000000000000ll : (long long)(e[k] + 896) << 52);
+    else f = __uint_as_float(e[k] == 0 ? 0x00400000u : e[k] == 255 ? 0x7fc00000u : e[k] << 23);
+    T out[8];
+#define DPC_PAIR(p)                                                                      \
+  {                                                                                      \
+    const v2f two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[k], 1.0f, p);          \
+    out[2 * p] = (T)(two[0] * f);                                                        \
+    out[2 * p + 1] = (T)(two[1] * f);                                                    \
+  }
+    DPC_PAIR(0) DPC_PAIR(1) DPC_PAIR(2) DPC_PAIR(3)
+#undef DPC_PAIR
+    T* py = y + r * ldy + c;
+    if (c + 8 <= ncols) {
+      __builtin_memcpy(py, out, sizeof(out));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c + i < ncols) py[i] = out[i];
+    }
+  }
+}
+
+// Calls f with a value of the element type.
+template <typename F>
+int by_elem(dpc_elem elem, F f) {
+  (void)hipGetLastError();  // report only what this launch raises
+  switch (elem) {
+    case DPC_ELEM_F64: f(double{}); break;
+    case DPC_ELEM_F32: f(float{}); break;
+    case DPC_ELEM_F16: f(_Float16{}); break;
+    default: f(__bf16{}); break;
+  }
+  return dpc_internal_launch_status();
+}
+
+int quant(hipStream_t s, dpc_elem elem, int ngroup, int nrows, int ncols, const void* x, int64_t ldx, uint8_t* q,
+          uint8_t* scale) {
+  const int64_t rows = (int64_t)ngroup * nrows;
+  return by_elem(elem, [&](auto t) {
+    typedef decltype(t) T;
+    hipLaunchKernelGGL(quant_kernel<T>, rows_grid(rows, ncols), dim3(kBlock), 0, s, rows, nrows, ncols, (const T*)x, ldx, q,
+                       scale);
+  });
+}
+
+// ---------------------------------------------------------------------------
+// product
+// ---------------------------------------------------------------------------
+struct Product {
+  int ntok, topk, m, n, k, steps, ngroup;
+  const uint8_t* qx;
+  const uint8_t* sx;
+  const int* rows;
+  const int* offsets;
+  const uint8_t* qw;
+  const uint8_t* sw;
+  const float* bias;
+};
+
+// Tiles of `size` rows that find_tile can be asked for.
+inline int64_t most_tiles(const Product& p, int size) {
+  if (!p.offsets) return ((int64_t)p.m + size - 1) / size;
+  const int64_t t = (int64_t)p.m / size + p.ngroup + 1;
+  return t < p.m ? t : p.m;
+}
+
+// One product of 16 rows of W and 16 rows of x, 128 columns: codes a and b of this
+// lane's block, whose scale is byte K of sa and sb.
+template <int K>
+__device__ __forceinline__ v4f mfma4(v4i a, v4i b, v4f c, int sa, int sb) {
+  const v8i a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, b8 = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, K, sa, K, sb);
+}
+
+template <typename TY>
+__device__ __forceinline__ TY result(float sum, float bias) {
+  float f = sum + bias;
+  if constexpr (sizeof(TY) == 2) asm("" : "+v"(f));  // the sum is rounded to float32 before
+  return (TY)f;
+}
+
+// 16 rows times 16 channels of y for each wavefront.
+template <typename TY>
+__global__ __launch_bounds__(256) void product_kernel(Product p, TY* __restrict__ y, int64_t ldy) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Tile t = find_tile(p, 16, blockIdx.y + gridDim.y * blockIdx.z);
+  const int c0 = (blockIdx.x * 4 + wave) * 16;
+  if (t.row0 >= t.end || c0 >= p.n) return;
+  const int group = max(t.group, 0), r = t.row0 + l16;
+  const int tok = t.group < 0 ? -1 : token_of(p, min(r, t.end - 1)), tk = max(tok, 0), ch = min(c0 + l16, p.n - 1);
+  const uint8_t* pw = p.qw + ((int64_t)group * p.n + ch) * p.steps * 128 + quad * 32;
+  const uint8_t* px = p.qx + (int64_t)tk * p.steps * 128 + quad * 32;
+  const uint8_t* psw = p.sw + ((int64_t)group * p.steps * p.n + ch) * 8 + quad * 2;
+  const uint8_t* psx = p.sx + (int64_t)tk * 8 + quad * 2;
+  v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < p.steps; ++s) {
+    const v4i* w = reinterpret_cast<const v4i*>(pw + (int64_t)s * 128);
+    const v4i* x = reinterpret_cast<const v4i*>(px + (int64_t)s * 128);
+    const int sw = *reinterpret_cast<const uint16_t*>(psw + (int64_t)s * p.n * 8);
+    const int sx = *reinterpret_cast<const uint16_t*>(psx + (int64_t)s * p.ntok * 8);
+    acc = mfma4<0>(w[0], x[0], acc, sw, sx);
+    acc = mfma4<1>(w[1], x[1], acc, sw, sx);
+  }
+  if (r >= t.end) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = c0 + quad * 4 + i;
+    if (c >= p.n) break;
+    const float bias = p.bias ? p.bias[(int64_t)group * p.n + c] : 0.0f;
+    y[(int64_t)r * ldy + c] = tok < 0 ? (TY)0 : result<TY>(acc[i], bias);
+  }
+}
+
+int product(hipStream_t s, dpc_elem elem_y, const Product& p, void* y, int64_t ldy) {
+  return by_elem(elem_y, [&](auto t) {
+    typedef decltype(t) TY;
+    const int64_t tiles = most_tiles(p, 16);
+    const unsigned gy = (unsigned)(tiles < 32768 ? tiles : 32768);
+    hipLaunchKernelGGL(product_kernel<TY>, dim3((unsigned)((p.n + 63) / 64), gy, (unsigned)((tiles + gy - 1) / gy)), dim3(256),
+                       0, s, p, (TY*)y, ldy);
+  });
+}
+
+int product_args(dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup) {
+  if (!elem_ok(elem_y) || ntok < 0 || topk < 1 || n < 1 || k < 1 || ngroup < 1) return DPC_EINVAL;
+  if (topk > DPC_MAX_TOPK || k > DPC_MAX_MX4_COLS || ngroup > DPC_MAX_EXPERTS || n > kMaxChannels ||
+      (int64_t)ntok * topk > kMaxProduct)
+    return DPC_ENOTSUP;
+  return DPC_OK;
+}
+
+bool product_ptrs(dpc_elem elem_y, int topk, int n, int ngroup, const int* rows, const int* offsets, const uint8_t* qw,
+                  const uint8_t* sw, const float* bias, const void* y, int64_t ldy) {
+  if ((!rows && topk != 1) || (!offsets && ngroup != 1)) return false;
+  return qw && sw && y && ldy >= n && elem_aligned(qw, 16) && elem_aligned(sw, 8) && elem_aligned(bias, 4) &&
+         elem_aligned(rows, 4) && elem_aligned(offsets, 4) && elem_aligned(y, elem_size(elem_y));
+}
+
+int rows_args(dpc_elem elem, int ngroup, int nrows, int ncols) {
+  if (!elem_ok(elem) || ngroup < 0 || nrows < 0 || ncols < 1) return DPC_EINVAL;
+  if (ncols > DPC_MAX_MX4_COLS || (int64_t)ngroup * nrows > kMaxRows) return DPC_ENOTSUP;
+  return DPC_OK;
+}
+bool rows_ptrs(dpc_elem elem, int ncols, const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scale) {
+  return x && q && scale && ldx >= ncols && elem_aligned(x, elem_size(elem)) && elem_aligned(q, 16) && elem_aligned(scale, 8);
+}
+
+}  // namespace
+
+extern "C" int dpc_quant_mx4(void* stream, dpc_elem elem, int ngroup, int nrows, int ncols, const void* x, int64_t ldx,
+                             uint8_t* q, uint8_t* scale) {
+  const int st = rows_args(elem, ngroup, nrows, ncols);
+  if (st != DPC_OK) return st;
+  if (ngroup == 0 || nrows == 0) return DPC_OK;
+  if (!rows_ptrs(elem, ncols, x, ldx, q, scale)) return DPC_EINVAL;
+  return quant(static_cast<hipStream_t>(stream), elem, ngroup, nrows, ncols, x, ldx, q, scale);
+}
+
+extern "C" int dpc_values_mx4(void* stream, dpc_elem elem, int ngroup, int nrows, int ncols, const uint8_t* q,
+                              const uint8_t* scale, void* y, int64_t ldy) {
+  const int st = rows_args(elem, ngroup, nrows, ncols);
+  if (st != DPC_OK) return st;
+  if (ngroup == 0 || nrows == 0) return DPC_OK;
+  if (!rows_ptrs(elem, ncols, y, ldy, q, scale)) return DPC_EINVAL;
+  const int64_t rows = (int64_t)ngroup * nrows;
+  return by_elem(elem, [&](auto t) {
+    typedef decltype(t) T;
+    hipLaunchKernelGGL(values_kernel<T>, rows_grid(rows, ncols), dim3(kBlock), 0, static_cast<hipStream_t>(stream), rows, nrows,
+                       ncols, q, scale, (T*)y, ldy);
+  });
+}
+
+extern "C" int dpc_matmul_mx4(void* stream, dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup, const uint8_t* qx,
+                              const uint8_t* sx, const int* rows, const int* offsets, const uint8_t* qw, const uint8_t* sw,
+                              const float* bias, void* y, int64_t ldy) {
+  const int st = product_args(elem_y, ntok, topk, n, k, ngroup);
+  if (st != DPC_OK) return st;
+  if (ntok == 0) return DPC_OK;
+  if (!qx || !sx || !elem_aligned(qx, 16) || !elem_aligned(sx, 8) ||
+      !product_ptrs(elem_y, topk, n, ngroup, rows, offsets, qw, sw, bias, y, ldy))
+    return DPC_EINVAL;
+  const Product p{ntok, topk, ntok * topk, n, k, DPC_MX4_LD(k) / 256, ngroup, qx, sx, rows, offsets, qw, sw, bias};
+  return product(static_cast<hipStream_t>(stream), elem_y, p, y, ldy);
+}
+
+extern "C" size_t dpc_linear_mx4_workspace_bytes(int ntok, int k) {
+  if (ntok < 0 || ntok > kMaxRows || k < 1 || k > DPC_MAX_MX4_COLS) return 0;
+  return ((size_t)ntok * (DPC_MX4_LD(k) / 256) * 136 + 255) / 256 * 256 + 256;
+}
+
+extern "C" int dpc_linear_mx4(void* stream, dpc_elem elem_x, dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup,
+                              const void* x, int64_t ldx, const int* rows, const int* offsets, const uint8_t* qw,
+                              const uint8_t* sw, const float* bias, void* workspace, size_t workspace_bytes, void* y,
+                              int64_t ldy) {
+  const int st = product_args(elem_y, ntok, topk, n, k, ngroup);
+  if (st != DPC_OK) return st;
+  if (!elem_ok(elem_x)) return DPC_EINVAL;
+  if (ntok == 0) return DPC_OK;
+  if (!x || ldx < k || !elem_aligned(x, elem_size(elem_x)) || !workspace || !elem_aligned(workspace, 16) ||
+      workspace_bytes < dpc_linear_mx4_workspace_bytes(ntok, k) ||
+      !product_ptrs(elem_y, topk, n, ngroup, rows, offsets, qw, sw, bias, y, ldy))
+    return DPC_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int steps = DPC_MX4_LD(k) / 256;
+  uint8_t* q = static_cast<uint8_t*>(workspace);
+  uint8_t* scale = q + (size_t)ntok * steps * 128;
+  const Product p{ntok, topk, ntok * topk, n, k, steps, ngroup, q, scale, rows, offsets, qw, sw, bias};
+  const int qs = quant(s, elem_x, 1, ntok, k, x, ldx, q, scale);
+  if (qs != DPC_OK) return qs;
+  return product(s, elem_y, p, y, ldy);
+}

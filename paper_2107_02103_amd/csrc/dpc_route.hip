@@ -1,14 +1,6 @@
 // Tokens sorted by expert and back (the routing calls of dpc.h).
 //
-// Plan: a stable counting sort of nslot expert numbers.  With h[e][c] the
-// number of slots of expert e in part c of the slots (parts in order), the
-// row of a slot is
-//   sum_{e' < e, c} h[e'][c] + sum_{c' < c} h[e][c'] + (slots of e before it in c).
-// A part is what one wavefront walks, 64 slots at a time: lanes with the same
-// expert find each other by one ballot per bit of the expert's number, and
-// their rank is the number of such lanes below.  No atomics: the order is the
-// same on every call.  Bound by latency: 3 us for a few slots, 12 to 16 us for
-// 331,776 in three launches of 1,024 slots to a workgroup (with 4,096 31 us).
+// Plan: a stable counting sort of nslot expert numbers (dpc_sort.h).
 //
 // Rows: the gather, the combine and its gradient move each row once and do
 // one or two FMA per element, so they are bound by HBM bandwidth (or by the
@@ -27,6 +19,7 @@
 #include "dpc.h"
 #include "dpc_elem.h"
 #include "dpc_internal.h"
+#include "dpc_sort.h"
 
 namespace {
 
@@ -36,213 +29,22 @@ constexpr int kMaxWidth = INT32_MAX - 127;  // a lane's next element (64 on) and
 // ---------------------------------------------------------------------------
 // plan
 // ---------------------------------------------------------------------------
-// Up to here one workgroup makes the whole plan.  With 64 experts, us: 4,096
-// slots 9.4 so and 13.6 in three launches, 8,192 14.4 and 14.1, 16,384 24.3 and
-// 14.1 (2 experts 6.9, 10.5; 9.5, 10.6; 14.8, 10.9).
-constexpr int kOneBlockSlots = 8192;
-constexpr int kPartSlots = 1024;       // slots of a workgroup beyond that, at least
-constexpr int kMaxBlocks = 1024;
-constexpr int kPlanWaves = 4;          // wavefronts of a workgroup of the three-launch plan
-
-inline int plan_blocks(int64_t nslot) {
-  const int64_t b = (nslot + kPartSlots - 1) / kPartSlots;
-  return (int)(b < kMaxBlocks ? b : kMaxBlocks);
-}
-// slots of a workgroup: every wavefront gets whole groups of 64
-inline int64_t plan_part(int64_t nslot, int blocks) {
-  const int64_t unit = 64 * kPlanWaves;
-  return ((nslot + blocks - 1) / blocks + unit - 1) / unit * unit;
-}
-
-// Walks slots [lo, hi) of one wavefront, 64 at a time in order, calling
-// f(slot, expert, lanes of the same expert) for the lanes with a kept slot.
-template <typename F>
-__device__ __forceinline__ void walk(const int* __restrict__ expert, int64_t lo, int64_t hi, int nexpert, F f) {
-  const int lane = threadIdx.x & 63;
-  const int bits = nexpert > 1 ? 32 - __clz(nexpert - 1) : 0;
-  for (int64_t s0 = lo; s0 < hi; s0 += 64) {
-    const int64_t s = s0 + lane;
-    const int e = s < hi ? expert[s] : -1;
-    const bool kept = (unsigned)e < (unsigned)nexpert;
-    unsigned long long same = __ballot(kept);
-    for (int b = 0; b < bits; ++b) {
-      const unsigned long long set = __ballot((e >> b) & 1);
-      same &= (e >> b) & 1 ? set : ~set;
-    }
-    f(s, s < hi, e, kept, same);
+struct PlanJob {
+  const int* __restrict__ expert;
+  int* __restrict__ offsets;
+  int* __restrict__ rows;
+  int* __restrict__ pos;
+  int nexpert;
+  __device__ __forceinline__ int key(int64_t s) const { return expert[s]; }
+  __device__ __forceinline__ int64_t size(int64_t n) const { return n; }
+  __device__ __forceinline__ void put(int64_t s, int, int row) const {
+    if (row >= 0) rows[row] = (int)s;
+    pos[s] = row;
   }
-}
-
-// Counts of the experts among the slots [lo, hi) of one wavefront, in LDS.
-__device__ __forceinline__ void count(const int* expert, int64_t lo, int64_t hi, int nexpert, int* cnt) {
-  const int lane = threadIdx.x & 63;
-  walk(expert, lo, hi, nexpert, [&](int64_t, bool, int e, bool kept, unsigned long long same) {
-    // the lowest lane of each expert adds for all of them: one lane per address
-    if (kept && (same & ((1ull << lane) - 1)) == 0) cnt[e] += __popcll(same);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  });
-}
-
-// Rows of the slots [lo, hi) of one wavefront; next[e]: its next row of expert e.
-__device__ __forceinline__ void place(const int* expert, int64_t lo, int64_t hi, int nexpert, int* next, int* rows,
-                                      int* pos) {
-  const int lane = threadIdx.x & 63;
-  walk(expert, lo, hi, nexpert, [&](int64_t s, bool in, int e, bool kept, unsigned long long same) {
-    const int before = __popcll(same & ((1ull << lane) - 1));
-    const int first = kept ? next[e] : 0;
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    if (kept) {
-      if (before == 0) next[e] = first + __popcll(same);
-      rows[first + before] = (int)s;
-    }
-    if (in) pos[s] = kept ? first + before : -1;
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  });
-}
-
-// Exclusive prefix sums of v[0 .. n) in LDS by the whole workgroup, total
-// returned; tmp holds one int per wavefront.
-__device__ __forceinline__ int block_scan(int* v, int n, int* tmp) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  int carry = 0;
-  for (int i0 = 0; i0 < n; i0 += blockDim.x) {
-    const int i = i0 + threadIdx.x;
-    const int mine = i < n ? v[i] : 0;
-    int sum = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(sum, d);
-      if (lane >= d) sum += up;
-    }
-    if (lane == 63) tmp[wave] = sum;
-    __syncthreads();
-    int before = carry, all = carry;
-    for (int w = 0; w < waves; ++w) {
-      if (w < wave) before += tmp[w];
-      all += tmp[w];
-    }
-    if (i < n) v[i] = before + sum - mine;
-    carry = all;
-    __syncthreads();
-  }
-  return carry;
-}
-
-// Few slots: one workgroup.  LDS: counts [waves][nexpert], totals [nexpert],
-// one int per wavefront.
-__global__ __launch_bounds__(1024) void plan_one_kernel(int nslot, int nexpert, const int* __restrict__ expert,
-                                                        int* __restrict__ offsets, int* __restrict__ rows,
-                                                        int* __restrict__ pos) {
-  extern __shared__ int plan_lds[];
-  const int waves = blockDim.x >> 6;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int* cnt = plan_lds;
-  int* tot = cnt + waves * nexpert;
-  int* tmp = tot + nexpert;
-  const int part = ((nslot + waves - 1) / waves + 63) & ~63;
-  const int lo = wave * part < nslot ? wave * part : nslot;
-  const int hi = lo + part < nslot ? lo + part : nslot;
-  for (int i = threadIdx.x; i < waves * nexpert; i += blockDim.x) cnt[i] = 0;
-  __syncthreads();
-  count(expert, lo, hi, nexpert, cnt + wave * nexpert);
-  __syncthreads();
-  for (int e = threadIdx.x; e < nexpert; e += blockDim.x) {
-    int run = 0;
-    for (int w = 0; w < waves; ++w) {
-      const int c = cnt[w * nexpert + e];
-      cnt[w * nexpert + e] = run;
-      run += c;
-    }
-    tot[e] = run;
-  }
-  __syncthreads();
-  const int kept = block_scan(tot, nexpert, tmp);
-  for (int e = threadIdx.x; e < nexpert; e += blockDim.x) {
-    const int first = tot[e];
-    offsets[e] = first;
-    for (int w = 0; w < waves; ++w) cnt[w * nexpert + e] += first;
-  }
-  if (threadIdx.x == 0) offsets[nexpert] = kept;
-  for (int r = kept + threadIdx.x; r < nslot; r += blockDim.x) rows[r] = -1;
-  __syncthreads();
-  place(expert, lo, hi, nexpert, cnt + wave * nexpert, rows, pos);
-}
-
-// Many slots, first launch: hist[e][block] = slots of expert e in the block's part.
-__global__ __launch_bounds__(64 * kPlanWaves) void plan_count_kernel(int64_t nslot, int64_t part, int nexpert,
-                                                                     const int* __restrict__ expert,
-                                                                     int* __restrict__ hist) {
-  extern __shared__ int plan_lds[];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int i = threadIdx.x; i < kPlanWaves * nexpert; i += blockDim.x) plan_lds[i] = 0;
-  __syncthreads();
-  const int64_t first = blockIdx.x * part + wave * (part / kPlanWaves);
-  const int64_t lo = first < nslot ? first : nslot;
-  const int64_t hi = lo + part / kPlanWaves < nslot ? lo + part / kPlanWaves : nslot;
-  count(expert, lo, hi, nexpert, plan_lds + wave * nexpert);
-  __syncthreads();
-  for (int e = threadIdx.x; e < nexpert; e += blockDim.x) {
-    int sum = 0;
-    for (int w = 0; w < kPlanWaves; ++w) sum += plan_lds[w * nexpert + e];
-    hist[(int64_t)e * gridDim.x + blockIdx.x] = sum;
-  }
-}
-
-// Second launch, one workgroup per expert: hist[e] to its exclusive prefix
-// sums over the blocks, total[e] to their sum.
-__global__ __launch_bounds__(256) void plan_scan_kernel(int blocks, int* __restrict__ hist, int* __restrict__ total) {
-  __shared__ int v[kMaxBlocks];
-  __shared__ int tmp[4];
-  int* h = hist + (int64_t)blockIdx.x * blocks;
-  for (int i = threadIdx.x; i < blocks; i += blockDim.x) v[i] = h[i];
-  __syncthreads();
-  const int sum = block_scan(v, blocks, tmp);
-  for (int i = threadIdx.x; i < blocks; i += blockDim.x) h[i] = v[i];
-  if (threadIdx.x == 0) total[blockIdx.x] = sum;
-}
-
-// Third launch: rows and positions of the block's part.
-__global__ __launch_bounds__(64 * kPlanWaves) void plan_place_kernel(int64_t nslot, int64_t part, int nexpert,
-                                                                     const int* __restrict__ expert,
-                                                                     const int* __restrict__ hist,
-                                                                     const int* __restrict__ total,
-                                                                     int* __restrict__ offsets, int* __restrict__ rows,
-                                                                     int* __restrict__ pos) {
-  extern __shared__ int plan_lds[];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int* cnt = plan_lds;
-  int* off = cnt + kPlanWaves * nexpert;
-  int* tmp = off + nexpert;
-  for (int i = threadIdx.x; i < kPlanWaves * nexpert; i += blockDim.x) cnt[i] = 0;
-  for (int e = threadIdx.x; e < nexpert; e += blockDim.x) off[e] = total[e];
-  __syncthreads();
-  const int kept = block_scan(off, nexpert, tmp);
-  const int64_t first = blockIdx.x * part + wave * (part / kPlanWaves);
-  const int64_t lo = first < nslot ? first : nslot;
-  const int64_t hi = lo + part / kPlanWaves < nslot ? lo + part / kPlanWaves : nslot;
-  count(expert, lo, hi, nexpert, cnt + wave * nexpert);
-  __syncthreads();
-  for (int e = threadIdx.x; e < nexpert; e += blockDim.x) {
-    int run = off[e] + hist[(int64_t)e * gridDim.x + blockIdx.x];
-    for (int w = 0; w < kPlanWaves; ++w) {
-      const int c = cnt[w * nexpert + e];
-      cnt[w * nexpert + e] = run;
-      run += c;
-    }
-    if (blockIdx.x == 0) offsets[e] = off[e];
-  }
-  if (blockIdx.x == 0 && threadIdx.x == 0) offsets[nexpert] = kept;
-  for (int64_t r = kept + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; r < nslot; r += (int64_t)gridDim.x * blockDim.x)
-    rows[r] = -1;
-  __syncthreads();
-  place(expert, lo, hi, nexpert, cnt + wave * nexpert, rows, pos);
-}
+  __device__ __forceinline__ void first(int e, int row) const { offsets[e] = row; }
+  __device__ __forceinline__ void total(int kept) const { offsets[nexpert] = kept; }
+  __device__ __forceinline__ void empty(int64_t r) const { rows[r] = -1; }
+};
 
 // ---------------------------------------------------------------------------
 // rows
@@ -262,16 +64,6 @@ struct Shape {
 constexpr int64_t kOnceBytes = (int64_t)192 << 20;
 
 constexpr int kBlock = 256;
-
-// weight times an element: a product in the type of sums, rounded to it before it
-// is rounded to the element's type (one fused multiply would round once, and
-// differ from what a caller gets from the two operations)
-template <typename T>
-__device__ __forceinline__ T times(typename ElemAcc<T>::type w, T v) {
-  typename ElemAcc<T>::type p = w * (typename ElemAcc<T>::type)v;
-  if constexpr (sizeof(T) == 2) asm("" : "+v"(p));  // the product is a value of its own
-  return (T)p;
-}
 
 template <typename T, bool WEIGHT, bool ONCE>
 __global__ __launch_bounds__(kBlock) void combine_kernel(Shape sh, const T* __restrict__ x, int64_t ldx,
@@ -500,8 +292,7 @@ extern "C" size_t dpc_route_workspace_bytes(int ntok, int topk, int nexpert) {
   if (ntok < 0 || topk < 1 || topk > DPC_MAX_TOPK || nexpert < 1 || nexpert > DPC_MAX_EXPERTS) return 0;
   const int64_t nslot = (int64_t)ntok * topk;
   if (nslot > kMaxSlots) return 0;
-  const size_t blocks = nslot <= kOneBlockSlots ? 0 : plan_blocks(nslot);
-  return ((blocks + 1) * nexpert * sizeof(int) + 255) / 256 * 256;
+  return sort_workspace_bytes(nslot, nexpert);
 }
 
 extern "C" int dpc_route_plan(void* stream, int ntok, int topk, int nexpert, const int* expert, void* workspace,
@@ -518,24 +309,7 @@ extern "C" int dpc_route_plan(void* stream, int ntok, int topk, int nexpert, con
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();  // report only what these launches raise
-  if (nslot <= kOneBlockSlots) {
-    const int waves = nslot <= 256 ? 4 : 16;
-    const size_t lds = ((size_t)(waves + 1) * nexpert + waves) * sizeof(int);
-    hipLaunchKernelGGL(plan_one_kernel, dim3(1), dim3(64 * waves), lds, s, (int)nslot, nexpert, expert, offsets, rows,
-                       pos);
-    return dpc_internal_launch_status();
-  }
-  const int blocks = plan_blocks(nslot);
-  const int64_t part = plan_part(nslot, blocks);
-  int* hist = static_cast<int*>(workspace);
-  int* total = hist + (size_t)blocks * nexpert;
-  const dim3 block(64 * kPlanWaves);
-  hipLaunchKernelGGL(plan_count_kernel, dim3(blocks), block, (size_t)kPlanWaves * nexpert * sizeof(int), s, nslot, part,
-                     nexpert, expert, hist);
-  hipLaunchKernelGGL(plan_scan_kernel, dim3(nexpert), dim3(256), 0, s, blocks, hist, total);
-  hipLaunchKernelGGL(plan_place_kernel, dim3(blocks), block,
-                     ((size_t)(kPlanWaves + 1) * nexpert + kPlanWaves) * sizeof(int), s, nslot, part, nexpert, expert,
-                     hist, total, offsets, rows, pos);
+  launch_sort(s, nslot, nexpert, PlanJob{expert, offsets, rows, pos, nexpert}, workspace);
   return dpc_internal_launch_status();
 }
 

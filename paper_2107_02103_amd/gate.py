@@ -1,0 +1,166 @@
+"""Convenience objects of the calls before a routing: the choice of experts and
+vectors of ids.  As Route's, their methods check arguments and allocate outputs;
+all arithmetic happens in libdpc, and no call is recorded for torch's autograd:
+gradients are methods of their own."""
+import ctypes as C
+
+import torch
+
+from . import binding as B
+from .experts import (_MOST, _check, _current_device, _elem_of, _enter, _lib, _on, _raw_stream, _rows, _too_large)
+
+_SCORES = {"softmax": B.DPC_SCORE_SOFTMAX, "sigmoid": B.DPC_SCORE_SIGMOID}
+
+
+class Gate:
+    """Which experts a token goes to, and with which weights, from its scores.
+
+    nexpert, topk  experts, and how many of them a token is sent to
+    score          "softmax" or "sigmoid" of the logits
+    bias           float32 [nexpert] or None: added to the scores for the choice
+                   alone, as what balances the experts' loads
+    groups, keep, best  the experts stand in `groups` groups of equal size, of
+                   which a token keeps the `keep` with the largest sum of their
+                   `best` (1 or 2) largest biased scores
+    renormalise    the weights of a token are divided by their sum
+    scale          factor of all weights
+
+    An expert whose logit is -infinity is closed to the token."""
+
+    def __init__(self, nexpert, topk, score="softmax", groups=1, keep=1, best=1, bias=None, renormalise=False, scale=1.0):
+        if score not in _SCORES:
+            raise ValueError(f"score is softmax or sigmoid, not {score!r}")
+        sizes = [int(v) for v in (nexpert, topk, groups, keep, best)]
+        if max(map(abs, sizes)) > _MOST:
+            _too_large("dpc_gate")
+        self.nexpert, self.topk = sizes[:2]
+        if bias is not None:
+            if bias.dtype != torch.float32 or bias.shape != (self.nexpert,) or not bias.is_contiguous():
+                raise ValueError("bias must be contiguous float32 [nexpert]")
+            _on(bias, None, "bias")
+        self.bias = bias
+        self.spec = B.dpc_gate_spec(self.nexpert, self.topk, _SCORES[score], sizes[2], sizes[3], sizes[4], bool(renormalise),
+                                    float(scale))
+        self._spec = C.byref(self.spec)
+
+    def _logits(self, logits, dev):
+        ld = _rows(logits, "logits", None, self.nexpert, None, dev)
+        if logits.shape[0] > _MOST:
+            _too_large("dpc_gate")
+        return ld, torch.float64 if logits.dtype == torch.float64 else torch.float32
+
+    def __call__(self, logits, stream=None):
+        """Experts int32 [tokens, topk], the best first (-1: none left), and their
+        weights [tokens, topk] (float64 for float64 logits, else float32): what
+        Route and Route.combine take."""
+        _on(logits, None, "logits")
+        dev = logits.get_device()
+        if stream is not None or _current_device() != dev:
+            with _enter(dev, stream):
+                return self(logits)
+        ld, wt = self._logits(logits, None)
+        bias = self.bias
+        if bias is not None:
+            _on(bias, dev, "bias")
+            bias = bias.data_ptr()
+        n, elem = logits.shape[0], _elem_of(logits.dtype)
+        shape = (n, max(self.topk, 0))
+        expert = torch.empty(shape, dtype=torch.int32, device=logits.device)
+        weight = torch.empty(shape, dtype=wt, device=logits.device)
+        _check(_lib.dpc_gate(_raw_stream(dev), elem, self._spec, n, logits.data_ptr(), ld, bias, expert.data_ptr(),
+                             weight.data_ptr()), "dpc_gate")
+        return expert, weight
+
+    def backward(self, logits, expert, dweight, out=None, stream=None):
+        """dE/dlogits from dE/dweight at the experts chosen (such as
+        Route.combine_backward gives)."""
+        _on(logits, None, "logits")
+        dev = logits.get_device()
+        if stream is not None or _current_device() != dev:
+            with _enter(dev, stream):
+                return self.backward(logits, expert, dweight, out)
+        ld, wt = self._logits(logits, None)
+        n, elem = logits.shape[0], _elem_of(logits.dtype)
+        for name, t, dt in (("expert", expert, torch.int32), ("dweight", dweight, wt)):
+            if t.dtype != dt or t.shape != (n, self.topk) or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {dt} [tokens, topk]")
+            _on(t, dev, name)
+        if out is None:
+            out, ldo = torch.empty((n, self.nexpert), dtype=logits.dtype, device=logits.device), self.nexpert
+        else:
+            ldo = _rows(out, "out", n, self.nexpert, logits.dtype, dev)
+        _check(_lib.dpc_gate_bwd(_raw_stream(dev), elem, self._spec, n, logits.data_ptr(), ld, expert.data_ptr(),
+                                 dweight.data_ptr(), out.data_ptr(), ldo), "dpc_gate_bwd")
+        return out
+
+
+def _ids(ids):
+    if ids.dtype != torch.int32 or ids.dim() != 1 or not ids.is_contiguous():
+        raise ValueError("ids must be contiguous int32 [tokens]")
+    _on(ids, None, "ids")
+    if ids.shape[0] > _MOST:
+        _too_large("dpc_embed")
+    return ids.get_device()
+
+
+class Embedding:
+    """A vector for each id (the species of an atom, a token), times a scale.
+
+    table  [ids, width], rows of any stride
+    An id outside [0, ids) stands for nothing: its vector is zeros, and it has no
+    part in the gradient."""
+
+    def __init__(self, table, scale=1.0):
+        self._ld = _rows(table, "table")
+        self.table, self.scale = table, float(scale)
+        self.ids, self.width = table.shape
+        self._device, self._elem = table.get_device(), _elem_of(table.dtype)
+        if self.ids > _MOST or self.width > _MOST:
+            _too_large("dpc_embed")
+
+    def __call__(self, ids, out=None, stream=None):
+        """[tokens, width] of ids int32 [tokens]."""
+        if stream is not None or _current_device() != self._device:
+            with _enter(self._device, stream):
+                return self(ids, out)
+        if _ids(ids) != self._device:
+            _on(ids, self._device, "ids")
+        n = ids.shape[0]
+        if out is None:
+            out, ldy = self.table.new_empty((n, self.width)), self.width or 1
+        else:
+            ldy = _rows(out, "out", n, self.width, self.table.dtype, self._device)
+        _check(_lib.dpc_embed(_raw_stream(self._device), self._elem, n, self.ids, self.width, ids.data_ptr(),
+                              self.table.data_ptr(), self._ld, self.scale, out.data_ptr(), ldy), "dpc_embed")
+        return out
+
+    def backward(self, ids, dy, dtype=None, out=None, stream=None):
+        """dE/dtable from dE/dy (see gradient)."""
+        if dy.dim() != 2 or dy.shape[1] != self.width:
+            raise ValueError(f"dy has shape {tuple(dy.shape)}, expected [tokens, {self.width}]")
+        _on(dy, self._device, "dy")
+        return Embedding.gradient(ids, dy, self.ids, self.scale, dtype, out, stream)
+
+    @staticmethod
+    def gradient(ids, dy, nid, scale=1.0, dtype=None, out=None, stream=None):
+        """[nid, width]: scale times the sum of the rows of dy [tokens, width] of
+        each id, in dy's type or (dtype=torch.float32) in float32."""
+        dev = _ids(ids)
+        if stream is not None or _current_device() != dev:
+            with _enter(dev, stream):
+                return Embedding.gradient(ids, dy, nid, scale, dtype, out)
+        n, nid = ids.shape[0], int(nid)
+        lddy, width = _rows(dy, "dy", n, None, None, dev), dy.shape[1]
+        if abs(nid) > _MOST or width > _MOST:
+            _too_large("dpc_embed_bwd")
+        dtype = dy.dtype if dtype is None else dtype
+        elem, elem_d = _elem_of(dy.dtype), _elem_of(dtype)
+        if out is None:
+            out, ldo = dy.new_empty((max(nid, 0), width), dtype=dtype), width or 1
+        else:
+            ldo = _rows(out, "out", nid, width, dtype, dev)
+        nb = _lib.dpc_embed_bwd_workspace_bytes(elem, n, nid, width)
+        ws = torch.empty(nb, dtype=torch.uint8, device=dy.device)
+        _check(_lib.dpc_embed_bwd(_raw_stream(dev), elem, elem_d, n, nid, width, ids.data_ptr(), dy.data_ptr(), lddy,
+                                  float(scale), ws.data_ptr(), nb, out.data_ptr(), ldo), "dpc_embed_bwd")
+        return out

@@ -1,0 +1,187 @@
+"""Convenience objects of the calls in microscaled 4-bit floating point, beside
+Int8Linear: they check arguments and allocate outputs; all arithmetic happens in
+libdpc.  No call is recorded for torch's autograd."""
+import torch
+
+from . import binding as B
+from .experts import (_MOST, _check, _current_device, _elem_of, _enter, _lib, _on, _raw_stream, _rows, _too_large)
+
+
+def _bytes(t, shape, name, device):
+    if t.dtype != torch.uint8 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous uint8 {list(shape)}")
+    _on(t, device, name)
+
+
+def _quantise(x, groups):
+    """Codes and scales of rows x, in `groups` matrices of equal size."""
+    dev, (rows, cols) = x.get_device(), x.shape
+    ldx = _rows(x, "x")
+    if rows > _MOST or cols > _MOST:
+        _too_large("dpc_quant_mx4")
+    ld, n = B.mx4_ld(cols), rows // groups if groups else 0
+    codes = torch.empty((groups, n, ld // 2), dtype=torch.uint8, device=x.device)
+    scales = torch.empty((groups, ld // 256, n, 8), dtype=torch.uint8, device=x.device)
+    _check(_lib.dpc_quant_mx4(_raw_stream(dev), _elem_of(x.dtype), groups, n, cols, x.data_ptr(), ldx, codes.data_ptr(),
+                              scales.data_ptr()), "dpc_quant_mx4")
+    return codes, scales
+
+
+def _values(codes, scales, cols, dtype, out, dev):
+    """Rows that codes [groups, n, .] and scales [groups, ., n, 8] stand for."""
+    groups, n = codes.shape[:2]
+    if out is None:
+        out, ldy = torch.empty((groups * n, cols), dtype=dtype, device=codes.device), cols
+    else:
+        ldy = _rows(out, "out", groups * n, cols, dtype, dev)
+    _check(_lib.dpc_values_mx4(_raw_stream(dev), _elem_of(dtype), groups, n, cols, codes.data_ptr(), scales.data_ptr(),
+                               out.data_ptr(), ldy), "dpc_values_mx4")
+    return out
+
+
+class Mx4Rows:
+    """Rows in 4-bit floating-point codes with a power of two for every 32 columns.
+
+    codes   uint8 [rows, mx4_ld(cols) / 2]: two columns in a byte
+    scales  uint8 [mx4_ld(cols) / 256, rows, 8]: exponents, plus 127"""
+
+    def __init__(self, codes, scales, cols):
+        self.cols = int(cols)
+        if self.cols < 1 or codes.dim() != 2:
+            raise ValueError("codes must be contiguous uint8 [rows, mx4_ld(cols) / 2]")
+        self._device, n, ld = codes.get_device(), codes.shape[0], B.mx4_ld(self.cols)
+        if n > _MOST or self.cols > _MOST:
+            _too_large("dpc_values_mx4")
+        _bytes(codes, (n, ld // 2), "codes", None)
+        _bytes(scales, (ld // 256, n, 8), "scales", self._device)
+        self.codes, self.scales = codes, scales
+
+    @classmethod
+    def from_rows(cls, x, stream=None):
+        """Codes the rows of x [rows, cols]."""
+        _rows(x, "x")
+        dev = x.get_device()
+        if stream is not None or _current_device() != dev:
+            with _enter(dev, stream):
+                return cls.from_rows(x)
+        codes, scales = _quantise(x, 1)
+        r = cls.__new__(cls)
+        r.cols, r._device, r.codes, r.scales = x.shape[1], dev, codes[0], scales[0]
+        return r
+
+    def values(self, dtype=torch.float32, out=None, stream=None):
+        """[rows, cols]: what the codes stand for."""
+        if stream is not None or _current_device() != self._device:
+            with _enter(self._device, stream):
+                return self.values(dtype, out)
+        return _values(self.codes[None], self.scales[None], self.cols, dtype, out, self._device)
+
+
+class Mx4Linear:
+    """A layer y = x W^T + b on 4-bit floating-point codes of x and W, or one layer
+    for each expert: as Int8Linear, with half its bytes.
+
+    Each product is off by 13 to 17% of its norm: for nets that were trained with
+    these codes, and for searches.  A layer of the codes of W^T approximates the
+    gradient in x; it is not the derivative of y.
+
+    codes   uint8 [experts, outer, mx4_ld(inner) / 2] (or [outer, ...] for one)
+    scales  uint8 [experts, mx4_ld(inner) / 256, outer, 8]
+    bias    float32 [experts, outer] or None"""
+
+    def __init__(self, codes, scales, inner, bias=None):
+        if codes.dim() == 2:
+            codes, scales = codes[None], scales[None]
+            bias = None if bias is None else bias[None]
+        self.inner = int(inner)
+        if codes.dim() != 3 or self.inner < 1:
+            raise ValueError("codes must be contiguous uint8 [experts, outer, mx4_ld(inner) / 2]")
+        self.experts, self.outer = codes.shape[:2]
+        if self.inner > _MOST or self.experts > _MOST or self.outer > _MOST:
+            _too_large("dpc_linear_mx4")
+        ld, self._device = B.mx4_ld(self.inner), codes.get_device()
+        _bytes(codes, (self.experts, self.outer, ld // 2), "codes", None)
+        _bytes(scales, (self.experts, ld // 256, self.outer, 8), "scales", self._device)
+        if bias is not None:
+            if bias.dtype != torch.float32 or bias.shape != codes.shape[:2] or not bias.is_contiguous():
+                raise ValueError("bias must be contiguous float32 [experts, outer]")
+            _on(bias, self._device, "bias")
+        self.codes, self.scales, self.bias = codes, scales, bias
+
+    @classmethod
+    def from_weight(cls, weight, bias=None, stream=None):
+        """Codes the rows (output channels) of weight [experts, outer, inner] or
+        [outer, inner]; bias of any floating type."""
+        w = weight[None] if weight.dim() == 2 else weight
+        if w.dim() != 3:
+            raise ValueError("weight must be [experts, outer, inner] or [outer, inner]")
+        _on(w, None, "weight")
+        if stream is not None or _current_device() != w.get_device():
+            with _enter(w.get_device(), stream):
+                return cls.from_weight(weight, bias)
+        g, n, k = w.shape
+        codes, scales = _quantise(w.contiguous().view(g * n, k), g)
+        if bias is not None:
+            bias = bias.to(torch.float32).reshape(g, n).contiguous()
+        return cls(codes, scales, k, bias)
+
+    def weight(self, dtype=torch.float32, stream=None):
+        """[experts, outer, inner]: the weights that the codes stand for."""
+        if stream is not None or _current_device() != self._device:
+            with _enter(self._device, stream):
+                return self.weight(dtype)
+        return _values(self.codes, self.scales, self.inner, dtype, None, self._device).view(
+            self.experts, self.outer, self.inner)
+
+    def __call__(self, x, route=None, offsets=None, dtype=None, out=None, stream=None):
+        """y [tokens, outer] of x [tokens, inner], or of Mx4Rows (rows coded once for
+        several layers).  With a route, x holds the tokens and y its rows (each from
+        its expert's layer); with offsets (int32 [experts + 1]), the rows of x are
+        sorted by expert already.  dtype: type of y (default: that of x; float32 for
+        Mx4Rows)."""
+        if stream is not None or _current_device() != self._device:
+            with _enter(self._device, stream):
+                return self(x, route, offsets, dtype, out)
+        dev, coded = self._device, isinstance(x, Mx4Rows)
+        ntok, topk, rows = x.codes.shape[0] if coded else x.shape[0], 1, None
+        if coded:
+            _on(x.codes, dev, "x")
+            if x.cols != self.inner or (route is not None and ntok != route.ntok):
+                raise ValueError(f"x has {ntok} rows of {x.cols} columns, expected "
+                                 f"{'rows' if route is None else route.ntok} of {self.inner}")
+        else:
+            ldx = _rows(x, "x", None if route is None else route.ntok, self.inner, None, dev)
+        if ntok > _MOST:
+            _too_large("dpc_linear_mx4")
+        if route is not None:
+            if offsets is not None:
+                raise ValueError("give a route or offsets, not both")
+            _on(route.rows, dev, "route")
+            topk, rows, offsets = route.topk, route.rows.data_ptr(), route.offsets
+        if offsets is not None:
+            if offsets.dtype != torch.int32 or not offsets.is_contiguous():
+                raise TypeError("offsets must be contiguous int32")
+            if len(offsets) != self.experts + 1:
+                raise ValueError(f"offsets for {len(offsets) - 1} experts, layers for {self.experts}")
+            _on(offsets, dev, "offsets")
+            offsets = offsets.data_ptr()
+        elif self.experts != 1:
+            raise ValueError("layers of several experts need a route or offsets")
+        if dtype is None:
+            dtype = torch.float32 if coded else x.dtype
+        if out is None:
+            out, ldy = torch.empty((ntok * topk, self.outer), dtype=dtype, device=self.codes.device), self.outer
+        else:
+            ldy = _rows(out, "out", ntok * topk, self.outer, dtype, dev)
+        tail = (rows, offsets, self.codes.data_ptr(), self.scales.data_ptr(),
+                None if self.bias is None else self.bias.data_ptr())
+        if coded:
+            _check(_lib.dpc_matmul_mx4(_raw_stream(dev), _elem_of(dtype), ntok, topk, self.outer, self.inner, self.experts,
+                                       x.codes.data_ptr(), x.scales.data_ptr(), *tail, out.data_ptr(), ldy), "dpc_matmul_mx4")
+            return out
+        nb = _lib.dpc_linear_mx4_workspace_bytes(ntok, self.inner)
+        ws = self.codes.new_empty(nb)
+        _check(_lib.dpc_linear_mx4(_raw_stream(dev), _elem_of(x.dtype), _elem_of(dtype), ntok, topk, self.outer, self.inner,
+                                   self.experts, x.data_ptr(), ldx, *tail, ws.data_ptr(), nb, out.data_ptr(), ldy),
+               "dpc_linear_mx4")
+        return out
