@@ -19,6 +19,7 @@
 #include "dpc.h"
 #include "dpc_elem.h"
 #include "dpc_groups.h"
+#include "dpc_i8_tiles.h"
 #include "dpc_internal.h"
 
 namespace {
@@ -252,14 +253,199 @@ __global__ __launch_bounds__(256) void product_kernel(Product p, TY* __restrict_
   }
 }
 
-int product(hipStream_t s, dpc_elem elem_y, const Product& p, void* y, int64_t ldy) {
-  return by_elem(elem_y, [&](auto t) {
-    typedef decltype(t) TY;
+// Tiles of BM rows times BN channels, K in steps of 256 columns: codes and scales
+// of both operands go from memory to LDS without passing registers, the next
+// step's while the matrix cores work on this one's.  A row of a step is 8 chunks of
+// 16 bytes, one block each; chunk c of row r lies in slot c ^ (r & 7), so that the
+// lanes of one LDS read (16 rows, the same chunk) meet all banks.  The scales of a
+// row are 8 bytes in a row, of which a lane reads the two of its chunks.
+template <typename TY, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, int col_tiles, TY* __restrict__ y,
+                                                                     int64_t ldy) {
+  constexpr int VE = 16 / sizeof(TY);
+  constexpr int kWaves = WM * WN, TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
+  constexpr int kStep = 128, kRows = BM + BN;
+  constexpr int kLoads = kRows / 8 / kWaves;       // 8 rows of codes each
+  constexpr int kScaleLoads = (kRows / 32 + kWaves - 1) / kWaves;  // 32 rows of scales each
+  static_assert(kLoads * kWaves * 8 == kRows && kRows % 32 == 0, "every load is whole");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2][kRows * kStep];
+  __shared__ __attribute__((aligned(16))) uint8_t scales[2][kRows * 8];
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave % WM, wn = wave / WM;
+
+  // consecutive workgroups go to different XCDs: each XCD gets a run of tiles
+  // of its own, in bands of 8 row tiles, so that its L2 serves tiles that share
+  // rows; the runs are cut from the tiles that exist, for equal work
+  const int row_tiles = count_tiles(p, BM);
+  const int total = row_tiles * col_tiles, per = (total + 7) / 8;
+  const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || id >= total) return;
+  const int band = id / (8 * col_tiles), in = id - band * 8 * col_tiles;
+  const int high = min(8, row_tiles - band * 8);
+  const int ct = in / high, rt = band * 8 + in % high;
+
+  const Tile t = find_tile(p, BM, rt);
+  if (t.row0 >= t.end) return;
+  const int c0 = ct * BN;
+
+  if (t.group < 0) {  // rows of no expert
+    const int high_rows = t.end - t.row0, wide = min(BN, p.n - c0);
+    for (int e = threadIdx.x; e < high_rows * wide; e += 64 * kWaves)
+      y[(int64_t)(t.row0 + e / wide) * ldy + c0 + e % wide] = (TY)0;
+    return;
+  }
+
+  v4f acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+  // this lane's rows of the loads: x rows first, then rows of W
+  const uint8_t* src[kLoads];
+  int dst[kLoads];
+#pragma unroll
+  for (int l = 0; l < kLoads; ++l) {
+    const int r8 = (wave * kLoads + l) * 8, r = r8 + (lane >> 3);
+    const int chunk = (lane & 7) ^ (r < BM ? r & 7 : turn_of<VE>(r));
+    const uint8_t* row;
+    if (r < BM) {
+      const int tok = token_of(p, min(t.row0 + r, t.end - 1));
+      row = p.qx + (int64_t)(tok < 0 ? 0 : tok) * p.steps * kStep;
+    } else {
+      row = p.qw + ((int64_t)t.group * p.n + min(c0 + r - BM, p.n - 1)) * p.steps * kStep;
+    }
+    src[l] = row + chunk * 16;
+    dst[l] = r8 * kStep;
+  }
+  // and of the scales: 4 bytes each, two lanes to a row
+  const uint8_t* ssrc[kScaleLoads];
+  int64_t sstep[kScaleLoads];
+#pragma unroll
+  for (int l = 0; l < kScaleLoads; ++l) {
+    const int r = min((l * kWaves + wave) * 32, kRows - 32) + (lane >> 1);
+    if (r < BM) {
+      const int tok = token_of(p, min(t.row0 + r, t.end - 1));
+      ssrc[l] = p.sx + (int64_t)(tok < 0 ? 0 : tok) * 8;
+      sstep[l] = (int64_t)p.ntok * 8;
+    } else {
+      ssrc[l] = p.sw + ((int64_t)t.group * p.steps * p.n + min(c0 + r - BM, p.n - 1)) * 8;
+      sstep[l] = (int64_t)p.n * 8;
+    }
+    ssrc[l] += (lane & 1) * 4;
+  }
+  auto fetch = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+      __builtin_amdgcn_global_load_lds((GlobalPtr)src[l], (LdsPtr)(&lds[buf][dst[l]]), 16, 0, 0);
+      src[l] += kStep;
+    }
+#pragma unroll
+    for (int l = 0; l < kScaleLoads; ++l) {
+      const int r32 = l * kWaves + wave;  // of every wavefront there is one, of some there may be one more
+      if (r32 * 32 < kRows) __builtin_amdgcn_global_load_lds((GlobalPtr)ssrc[l], (LdsPtr)(&scales[buf][r32 * 256]), 4, 0, 0);
+      ssrc[l] += sstep[l];
+    }
+  };
+  fetch(0);
+  for (int s = 0; s < p.steps; ++s) {
+    // vmcnt(0), lgkmcnt(0): this step's rows are in LDS, the step before has
+    // been read; the barrier says so for every wavefront
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (s + 1 < p.steps) fetch((s + 1) & 1);
+    const uint8_t* xs = &lds[s & 1][wm * TM * kStep];
+    const uint8_t* ws = &lds[s & 1][(BM + wn * TN) * kStep];
+    const uint8_t* xe = &scales[s & 1][wm * TM * 8 + quad * 2];
+    const uint8_t* we = &scales[s & 1][(BM + wn * TN) * 8 + quad * 2];
+    v4i a[2][NI], b[2][MI];
+    int ea[NI], eb[MI];
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+      ea[j] = *reinterpret_cast<const uint16_t*>(we + (channel_of<VE>(j, 0) + channel_of<VE>(0, l16)) * 8);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) eb[i] = *reinterpret_cast<const uint16_t*>(xe + (i * 16 + l16) * 8);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int slot = ((quad * 2 + k) ^ (l16 & 7)) * 16;
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+        a[k][j] = *reinterpret_cast<const v4i*>(ws + (channel_of<VE>(j, 0) + channel_of<VE>(0, l16)) * kStep + slot);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) b[k][i] = *reinterpret_cast<const v4i*>(xs + (i * 16 + l16) * kStep + slot);
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) acc[i][j] = mfma4<0>(a[0][j], b[0][i], acc[i][j], ea[j], eb[i]);
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) acc[i][j] = mfma4<1>(a[1][j], b[1][i], acc[i][j], ea[j], eb[i]);
+    asm volatile("" ::: "memory");
+  }
+
+  // this lane's results: row l16 of each row tile, runs of VE channels from
+  // first, first + 4 VE, ...
+  constexpr int kRuns = NI * 4 / VE;
+  const int first = c0 + wn * TN + quad * VE;
+  const bool whole = c0 + BN <= p.n;
+  float bias[kRuns][VE];
+#pragma unroll
+  for (int g = 0; g < kRuns; ++g)
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const int c = min(first + g * 4 * VE + e, p.n - 1);
+      bias[g][e] = p.bias ? p.bias[(int64_t)t.group * p.n + c] : 0.0f;
+    }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int r = t.row0 + wm * TM + i * 16 + l16;
+    const int tok = token_of(p, min(r, t.end - 1));
+    TY* py = y + (int64_t)r * ldy + first;
+#pragma unroll
+    for (int g = 0; g < kRuns; ++g) {
+      TY out[VE];
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        out[e] = result<TY>(acc[i][(g * VE + e) / 4][(g * VE + e) % 4], bias[g][e]);
+        if (tok < 0) out[e] = (TY)0;  // a row of the group that no slot owns
+      }
+      const int left = r >= t.end ? 0 : whole ? VE : p.n - (first + g * 4 * VE);
+      put_run(py + g * 4 * VE, out, left);
+    }
+  }
+}
+
+template <typename TY, int BM, int BN, int WM, int WN>
+void launch_tiled(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
+  const int col_tiles = (p.n + BN - 1) / BN;
+  const unsigned per = ((unsigned)most_tiles(p, BM) * (unsigned)col_tiles + 7) / 8;
+  hipLaunchKernelGGL((product_tiled_kernel<TY, BM, BN, WM, WN>), dim3(per * 8), dim3(64 * WM * WN), 0, s, p, col_tiles,
+                     y, ldy);
+}
+
+template <typename TY>
+void launch_product(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
+  if (i8_few_rows(p.m, p.n, p.ngroup, p.offsets != nullptr)) {
     const int64_t tiles = most_tiles(p, 16);
     const unsigned gy = (unsigned)(tiles < 32768 ? tiles : 32768);
     hipLaunchKernelGGL(product_kernel<TY>, dim3((unsigned)((p.n + 63) / 64), gy, (unsigned)((tiles + gy - 1) / gy)), dim3(256),
-                       0, s, p, (TY*)y, ldy);
-  });
+                       0, s, p, y, ldy);
+    return;
+  }
+  switch (i8_tile(p.m, p.n, p.steps * 128, p.ngroup, p.offsets != nullptr)) {
+    case 0: return launch_tiled<TY, 256, 256, 2, 4>(s, p, y, ldy);
+    case 1: return launch_tiled<TY, 128, 128, 2, 2>(s, p, y, ldy);
+    case 2: return launch_tiled<TY, 128, 64, 2, 2>(s, p, y, ldy);
+    default: return launch_tiled<TY, 64, 64, 2, 2>(s, p, y, ldy);
+  }
+}
+
+int product(hipStream_t s, dpc_elem elem_y, const Product& p, void* y, int64_t ldy) {
+  return by_elem(elem_y, [&](auto t) { launch_product(s, p, (decltype(t)*)y, ldy); });
 }
 
 int product_args(dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup) {
