@@ -268,8 +268,9 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
   constexpr int kLoads = kRows / 8 / kWaves;       // 8 rows of codes each
   constexpr int kScaleLoads = (kRows / 32 + kWaves - 1) / kWaves;  // 32 rows of scales each
   static_assert(kLoads * kWaves * 8 == kRows && kRows % 32 == 0, "every load is whole");
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2][kRows * kStep];
-  __shared__ __attribute__((aligned(16))) uint8_t scales[2][kRows * 8];
+  // codes, then scales: of two arrays the compiler would wait for every load before
+  // it reads one
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2][kRows * (kStep + 8)];
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % WM, wn = wave / WM;
@@ -344,7 +345,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
 #pragma unroll
     for (int l = 0; l < kScaleLoads; ++l) {
       const int r32 = l * kWaves + wave;  // of every wavefront there is one, of some there may be one more
-      if (r32 * 32 < kRows) __builtin_amdgcn_global_load_lds((GlobalPtr)ssrc[l], (LdsPtr)(&scales[buf][r32 * 256]), 4, 0, 0);
+      if (r32 * 32 < kRows) __builtin_amdgcn_global_load_lds((GlobalPtr)ssrc[l], (LdsPtr)(&lds[buf][kRows * kStep + r32 * 256]), 4, 0, 0);
       ssrc[l] += sstep[l];
     }
   };
@@ -358,8 +359,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
     if (s + 1 < p.steps) fetch((s + 1) & 1);
     const uint8_t* xs = &lds[s & 1][wm * TM * kStep];
     const uint8_t* ws = &lds[s & 1][(BM + wn * TN) * kStep];
-    const uint8_t* xe = &scales[s & 1][wm * TM * 8 + quad * 2];
-    const uint8_t* we = &scales[s & 1][(BM + wn * TN) * 8 + quad * 2];
+    const uint8_t* xe = &lds[s & 1][kRows * kStep + wm * TM * 8 + quad * 2];
+    const uint8_t* we = &lds[s & 1][kRows * kStep + (BM + wn * TN) * 8 + quad * 2];
     v4i a[2][NI], b[2][MI];
     int ea[NI], eb[MI];
 #pragma unroll
@@ -384,6 +385,15 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, 
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int j = 0; j < NI; ++j) acc[i][j] = mfma4<1>(a[1][j], b[1][i], acc[i][j], ea[j], eb[i]);
+    // LDS reads of the second half between the products of the first
+    constexpr int kReads = NI + MI, kSpaced = 2 * kReads <= MI * NI ? 2 : 1;
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * kReads, 0);
+#pragma unroll
+    for (int q = 0; q < kReads; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, kSpaced, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 2 * MI * NI - kSpaced * kReads, 0);
     asm volatile("" ::: "memory");
   }
 
