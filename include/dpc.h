@@ -534,9 +534,8 @@ int dpc_embed(void* stream, dpc_elem elem, int ntok, int nid, int width, const i
 
 /* Gradient of dpc_embed in its table: tokens are sorted by id, then
  *   dtable[v] = scale * sum over t with ids[t] = v of dy[t]
- * (zeros for an id without tokens).  Runs of a few rows are summed in float32
- * (float64 for DPC_ELEM_F64), longer ones joined in float64, in an order that
- * depends on the sizes alone; rounded once.
+ * (zeros for an id without tokens).  Sums and scale are float64, in an order that
+ * depends on the sizes and the ids alone; rounded once.
  *   dy       device [ntok] rows of `width` elements of type `elem`
  *   dtable   device out [nid] rows of type elem_d: elem or DPC_ELEM_F32
  *   workspace  device, 16-byte aligned, >= dpc_embed_bwd_workspace_bytes()

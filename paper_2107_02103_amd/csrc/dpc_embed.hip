@@ -5,9 +5,9 @@
 //
 // Gradient: tokens are sorted by id (dpc_sort.h, up to 10 bits of the id a
 // pass), so that an id's tokens are a run of positions.  The positions are cut into
-// parts.  A group of lanes sums the runs of its part, in order; a run inside one
-// part is written out, of a run that crosses into another part both keep the
-// sum of their piece, which a second kernel joins.
+// parts.  A group of lanes sums the runs of its part, in order and in float64; a
+// run inside one part is written out, of a run that crosses into another part both
+// keep the sum of their piece, which a second kernel joins.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -35,30 +35,49 @@ int log2_lanes(int width, size_t es) {
 // ---------------------------------------------------------------------------
 // lookup
 // ---------------------------------------------------------------------------
-template <typename T>
+constexpr int kRowsAtOnce = 4;  // rows whose loads a group of lanes has under way
+
+// Results of 192 MiB and more (with addresses and strides multiples of 16 bytes)
+// go past the caches: they would not be found there by the call that uses them.
+constexpr int64_t kOnceBytes = (int64_t)192 << 20;
+
+template <typename T, bool ONCE>
 __global__ __launch_bounds__(kBlock) void embed_kernel(int ntok, int nid, int width, int lanes_log2,
                                                        const int* __restrict__ ids, const T* __restrict__ table, int64_t ldt,
                                                        typename ElemAcc<T>::type scale, T* __restrict__ y, int64_t ldy) {
-  constexpr int VE = Chunk<T>::kElems;
+  constexpr int VE = Chunk<T>::kElems, R = kRowsAtOnce;
   const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1);
-  const int64_t groups = ((int64_t)gridDim.x * kBlock) >> lanes_log2;
   const int nch = (width + VE - 1) / VE;
-  for (int64_t t = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> lanes_log2; t < ntok; t += groups) {
-    const int id = ids[t];
-    const bool live = (unsigned)id < (unsigned)nid;
-    const T* px = table + (int64_t)(live ? id : 0) * ldt;
-    T* py = y + t * ldy;
-    if (width < VE) {
-      for (int c = lane; c < width; c += lanes) py[c] = live ? times<T>(scale, px[c]) : (T)0;
-      continue;
-    }
-    for (int c = lane; c < nch; c += lanes) {
-      const int at = c * VE < width - VE ? c * VE : width - VE;
-      Chunk<T> ch;
-      ch.load(px + at);
+  const int64_t t0 = ((((int64_t)blockIdx.x * kBlock + threadIdx.x) >> lanes_log2)) * R;
+  if (t0 >= ntok) return;
+  const T* px[R];
+  bool live[R];
 #pragma unroll
-      for (int i = 0; i < VE; ++i) ch.v[i] = live ? times<T>(scale, ch.v[i]) : (T)0;
-      ch.store(py + at);
+  for (int j = 0; j < R; ++j) {
+    const int id = ids[t0 + j < ntok ? t0 + j : ntok - 1];
+    live[j] = (unsigned)id < (unsigned)nid;
+    px[j] = table + (int64_t)(live[j] ? id : 0) * ldt;
+  }
+  if (width < VE) {
+    for (int c = lane; c < width; c += lanes)
+#pragma unroll
+      for (int j = 0; j < R; ++j)
+        if (t0 + j < ntok) y[(t0 + j) * ldy + c] = live[j] ? times<T>(scale, px[j][c]) : (T)0;
+    return;
+  }
+  for (int c = lane; c < nch; c += lanes) {
+    const int at = c * VE < width - VE ? c * VE : width - VE;
+    Chunk<T> ch[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) ch[j].load(px[j] + at);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      if (t0 + j >= ntok) break;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) ch[j].v[i] = live[j] ? times<T>(scale, ch[j].v[i]) : (T)0;
+      T* py = y + (t0 + j) * ldy + at;
+      if (ONCE) ch[j].store_once(py);
+      else ch[j].store(py);
     }
   }
 }
@@ -108,14 +127,13 @@ struct Runs {
   const int* __restrict__ id;   // of each position, ascending
   const int* __restrict__ tok;
   const int* __restrict__ kept; // positions
-  int nid, width, part, parts, slabs, lanes_log2;
+  int nid, width, part, parts, slabs, lanes_log2, join_slabs, join_log2;
 };
 
-// Chunk of a lane: its first element, or -1.  Widths under a chunk: an element.
+// First element of chunk c, or -1.  Widths under a chunk: element c.
 template <typename T>
-__device__ __forceinline__ int chunk_at(const Runs& r, int slab, int lane) {
+__device__ __forceinline__ int chunk_at(const Runs& r, int c) {
   constexpr int VE = Chunk<T>::kElems;
-  const int c = (slab << r.lanes_log2) + lane;
   if (r.width < VE) return c < r.width ? c : -1;
   const int nch = (r.width + VE - 1) / VE;
   return c >= nch ? -1 : c * VE < r.width - VE ? c * VE : r.width - VE;
@@ -128,107 +146,219 @@ __device__ __forceinline__ void write_row(TD* p, int at, bool narrow, const S (&
     if (i == 0 || !narrow) p[at + i] = (TD)(sum[i] * scale);
 }
 
-// partial sums: [parts][2][width], 0: the run that comes from the part before,
-// 1: a run that starts here and goes on
-template <typename T, typename TD>
-__global__ __launch_bounds__(kBlock) void runs_kernel(Runs r, const T* __restrict__ dy, int64_t lddy,
-                                                      typename ElemAcc<T>::type scale,
-                                                      typename ElemAcc<T>::type* __restrict__ partial,
-                                                      TD* __restrict__ dtable, int64_t ldt) {
-  typedef typename ElemAcc<T>::type A;
-  constexpr int VE = Chunk<T>::kElems;
-  const int lane = threadIdx.x & ((1 << r.lanes_log2) - 1);
-  const int64_t item = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> r.lanes_log2;
-  if (item >= (int64_t)r.parts * r.slabs) return;
-  const int part = (int)(item / r.slabs), slab = (int)(item % r.slabs);
-  const int64_t n = *r.kept, p0 = (int64_t)part * r.part, p1 = min(n, p0 + r.part);
-  const int at = chunk_at<T>(r, slab, lane);
-  if (p0 >= p1 || at < 0) return;
-  const bool narrow = r.width < VE;
-  const int before = p0 > 0 ? r.id[p0 - 1] : -1, after = p1 < n ? r.id[p1] : -1;
-  A sum[VE];
-#pragma unroll
-  for (int i = 0; i < VE; ++i) sum[i] = (A)0;
-  int cur = r.id[p0];
-  auto flush = [&](int64_t end) {
-    const bool open_left = cur == before, open_right = end == p1 && cur == after;
-    if (!open_left && !open_right) {
-      write_row<TD>(dtable + cur * ldt, at, narrow, sum, scale);
-    } else {
-      // a run that fills the part and goes on both ways counts as one from the left
-      A* to = partial + ((int64_t)part * 2 + (open_left ? 0 : 1)) * r.width;
-      write_row<A>(to, at, narrow, sum, (A)1);
-    }
-  };
-  for (int64_t p = p0; p < p1; ++p) {
-    const int id = r.id[p];
-    if (id != cur) {
-      flush(p);
-      cur = id;
-#pragma unroll
-      for (int i = 0; i < VE; ++i) sum[i] = (A)0;
-    }
-    const T* px = dy + (int64_t)r.tok[p] * lddy + at;
-    if (narrow) {
-      sum[0] += (A)px[0];
-    } else {
-      Chunk<T> ch;
-      ch.load(px);
-#pragma unroll
-      for (int i = 0; i < VE; ++i) sum[i] += (A)ch.v[i];
-    }
-  }
-  flush(p1);
-}
-
-// First position from lo on (of n) whose id is above v.
-__device__ __forceinline__ int64_t behind(const int* id, int64_t lo, int64_t n, int v) {
-  int64_t hi = n;
+// First position (of n) whose id is v or above.
+__device__ __forceinline__ int64_t reaches(const int* id, int64_t n, int64_t v) {
+  int64_t lo = 0, hi = n;
   while (lo < hi) {
     const int64_t mid = (lo + hi) / 2;
-    if (id[mid] > v) hi = mid;
+    if (id[mid] >= v) hi = mid;
     else lo = mid + 1;
   }
   return lo;
 }
 
-template <typename T, typename TD>
-__global__ __launch_bounds__(kBlock) void join_kernel(Runs r, typename ElemAcc<T>::type scale,
-                                                      const typename ElemAcc<T>::type* __restrict__ partial,
+// Zeros in the rows of the ids of [64 k, 64 k + 64) that have no token, by one
+// wavefront: each lane looks for one id.
+template <typename TD>
+__device__ __forceinline__ void absent(const Runs& r, int64_t k, int64_t n, TD* dtable, int64_t ldt) {
+  constexpr int VE = Chunk<TD>::kElems;
+  const int lane = threadIdx.x & 63;
+  const int64_t v = k * 64 + lane;
+  const int64_t at = v < r.nid ? reaches(r.id, n, v) : 0;
+  const bool none = v < r.nid && (at >= n || r.id[at] != v);
+  Chunk<TD> zero;
+#pragma unroll
+  for (int i = 0; i < VE; ++i) zero.v[i] = (TD)0;
+  for (unsigned long long left = __ballot(none); left; left &= left - 1) {
+    TD* p = dtable + (k * 64 + __ffsll(left) - 1) * ldt;
+    if (r.width < VE) {
+      if (lane < r.width) p[lane] = (TD)0;
+    } else {
+      const int nch = (r.width + VE - 1) / VE;
+      for (int c = lane; c < nch; c += 64) zero.store(p + (c * VE < r.width - VE ? c * VE : r.width - VE));
+    }
+  }
+}
+
+// Sums of the runs of each part, and zeros in the rows of ids without tokens (the
+// workgroups from run_blocks on): one launch, since neither waits for the other.
+// partial sums: [parts][2][width], 0: the run that comes from the part before,
+// 1: a run that starts here and goes on.
+// kAtOnce rows of a part are under way at a time, whichever ids they belong to.
+// WIDE: a row takes a whole wavefront, and what is known of positions is scalar.
+constexpr int kAtOnce = 8;
+
+template <typename T, typename TD, bool WIDE>
+__global__ __launch_bounds__(kBlock) void runs_kernel(Runs r, unsigned run_blocks, const T* __restrict__ dy, int64_t lddy,
+                                                      double scale, double* __restrict__ partial,
                                                       TD* __restrict__ dtable, int64_t ldt) {
   constexpr int VE = Chunk<T>::kElems;
+  const int64_t n = *r.kept;
+  if (blockIdx.x >= run_blocks) {
+    const int64_t k = (int64_t)(blockIdx.x - run_blocks) * (kBlock / 64) + threadIdx.x / 64;
+    if (k * 64 < r.nid) absent<TD>(r, k, n, dtable, ldt);
+    return;
+  }
   const int lane = threadIdx.x & ((1 << r.lanes_log2) - 1);
   const int64_t item = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> r.lanes_log2;
   if (item >= (int64_t)r.parts * r.slabs) return;
-  const int part = (int)(item / r.slabs), slab = (int)(item % r.slabs);
-  const int64_t n = *r.kept, p0 = (int64_t)part * r.part, p1 = min(n, p0 + r.part);
-  const int at = chunk_at<T>(r, slab, lane);
-  if (p1 >= n || p0 >= p1 || at < 0) return;
-  const int v = r.id[p1 - 1];
-  if (r.id[p1] != v || (p0 > 0 && r.id[p0 - 1] == v)) return;  // the run ends here, or starts before
+  int part = (int)(item / r.slabs);
+  const int slab = (int)(item % r.slabs);
+  if (WIDE) part = __builtin_amdgcn_readfirstlane(part);
+  const int64_t p0 = (int64_t)part * r.part, p1 = min(n, p0 + r.part);
+  const int at = chunk_at<T>(r, (slab << r.lanes_log2) + lane);
+  if (p0 >= p1 || (!WIDE && at < 0)) return;
   const bool narrow = r.width < VE;
-  const int last = (int)((behind(r.id, p1, n, v) - 1) / r.part);
+  const int before = p0 > 0 ? r.id[p0 - 1] : -1, after = p1 < n ? r.id[p1] : -1;
   double sum[VE];
 #pragma unroll
-  for (int i = 0; i < VE; ++i) sum[i] = i == 0 || !narrow ? (double)partial[((int64_t)part * 2 + 1) * r.width + at + i] : 0.0;
-  for (int q = part + 1; q <= last; ++q) {
+  for (int i = 0; i < VE; ++i) sum[i] = 0.0;
+  int cur = r.id[p0];
+  auto flush = [&](int64_t end) __attribute__((always_inline)) {
+    const bool open_left = cur == before, open_right = end == p1 && cur == after;
+    if (at < 0) return;
+    if (!open_left && !open_right) {
+      write_row<TD>(dtable + cur * ldt, at, narrow, sum, scale);
+    } else {
+      // a run that fills the part and goes on both ways counts as one from the left
+      write_row<double>(partial + ((int64_t)part * 2 + (open_left ? 0 : 1)) * r.width, at, narrow, sum, 1.0);
+    }
+  };
+  for (int64_t p = p0; p < p1; p += kAtOnce) {
+    int id[kAtOnce], tok[kAtOnce];
 #pragma unroll
-    for (int i = 0; i < VE; ++i)
-      if (i == 0 || !narrow) sum[i] += (double)partial[(int64_t)q * 2 * r.width + at + i];
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int64_t q = p + k < p1 ? p + k : p1 - 1;
+      id[k] = r.id[q];
+      tok[k] = r.tok[q];
+    }
+    Chunk<T> ch[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const T* px = dy + (int64_t)tok[k] * lddy + max(at, 0);
+      if (narrow) ch[k].v[0] = px[0];
+      else ch[k].load(px);
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (p + k >= p1) break;
+      if (id[k] != cur) {
+        flush(p + k);
+        cur = id[k];
+#pragma unroll
+        for (int i = 0; i < VE; ++i) sum[i] = 0.0;
+      }
+#pragma unroll
+      for (int i = 0; i < VE; ++i)
+        if (i == 0 || !narrow) sum[i] += (double)ch[k].v[i];
+    }
   }
-  write_row<TD>(dtable + v * ldt, at, narrow, sum, (double)scale);
+  flush(p1);
 }
 
-// Zeros in the rows of ids without tokens.
-template <typename TD>
-__global__ __launch_bounds__(kBlock) void absent_kernel(Runs r, TD* __restrict__ dtable, int64_t ldt) {
+// Sums of the runs that cross parts, 2^join_log2 chunks of a row at a time.  A
+// group of lanes looks at the part where such a run starts; of up to kAlone parts
+// it joins them itself, longer ones are joined by the whole workgroup, one after
+// the other.  Few columns to a workgroup: a run of hundreds of parts would take the
+// CU's whole bandwidth else (331,776 rows of 960 bytes for 2 ids: whole rows 56 us).
+constexpr int kJoinBlock = 1024, kAlone = 64;
+
+// Partial sums of parts first, first + step, ... up to last; the run starts in `part`.
+template <int VE, bool NARROW>
+__device__ __forceinline__ void add_parts(const Runs& r, const double* partial, int part, int first, int step, int last,
+                                          int at, double (&sum)[VE]) {
+  constexpr int U = NARROW ? 8 : 32 / VE, N = NARROW ? 1 : VE;
+  for (int64_t q = first; q <= last; q += U * step) {
+    double v[U][N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t w = min(q + u * step, (int64_t)last);
+      __builtin_memcpy(v[u], partial + (w * 2 + (w == part)) * r.width + at, N * sizeof(double));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (q + u * step <= last) sum[i] += v[u][i];
+  }
+}
+
+template <typename T, typename TD>
+__global__ __launch_bounds__(kJoinBlock) void join_kernel(Runs r, double scale, const double* __restrict__ partial,
+                                                          TD* __restrict__ dtable, int64_t ldt) {
+  constexpr int VE = Chunk<T>::kElems;
+  __shared__ double sums[kJoinBlock * VE];
+  __shared__ int list[kJoinBlock][3], listed;
+  const int lane = threadIdx.x & ((1 << r.join_log2) - 1), sub = threadIdx.x >> r.join_log2;
+  const int subs = kJoinBlock >> r.join_log2;
   const int64_t n = *r.kept;
-  const int lane = threadIdx.x & 63;
-  const int64_t waves = (int64_t)gridDim.x * (kBlock / 64);
-  for (int64_t v = (int64_t)blockIdx.x * (kBlock / 64) + threadIdx.x / 64; v < r.nid; v += waves) {
-    const int64_t at = behind(r.id, 0, n, (int)v);
-    if (at > 0 && r.id[at - 1] == v) continue;
-    for (int c = lane; c < r.width; c += 64) dtable[v * ldt + c] = (TD)0;
+  const bool narrow = r.width < VE;
+  if (threadIdx.x == 0) listed = 0;
+  __syncthreads();
+  auto add = [&](int part, int first, int step, int last, int at, double (&sum)[VE]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < VE; ++i) sum[i] = 0.0;
+    if (narrow) add_parts<VE, true>(r, partial, part, first, step, last, at, sum);
+    else add_parts<VE, false>(r, partial, part, first, step, last, at, sum);
+  };
+  // neighbouring groups take neighbouring parts of the same columns
+  const int64_t item = (int64_t)blockIdx.x * subs + sub;
+  const int slab = (int)(item / r.parts), part = (int)(item % r.parts);
+  const int at = slab < r.join_slabs ? chunk_at<T>(r, (slab << r.join_log2) + lane) : -1;
+  const int64_t p0 = (int64_t)part * r.part, p1 = p0 + r.part;
+  if (slab < r.join_slabs && p1 < n) {
+    const int v = r.id[p1 - 1];
+    if (r.id[p1] == v && (p0 == 0 || r.id[p0 - 1] != v)) {  // starts here and goes on
+      // part q belongs to the run if its first position does: last does, past does not
+      const int end = (int)((n + r.part - 1) / r.part);
+      const auto has = [&](int q) { return q < end && r.id[(int64_t)q * r.part] == v; };
+      int last = part + 1, past = part + 2;
+      while (has(past)) {
+        const int ahead = past - part;
+        last = past;
+        past = min(past + ahead, end);
+      }
+      while (past - last > 1) {
+        const int mid = last + (past - last) / 2;
+        if (has(mid)) last = mid;
+        else past = mid;
+      }
+      if (last - part >= kAlone) {
+        if (lane == 0) {
+          int* entry = list[atomicAdd(&listed, 1)];
+          entry[0] = sub;
+          entry[1] = last;
+          entry[2] = v;
+        }
+      } else if (at >= 0) {
+        double sum[VE];
+        add(part, part, 1, last, at, sum);
+        write_row<TD>(dtable + v * ldt, at, narrow, sum, scale);
+      }
+    }
+  }
+  __syncthreads();
+  for (int l = 0; l < listed; ++l) {
+    const int64_t it = (int64_t)blockIdx.x * subs + list[l][0];
+    const int first = (int)(it % r.parts), last = list[l][1];
+    const int at_it = chunk_at<T>(r, ((int)(it / r.parts) << r.join_log2) + lane);
+    double sum[VE];
+    if (at_it >= 0) add(first, first + sub, subs, last, at_it, sum);
+#pragma unroll
+    for (int i = 0; i < VE; ++i) sums[i * kJoinBlock + threadIdx.x] = at_it >= 0 ? sum[i] : 0.0;
+    for (int d = subs / 2; d; d >>= 1) {
+      __syncthreads();
+      if (sub < d)
+#pragma unroll
+        for (int i = 0; i < VE; ++i) sums[i * kJoinBlock + threadIdx.x] += sums[i * kJoinBlock + threadIdx.x + (d << r.join_log2)];
+    }
+    __syncthreads();
+    if (sub == 0 && at_it >= 0) {
+#pragma unroll
+      for (int i = 0; i < VE; ++i) sum[i] = sums[i * kJoinBlock + threadIdx.x];
+      write_row<TD>(dtable + list[l][2] * ldt, at_it, narrow, sum, scale);
+    }
+    __syncthreads();
   }
 }
 
@@ -244,6 +374,7 @@ Layout layout_for(dpc_elem elem, int ntok, int nid, int width) {
   l.lanes_log2 = log2_lanes(width, elem_size(elem));
   const int VE = (int)(16 / elem_size(elem)), nch = width < VE ? width : (width + VE - 1) / VE;
   l.slabs = (int)(((int64_t)nch + (1 << l.lanes_log2) - 1) >> l.lanes_log2);
+  // about 4,096 groups of lanes in all
   const int64_t part = ((int64_t)ntok * l.slabs + 4095) / 4096;
   l.part = (int)(part < 16 ? 16 : part > 1024 ? 1024 : part);
   l.parts = (int)(((int64_t)ntok + l.part - 1) / l.part);
@@ -259,7 +390,7 @@ Layout layout_for(dpc_elem elem, int ntok, int nid, int width) {
   }
   l.kept = take(4 * sizeof(int));
   l.sort = take(sort_workspace_bytes(ntok, 1 << l.passes.bits));
-  l.partial = take((size_t)l.parts * 2 * width * (elem == DPC_ELEM_F64 ? 8 : 4));
+  l.partial = take((size_t)l.parts * 2 * width * sizeof(double));
   l.bytes = at;
   return l;
 }
@@ -292,12 +423,15 @@ extern "C" int dpc_embed(void* stream, dpc_elem elem, int ntok, int nid, int wid
       !elem_aligned(table, elem_size(elem)) || !elem_aligned(y, elem_size(elem)))
     return DPC_EINVAL;
   (void)hipGetLastError();  // report only what this launch raises
+  const size_t es = elem_size(elem);
+  const int l = log2_lanes(width, es);
+  const int64_t per = (int64_t)(kBlock >> l) * kRowsAtOnce;
+  const bool once = (int64_t)ntok * width * (int64_t)es >= kOnceBytes && width * es % 16 == 0 && ldy * es % 16 == 0 &&
+                    elem_aligned(y, 16);
   by_elem(elem, [&](auto tt) {
     typedef decltype(tt) T;
-    const int l = log2_lanes(width, sizeof(T));
-    const int64_t per = kBlock >> l, blocks = (ntok + per - 1) / per, most = 1 << 20;
-    hipLaunchKernelGGL(embed_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(kBlock), 0,
-                       static_cast<hipStream_t>(stream), ntok, nid, width, l, ids, (const T*)table, ldt,
+    hipLaunchKernelGGL((once ? embed_kernel<T, true> : embed_kernel<T, false>), dim3((unsigned)((ntok + per - 1) / per)),
+                       dim3(kBlock), 0, static_cast<hipStream_t>(stream), ntok, nid, width, l, ids, (const T*)table, ldt,
                        (typename ElemAcc<T>::type)scale, (T*)y, ldy);
   });
   return dpc_internal_launch_status();
@@ -334,23 +468,23 @@ extern "C" int dpc_embed_bwd(void* stream, dpc_elem elem, dpc_elem elem_d, int n
     tok = job.to_tok;
     left = kept;
   }
-  const Runs r{id, tok, left, nid, width, l.part, l.parts, l.slabs, l.lanes_log2};
+  const int join_log2 = l.lanes_log2 < 3 ? l.lanes_log2 : 3;
+  const int64_t join_slabs = (int64_t)l.slabs << (l.lanes_log2 - join_log2);
+  const Runs r{id, tok, left, nid, width, l.part, l.parts, l.slabs, l.lanes_log2, (int)join_slabs, join_log2};
   const int64_t threads = ((int64_t)l.parts * l.slabs) << l.lanes_log2;
-  const dim3 grid((unsigned)((threads + kBlock - 1) / kBlock));
+  const unsigned run_blocks = (unsigned)((threads + kBlock - 1) / kBlock);
+  const unsigned absent_blocks = (unsigned)((nid + 255) / 256);
   by_elem(elem, [&](auto tt) {
     typedef decltype(tt) T;
-    typedef typename ElemAcc<T>::type A;
     const auto go = [&](auto dd) {
       typedef decltype(dd) TD;
-      if (ntok > 0) {
-        hipLaunchKernelGGL((runs_kernel<T, TD>), grid, dim3(kBlock), 0, s, r, (const T*)dy, lddy, (A)scale,
-                           (A*)(ws + l.partial), (TD*)dtable, lddt);
-        hipLaunchKernelGGL((join_kernel<T, TD>), grid, dim3(kBlock), 0, s, r, (A)scale, (const A*)(ws + l.partial),
-                           (TD*)dtable, lddt);
-      }
-      const int64_t blocks = ((int64_t)nid + 3) / 4, most = 1 << 20;
-      hipLaunchKernelGGL(absent_kernel<TD>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(kBlock), 0, s, r,
-                         (TD*)dtable, lddt);
+      double* partial = reinterpret_cast<double*>(ws + l.partial);
+      hipLaunchKernelGGL((l.lanes_log2 == 6 ? runs_kernel<T, TD, true> : runs_kernel<T, TD, false>),
+                         dim3(run_blocks + absent_blocks), dim3(kBlock), 0, s, r, run_blocks, (const T*)dy, lddy, scale,
+                         partial, (TD*)dtable, lddt);
+      if (l.parts > 1)
+        hipLaunchKernelGGL((join_kernel<T, TD>), dim3((unsigned)((threads + kJoinBlock - 1) / kJoinBlock)), dim3(kJoinBlock),
+                           0, s, r, scale, partial, (TD*)dtable, lddt);
     };
     if (elem_d == elem) go(T{});
     else go(float{});
