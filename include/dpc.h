@@ -472,6 +472,7 @@ int dpc_linear_i8(void* stream, dpc_elem elem_x, dpc_elem elem_y, int ntok, int 
  * From the scores of a token for each expert to the experts that it is sent to
  * and their weights: the inputs of dpc_route_plan and dpc_route_combine.
  *   s_e = exp(z_e) / sum exp(z), or 1 / (1 + exp(-z_e));  c_e = s_e + bias_e
+ * (with neither bias nor groups c_e = z_e: the order of the s_e, unrounded).
  * An expert with z_e = -infinity is closed: its s_e is 0, it is never chosen and
  * does not count in its group.  The experts stand in `groups` groups of equal
  * size; the value of a group is the sum of its `best` (1 or 2) largest c, and the
@@ -480,8 +481,8 @@ int dpc_linear_i8(void* stream, dpc_elem elem_x, dpc_elem elem_y, int ntok, int 
  * first.  Ties go to the lower group and the lower expert.  A bias of -infinity
  * closes its expert for all tokens (its s_e keeps its share).  The weights are
  *   w_j = scale * s_j,  or (renorm)  scale * s_j / sum_j s_j   (0 if the sum is 0)
- * s, c, groups' values and sums are float64, whatever the type of z, rounded
- * once to the weights' type: equal choices on every card and in every order.
+ * s, c, groups' values and sums are float64, whatever the type of z, and so is
+ * the choice; weights are rounded once to their type.
  * Slots without an open expert get expert -1 (which dpc_route_plan drops) and
  * weight 0.  A token with a NaN among its z or c (or, in a softmax, z = +infinity)
  * gets the experts 0 .. topk - 1 and weights NaN.                            */

@@ -23,8 +23,9 @@ def choose(z, topk, kind="softmax", bias=None, groups=1, keep=1, best=1, renorm=
     expert, weight = np.full((n, topk), -1), np.zeros((n, topk))
     per = E // groups
     for t in range(n):
-        c = s[t] + (0.0 if bias is None else np.asarray(bias, np.float64))
-        if np.isnan(c).any():
+        # with neither bias nor groups the order is that of the logits (whose scores may round to equal numbers)
+        c = z[t] if bias is None and groups == 1 else s[t] + (0.0 if bias is None else np.asarray(bias, np.float64))
+        if np.isnan(c + s[t]).any():
             expert[t], weight[t] = np.arange(topk), np.nan
             continue
         open_ = (z[t] != -np.inf) & (c != -np.inf)
