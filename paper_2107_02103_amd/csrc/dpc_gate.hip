@@ -27,43 +27,61 @@ constexpr int kBlock = 256;
 struct Gate {
   int ntok, nexpert, topk, sigmoid, groups, per, keep, best, renorm;
   double scale;
+  int lanes;      // lanes of a group, if a group is that many whole lanes (1, 2, 4, ...), else 0
+  float inverse;  // 1 / per
+  // e / per: (e + 1/2) / per is 1/2 / per or more from a whole number, a thousand
+  // times what float32 is off by.  (Experts that do not exist are given one, too.)
+  __device__ __forceinline__ int group_of(int e) const { return (int)(((float)e + 0.5f) * inverse) & 63; }
 };
 
 // ---------------------------------------------------------------------------
 // across lanes
 // ---------------------------------------------------------------------------
-// v of the lane that step M (1, 2, 4, .. 32) of a reduction pairs this one with:
-// all lanes of a group of M hold the same, so that any lane of the other group will do.
+// v of this lane and of the one that step M (1, 2, 4, .. 32) of a reduction pairs
+// it with, in any order: all lanes of a group of M hold the same, so that any lane
+// of the other group will do.
+struct Two {
+  unsigned a, b;
+};
 template <int M>
-__device__ __forceinline__ unsigned partner(unsigned v) {
-  if constexpr (M == 1) return __builtin_amdgcn_update_dpp(v, v, 0xb1, 0xf, 0xf, false);        // lanes 1 0 3 2
-  else if constexpr (M == 2) return __builtin_amdgcn_update_dpp(v, v, 0x4e, 0xf, 0xf, false);   // 2 3 0 1
-  else if constexpr (M == 4) return __builtin_amdgcn_update_dpp(v, v, 0x141, 0xf, 0xf, false);  // mirrored in 8
-  else if constexpr (M == 8) return __builtin_amdgcn_update_dpp(v, v, 0x140, 0xf, 0xf, false);  // mirrored in 16
-  else return (unsigned)__shfl_xor((int)v, M);
+__device__ __forceinline__ Two both(unsigned v) {
+  if constexpr (M == 1) return {v, (unsigned)__builtin_amdgcn_update_dpp(v, v, 0xb1, 0xf, 0xf, false)};        // lanes 1 0 3 2
+  else if constexpr (M == 2) return {v, (unsigned)__builtin_amdgcn_update_dpp(v, v, 0x4e, 0xf, 0xf, false)};   // 2 3 0 1
+  else if constexpr (M == 4) return {v, (unsigned)__builtin_amdgcn_update_dpp(v, v, 0x141, 0xf, 0xf, false)};  // mirrored in 8
+  else if constexpr (M == 8) return {v, (unsigned)__builtin_amdgcn_update_dpp(v, v, 0x140, 0xf, 0xf, false)};  // mirrored in 16
+  else if constexpr (M == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);  // rows 0 0 2 2 and 1 1 3 3
+    return {r[0], r[1]};
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);  // the halves
+    return {r[0], r[1]};
+  }
 }
 template <int M, typename V>
-__device__ __forceinline__ V partner_of(V v) {
-  if constexpr (sizeof(V) == 4) {
-    unsigned u;
-    __builtin_memcpy(&u, &v, 4);
-    u = partner<M>(u);
-    __builtin_memcpy(&v, &u, 4);
-  } else {
-    unsigned u[2];
-    __builtin_memcpy(u, &v, 8);
-    u[0] = partner<M>(u[0]);
-    u[1] = partner<M>(u[1]);
-    __builtin_memcpy(&v, u, 8);
+__device__ __forceinline__ void both_of(V v, V* x, V* y) {
+  unsigned u[sizeof(V) / 4], a[sizeof(V) / 4], b[sizeof(V) / 4];
+  __builtin_memcpy(u, &v, sizeof(V));
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(V) / 4); ++i) {
+    const Two t = both<M>(u[i]);
+    a[i] = t.a;
+    b[i] = t.b;
   }
-  return v;
+  __builtin_memcpy(x, a, sizeof(V));
+  __builtin_memcpy(y, b, sizeof(V));
 }
 // f over LANES lanes, for all of them.
 template <int LANES, int M = 1, typename V, typename F>
 __device__ __forceinline__ V across(V v, F f) {
-  if constexpr (M >= LANES) return v;
-  else return across<LANES, 2 * M>(f(v, partner_of<M>(v)), f);
+  if constexpr (M >= LANES) {
+    return v;
+  } else {
+    V a, b;
+    both_of<M>(v, &a, &b);
+    return across<LANES, 2 * M>(f(a, b), f);
+  }
 }
+
 // (numbers: a NaN gives way)
 struct Larger {
   __device__ __forceinline__ float operator()(float a, float b) const { return __builtin_fmaxf(a, b); }
@@ -111,7 +129,17 @@ __device__ __forceinline__ double exp64(double x) {
   for (int i = 0; i < 13; ++i) p = fma(p, r, c[i]);
   return ldexp(p, (int)n);
 }
-__device__ __forceinline__ double sigmoid64(double z) { return 1.0 / (1.0 + exp64(-z)); }
+// 1 / x of a normal x: the hardware's estimate (14 bits or more) and two steps of
+// Newton's, within an ulp.
+__device__ __forceinline__ double inverse64(double x) {
+  double r = __builtin_amdgcn_rcp(x);
+  r = fma(r, fma(-x, r, 1.0), r);
+  r = fma(r, fma(-x, r, 1.0), r);
+  return fma(r, fma(-x, r, 1.0), r);
+}
+__device__ __forceinline__ double sigmoid64(double z) {
+  return z < -700.0 ? exp64(z) : inverse64(1.0 + exp64(-z));  // below, 1 + exp(-z) is exp(-z)
+}
 
 // The same in float32 by the hardware's exponential and reciprocal.
 __device__ __forceinline__ float exp32(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
@@ -120,64 +148,90 @@ __device__ __forceinline__ float sigmoid32(float z) { return __builtin_amdgcn_rc
 // How far a float32 score may be from its exact value.  2^-24 is a rounding.
 // Sigmoid: the exponential is off by |z| + 2 roundings of itself (its argument's and
 // its own), which s (1 - s) makes 0.23 + 0.5 of an absolute one, and the sum and the
-// reciprocal add 3 of s.  Softmax: exponentials off by |z - top| + 2 roundings and
+// reciprocal add 3 of s: under 4 of them.  Softmax: exponentials off by |z - top| + 2 roundings and
 // a sum of up to 1,024 of them (16 in a lane, 6 steps across), which come to s (|z -
 // top| + sum s |z - top| + 28), and s |z - top| <= 0.37, s sum s |z - top| <= s ln
-// (1,024 / s) + .. <= 3: under 32 of them.  Both under 2^-19; c = s + bias adds one
-// rounding of c, a key without its last bits EPL 2^-23 of it: `most` is the largest
-// magnitude among the token's c.
+// (1,024 / s) + .. <= 3: under 32 of them.  Twice that is allowed for; c = s + bias
+// adds one rounding of c, and a key without its last bits EPL 2^-23 of it.
+__device__ __forceinline__ float score_off_by(bool sigmoid) { return sigmoid ? 0x1p-21f : 0x1p-18f; }
 template <int EPL>
-__device__ __forceinline__ float off_by(float most) { return 0x1p-19f + (EPL + 1) * 0x1p-23f * most; }
+__device__ __forceinline__ float off_by(bool sigmoid, float c) {
+  return score_off_by(sigmoid) + (EPL + 1) * 0x1p-23f * __builtin_fabsf(c);
+}
 
 // A key whose order as a whole number is the number's.
 __device__ __forceinline__ unsigned ordered(float v) {
   const unsigned u = __float_as_uint(v);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float number(unsigned key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
-// LDS of a wavefront: chosen experts [tokens][topk], then for groups values
-// [tokens][nexpert] and groups' values [tokens][groups], as doubles.
-__host__ __device__ constexpr size_t chosen_bytes(int tokens, int topk) { return ((size_t)tokens * topk * 4 + 15) / 16 * 16; }
-__host__ __device__ constexpr size_t wave_bytes(int tokens, const Gate& g) {
-  return chosen_bytes(tokens, g.topk) + (g.groups > 1 ? (size_t)tokens * (g.nexpert + g.groups) * 8 : 0);
+// LDS of a wavefront: chosen experts [tokens][topk], groups' values [tokens][groups]
+// as doubles, and, one after the other, values [tokens][nexpert] of groups that are
+// no whole lanes, as doubles, and keys [EPL][64].
+__host__ __device__ constexpr size_t chosen_bytes(int tokens, const Gate& g) { return ((size_t)tokens * g.topk * 4 + 15) / 16 * 16; }
+__host__ __device__ constexpr size_t group_bytes(int tokens, const Gate& g) {
+  return g.groups > 1 ? ((size_t)tokens * g.groups * 8 + 15) / 16 * 16 : 0;
+}
+__host__ __device__ constexpr size_t wave_bytes(int tokens, int epl, const Gate& g) {
+  const size_t keys = (size_t)epl * 256, values = g.groups > 1 && !g.lanes ? (size_t)tokens * g.nexpert * 8 : 0;
+  return chosen_bytes(tokens, g) + group_bytes(tokens, g) + ((keys > values ? keys : values) + 15) / 16 * 16;
 }
 
 // Which groups stay (bit by bit) of values c, -infinity where an expert cannot be
 // chosen; *near: two at the border are closer than what float32 can tell apart.
 template <int LANES, int EPL, typename V>
-__device__ __forceinline__ unsigned long long kept_groups(const Gate& g, const V (&c)[EPL], int lane, V* values, V off,
+__device__ __forceinline__ unsigned long long kept_groups(const Gate& g, const V (&c)[EPL], int lane, V* values, V* group,
                                                           bool* near) {
   const int e0 = lane * EPL;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i)
-    if (e0 + i < g.nexpert) values[e0 + i] = c[i];
-  wave_sync();
-  V* group = values + g.nexpert;
-  // as many lanes to a group as there are
-  int some = 1;
-  while (some * 2 * g.groups <= LANES) some *= 2;
-  const int part = lane & (some - 1);
-  for (int q = lane / some; q < g.groups; q += LANES / some) {
-    V first = -(V)INFINITY, second = -(V)INFINITY;
-    for (int i = part; i < g.per; i += some) {
-      const V v = values[q * g.per + i];
-      second = Larger()(second, Smaller()(v, first));
-      first = Larger()(first, v);
-    }
-    // (the lanes of a group are in this together; the two best of two pairs)
-    auto merge = [&](V of, V os) {
-      second = Larger()(Larger()(second, os), Smaller()(first, of));
-      first = Larger()(first, of);
+  V first, second, size = (V)0;  // the two best of a group; their magnitudes, largest of all groups
+  auto put = [&](int q) __attribute__((always_inline)) {
+    const bool two = g.best == 2 && second != -(V)INFINITY;
+    group[q] = two ? first + second : first;
+    if (first != -(V)INFINITY) size = Larger()(size, (V)(__builtin_fabs(first) + (two ? __builtin_fabs(second) : 0.0)));
+  };
+  auto take = [&](V v) __attribute__((always_inline)) {
+    second = Larger()(second, Smaller()(v, first));
+    first = Larger()(first, v);
+  };
+  // the two best of two pairs; all lanes of a group of `some` are here
+  auto merge = [&](int some) __attribute__((always_inline)) {
+    auto step = [&](auto m) __attribute__((always_inline)) {
+      V f[2], n[2];
+      both_of<decltype(m)::value>(first, f, f + 1);
+      both_of<decltype(m)::value>(second, n, n + 1);
+      second = Larger()(Larger()(n[0], n[1]), Smaller()(f[0], f[1]));
+      first = Larger()(f[0], f[1]);
     };
-    if constexpr (LANES > 1) { if (some > 1) merge(partner_of<1>(first), partner_of<1>(second)); }
-    if constexpr (LANES > 2) { if (some > 2) merge(partner_of<2>(first), partner_of<2>(second)); }
-    if constexpr (LANES > 4) { if (some > 4) merge(partner_of<4>(first), partner_of<4>(second)); }
-    if constexpr (LANES > 8) { if (some > 8) merge(partner_of<8>(first), partner_of<8>(second)); }
-    if constexpr (LANES > 16) { if (some > 16) merge(partner_of<16>(first), partner_of<16>(second)); }
-    if (part == 0) group[q] = g.best == 2 && second != -(V)INFINITY ? first + second : first;
+    if constexpr (LANES > 1) { if (some > 1) step(std::integral_constant<int, 1>{}); }
+    if constexpr (LANES > 2) { if (some > 2) step(std::integral_constant<int, 2>{}); }
+    if constexpr (LANES > 4) { if (some > 4) step(std::integral_constant<int, 4>{}); }
+    if constexpr (LANES > 8) { if (some > 8) step(std::integral_constant<int, 8>{}); }
+    if constexpr (LANES > 16) { if (some > 16) step(std::integral_constant<int, 16>{}); }
+  };
+  if (g.lanes) {  // a group is a whole number of lanes, 1, 2, 4, ...
+    first = second = -(V)INFINITY;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) take(c[i]);
+    merge(g.lanes);
+    if (!(lane & (g.lanes - 1)) && e0 < g.nexpert) put(g.group_of(e0));
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i)
+      if (e0 + i < g.nexpert) values[e0 + i] = c[i];
+    wave_sync();
+    // as many lanes to a group as there are
+    int some = 1;
+    while (some * 2 * g.groups <= LANES) some *= 2;
+    const int part = lane & (some - 1);
+    for (int q = lane / some; q < g.groups; q += LANES / some) {
+      first = second = -(V)INFINITY;
+      for (int i = part; i < g.per; i += some) take(values[q * g.per + i]);
+      merge(some);
+      if (part == 0) put(q);
+    }
   }
   wave_sync();
   unsigned long long kept = 0;
@@ -199,9 +253,36 @@ __device__ __forceinline__ unsigned long long kept_groups(const Gate& g, const V
   if constexpr (sizeof(V) == 4) {
     low = across<LANES>(low, Smaller());
     high = across<LANES>(high, Larger());
-    *near = high != -(V)INFINITY && !(low - high > 8 * off);
+    size = across<LANES>(size, Larger());
+    // a value is off by its terms' errors, a rounding of each and one of its own
+    *near = high != -(V)INFINITY && !(low - high > 4 * score_off_by(g.sigmoid) + 0x1p-21f * size);
   }
   return kept;
+}
+
+// -infinity for the experts of the groups that do not stay.
+template <int EPL, typename V>
+__device__ __forceinline__ void drop(const Gate& g, unsigned long long kept, int e0, V (&c)[EPL]) {
+  if (g.lanes) {
+    const bool stays = kept >> g.group_of(e0) & 1;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) c[i] = stays ? c[i] : -(V)INFINITY;
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i)
+      if (!(kept >> g.group_of(e0 + i) & 1)) c[i] = -(V)INFINITY;
+  }
+}
+
+// Whether float32 cannot tell the order of two neighbouring keys: equal but for the
+// last bits, or (plain: exact numbers) closer than their errors.
+template <int EPL>
+__device__ __forceinline__ bool close(bool plain, bool sigmoid, unsigned high, unsigned low) {
+  high &= ~(EPL - 1u);
+  low &= ~(EPL - 1u);
+  if (plain) return high == low;
+  const float a = number(high), b = number(low);
+  return !(a - b > off_by<EPL>(sigmoid, a) + off_by<EPL>(sigmoid, b));
 }
 
 // The order in float64, one expert after the other.
@@ -237,9 +318,13 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
   const int64_t t = (blockIdx.y * (int64_t)gridDim.x + blockIdx.x) * (kBlock / LANES) + threadIdx.x / LANES;
   const bool in = t < g.ntok;
   const int e0 = lane * EPL;
-  char* lds = gate_lds + (threadIdx.x >> 6) * wave_bytes(kTokens, g);
+  char* lds = gate_lds + (threadIdx.x >> 6) * wave_bytes(kTokens, EPL, g);
   int* chosen = reinterpret_cast<int*>(lds) + mine * g.topk;
-  double* values = reinterpret_cast<double*>(lds + chosen_bytes(kTokens, g.topk)) + (size_t)mine * (g.nexpert + g.groups);
+  lds += chosen_bytes(kTokens, g);
+  double* group = reinterpret_cast<double*>(lds) + mine * g.groups;
+  lds += group_bytes(kTokens, g);
+  unsigned* keys = reinterpret_cast<unsigned*>(lds);
+  double* values = reinterpret_cast<double*>(lds) + mine * g.nexpert;
   const T* pz = logits + (in ? t : 0) * ldl;
   // with neither bias nor groups the order is that of the logits
   const bool plain = !bias && g.groups == 1;
@@ -253,36 +338,42 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
       Chunk<T> ch;
       ch.load(pz + e0 + i);
 #pragma unroll
-      for (int k = 0; k < VE && i + k < EPL; ++k) z[i + k] = in ? (A)ch.v[k] : -(A)INFINITY;
+      for (int k = 0; k < VE && i + k < EPL; ++k) z[i + k] = (A)ch.v[k];
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) z[i] = in && e0 + i < g.nexpert ? (A)pz[e0 + i] : -(A)INFINITY;
+    for (int i = 0; i < EPL; ++i) z[i] = e0 + i < g.nexpert ? (A)pz[e0 + i] : -(A)INFINITY;
   }
+  if (!bias) {
 #pragma unroll
-  for (int i = 0; i < EPL; ++i) b[i] = bias && e0 + i < g.nexpert ? bias[e0 + i] : 0.0f;
+    for (int i = 0; i < EPL; ++i) b[i] = 0.0f;
+  } else if (e0 + EPL <= g.nexpert) {
+    __builtin_memcpy(b, bias + e0, sizeof(b));
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) b[i] = e0 + i < g.nexpert ? bias[e0 + i] : 0.0f;
+  }
 
-  // A NaN, or in a softmax +infinity: no order.  The sum of a finite number's
-  // difference to itself is 0.
-  int bad = 0;
-  A top = -(A)INFINITY;
+  // A NaN, or in a softmax +infinity: no order.
+  bool bad = false;
 #pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    bad |= z[i] != z[i] || b[i] != b[i] || (!g.sigmoid && z[i] == (A)INFINITY);
-    top = Larger()(top, z[i]);
-  }
-  bad = across<LANES>(bad, Or());
+  for (int i = 0; i < EPL; ++i) bad |= __builtin_isunordered((float)z[i], b[i]);
+  A top = (A)0;
   if (!g.sigmoid) {
+    top = z[0];
+#pragma unroll
+    for (int i = 1; i < EPL; ++i) top = Larger()(top, z[i]);
     top = across<LANES>(top, Larger());
+    bad |= top == (A)INFINITY;
     if (top == -(A)INFINITY) top = (A)0;
   }
+  if (__any(bad)) bad = across<LANES>((int)bad, Or());
 
   bool unsure = sizeof(T) == 8;
   if constexpr (sizeof(T) != 8) {
-    // keys: 0 for what cannot be chosen
-    unsigned key[EPL];
+    unsigned key[EPL];  // 0 for what cannot be chosen
     constexpr unsigned kLow = EPL - 1;  // a key's last bits say which expert of the lane it is
-    float c[EPL], off = 0.0f;
+    float c[EPL];
     if (!plain) {
       if (g.sigmoid) {
 #pragma unroll
@@ -300,18 +391,13 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
         for (int i = 0; i < EPL; ++i) c[i] *= inverse;
       }
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) {
-        c[i] = z[i] == -INFINITY ? -INFINITY : c[i] + b[i];
-        if (c[i] != -INFINITY) off = Larger()(off, __builtin_fabsf(c[i]));
-      }
-      off = off_by<EPL>(across<LANES>(off, Larger()));
+      for (int i = 0; i < EPL; ++i) c[i] = z[i] == -INFINITY ? -INFINITY : c[i] + b[i];
       if (g.groups > 1) {
         bool near = false;
-        const unsigned long long kept = kept_groups<LANES>(g, c, lane, reinterpret_cast<float*>(values), off, &near);
+        const unsigned long long kept = kept_groups<LANES>(g, c, lane, reinterpret_cast<float*>(values),
+                                                                    reinterpret_cast<float*>(group), &near);
         unsure = near;
-#pragma unroll
-        for (int i = 0; i < EPL; ++i)
-          if (!(kept >> (min(e0 + i, g.nexpert - 1) / g.per) & 1)) c[i] = -INFINITY;
+        drop(g, kept, e0, c);
       }
     } else {
 #pragma unroll
@@ -322,13 +408,12 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
     if (whole) {
 #pragma unroll
       for (int i = 0; i < EPL; ++i) {
-        unsigned u;
+        unsigned u = 0;
         if constexpr (sizeof(T) == 2) {
-          const T v = (T)z[i];
+          const T v = (T)c[i];
           unsigned short h;
           __builtin_memcpy(&h, &v, 2);
-          // +0 and -0 are equal
-          u = h == 0x8000u ? 0x8000u : h & 0x8000u ? (unsigned)(unsigned short)~h : h | 0x8000u;
+          u = h & 0x8000u ? (unsigned)(unsigned short)~h : h | 0x8000u;
         }
         key[i] = c[i] == -INFINITY ? 0u : u << 16 | (0xffffu - (unsigned)(e0 + i));
       }
@@ -351,43 +436,49 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
               key[i + j] = max(x, y);
               key[i + j + k] = min(x, y);
             }
-    // the largest of all heads is the next: its lane goes on to its next key
-    unsigned before = 0;
-    for (int j = 0; j <= g.topk; ++j) {
-      const unsigned best = across<LANES>(key[0], Larger());
-      if (!whole && j > 0) {
-        // neighbours: equal but for the last bits, or closer than their errors
-        const unsigned a = before & ~kLow, d = best & ~kLow;
-        unsure |= best != 0 && (plain ? a == d : !(number(a) - number(d) > 4 * off));
-      }
-      if (j == g.topk) break;
-      const bool hit = key[0] == best && best != 0;
-      if (!whole && LANES > 1) {  // equal ones in two lanes
-        const unsigned long long hits = __ballot(hit) >> (mine * LANES) & (~0ull >> (64 - LANES));
-        unsure |= (hits & (hits - 1)) != 0;
-      }
-      if (hit) {
-        chosen[j] = whole ? (int)(0xffffu - (best & 0xffffu)) : e0 + (int)(kLow - (best & kLow));
+    // they wait in LDS: key j of this lane in place j * 64 + lane, 0 behind the last
+    unsigned* mykeys = keys + (threadIdx.x & 63);
 #pragma unroll
-        for (int i = 0; i + 1 < EPL; ++i) key[i] = key[i + 1];
-        key[EPL - 1] = 0u;
-      } else if (best == 0 && lane == 0) {
-        chosen[j] = -1;
+    for (int i = 1; i < EPL; ++i) mykeys[(i - 1) * 64] = key[i];
+    mykeys[(EPL - 1) * 64] = 0u;
+    // The largest of all heads is the next: its lane goes on to its next key.  Lane
+    // j keeps the j-th for what follows, if there are as many.
+    const bool few = g.topk < LANES;
+    unsigned head = key[0], before = 0, kept = 0;
+    int taken = 0, rounds = 0;
+    for (int j = 0; j <= g.topk; ++j) {
+      const unsigned best = across<LANES>(head, Larger());
+      if (few) kept = lane == j ? best : kept;
+      else if (!whole && j > 0) unsure |= best != 0 && close<EPL>(plain, g.sigmoid, before, best);
+      if (j == g.topk) break;
+      if (head == best) {
+        chosen[j] = best == 0 ? -1 : whole ? (int)(0xffffu - (best & 0xffffu)) : e0 + (int)(kLow - (best & kLow));
+        head = mykeys[min(taken, EPL - 1) * 64];
+        taken += best != 0;
       }
+      rounds += best != 0;
       before = best;
+    }
+    if (!whole) {
+      if (few && LANES > 1) {
+        const unsigned next = (unsigned)__shfl_down((int)kept, 1);
+        unsure |= lane < g.topk && next != 0 && close<EPL>(plain, g.sigmoid, kept, next);
+      }
+      // equal ones in two lanes were taken at once
+      if (LANES > 1) unsure |= across<LANES>(taken, Sum()) != rounds;
     }
   }
 
   // Exactly, where that did not settle it.
   const bool all = !g.sigmoid && !g.renorm;  // the sum of all exponentials counts
-  double sum = 1.0;
+  double inverse = 1.0;
   const bool again = __any(unsure && in && !bad);
   if (all || (again && !plain && !g.sigmoid)) {
-    sum = 0.0;
+    double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) sum += exp64((double)z[i] - (double)top);
     sum = across<LANES>(sum, Sum());
-    if (sum == 0.0) sum = 1.0;
+    inverse = sum == 0.0 ? 0.0 : 1.0 / sum;
   }
   if (again) {
     double c[EPL];
@@ -395,37 +486,35 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
     for (int i = 0; i < EPL; ++i) {
       c[i] = (double)z[i];
       if (!plain && z[i] != -(A)INFINITY)
-        c[i] = (g.sigmoid ? sigmoid64((double)z[i]) : exp64((double)z[i] - (double)top) / sum) + (double)b[i];
+        c[i] = (g.sigmoid ? sigmoid64((double)z[i]) : exp64((double)z[i] - (double)top) * inverse) + (double)b[i];
     }
     wave_sync();
     if (g.groups > 1) {
-      const unsigned long long kept = kept_groups<LANES>(g, c, lane, values, 0.0, nullptr);
-#pragma unroll
-      for (int i = 0; i < EPL; ++i)
-        if (!(kept >> (min(e0 + i, g.nexpert - 1) / g.per) & 1)) c[i] = -INFINITY;
+      const unsigned long long kept = kept_groups<LANES>(g, c, lane, values, group, nullptr);
+      drop(g, kept, e0, c);
     }
     choose64<LANES>(g, c, lane, chosen);
   }
   wave_sync();
 
-  // weights of the chosen, a slot to a lane
-  double total = 0.0;
-  for (int j = lane; j < g.topk; j += LANES) {
-    const int e = chosen[j];
-    if (e >= 0 && !bad && in) total += g.sigmoid ? sigmoid64((double)pz[e]) : exp64((double)pz[e] - (double)top) / sum;
-  }
+  // weights of the chosen, a slot to a lane (and further ones if there are more)
+  auto score = [&](int e) __attribute__((always_inline)) {
+    if (bad || !in || e < 0) return 0.0;
+    const double v = (double)pz[e];
+    return g.sigmoid ? sigmoid64(v) : exp64(v - (double)top) * inverse;
+  };
+  const int e1 = lane < g.topk ? chosen[lane] : -1;
+  const double s1 = score(e1);
+  double total = s1;
+  for (int j = lane + LANES; j < g.topk; j += LANES) total += score(chosen[j]);
   total = across<LANES>(total, Sum());
   for (int j = lane; in && j < g.topk; j += LANES) {
-    const int e = bad ? j : chosen[j];
-    double w = 0.0;
-    if (bad) {
-      w = NAN;
-    } else if (e >= 0) {
-      const double s = g.sigmoid ? sigmoid64((double)pz[e]) : exp64((double)pz[e] - (double)top) / sum;
-      w = g.scale * (g.renorm ? total > 0.0 ? s / total : 0.0 : s);
-    }
-    expert[t * g.topk + j] = e;
-    weight[t * g.topk + j] = (A)w;
+    const int e = j == lane ? e1 : chosen[j];
+    double w = j == lane ? s1 : score(e);
+    if (g.renorm && total > 0.0) w = w / total;
+    w *= g.scale;
+    expert[t * g.topk + j] = bad ? j : e;
+    weight[t * g.topk + j] = (A)(bad ? (double)NAN : w);
   }
 }
 
@@ -521,18 +610,21 @@ dim3 grid_for(int ntok, int per) {
   return blocks <= wide ? dim3((unsigned)blocks) : dim3((unsigned)wide, (unsigned)((blocks + wide - 1) / wide));
 }
 
-// Calls f<LANES, EPL> for the number of experts.
-template <typename F>
+// Calls f<LANES, EPL> for the number of experts; EPL is 16 from 9 experts on, or 8.
+template <int MOST, typename F>
 void by_width(int nexpert, F f) {
-  if (nexpert <= 4) f(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
-  else if (nexpert <= 8) f(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
-  else if (nexpert <= 16) f(std::integral_constant<int, 2>{}, std::integral_constant<int, 8>{});
-  else if (nexpert <= 32) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{});
-  else if (nexpert <= 64) f(std::integral_constant<int, 8>{}, std::integral_constant<int, 8>{});
-  else if (nexpert <= 128) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 8>{});
-  else if (nexpert <= 256) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 8>{});
-  else if (nexpert <= 512) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 8>{});
-  else f(std::integral_constant<int, 64>{}, std::integral_constant<int, 16>{});
+  const auto go = [&](auto lanes, auto epl) { f(lanes, epl); };
+  if (nexpert <= 4) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+  if (nexpert <= 8) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+  const std::integral_constant<int, MOST> epl;
+  const int lanes = (nexpert + MOST - 1) / MOST;
+  if (lanes <= 1) go(std::integral_constant<int, 1>{}, epl);
+  else if (lanes <= 2) go(std::integral_constant<int, 2>{}, epl);
+  else if (lanes <= 4) go(std::integral_constant<int, 4>{}, epl);
+  else if (lanes <= 8) go(std::integral_constant<int, 8>{}, epl);
+  else if (lanes <= 16) go(std::integral_constant<int, 16>{}, epl);
+  else if (lanes <= 32) go(std::integral_constant<int, 32>{}, epl);
+  else go(std::integral_constant<int, 64>{}, std::integral_constant<int, 16>{});
 }
 
 template <typename F>
@@ -557,7 +649,7 @@ int gate_args(dpc_elem elem, const dpc_gate_spec* s, int ntok, Gate* g) {
     return DPC_ENOTSUP;
   if (s->nexpert % s->groups || s->topk > s->keep * (s->nexpert / s->groups)) return DPC_EINVAL;
   *g = Gate{ntok, s->nexpert, s->topk, s->score == DPC_SCORE_SIGMOID, s->groups, s->nexpert / s->groups, s->keep, s->best,
-            s->renorm != 0, s->scale};
+            s->renorm != 0, s->scale, 0, 1.0f / (float)(s->nexpert / s->groups)};
   return DPC_OK;
 }
 
@@ -575,11 +667,14 @@ extern "C" int dpc_gate(void* stream, dpc_elem elem, const dpc_gate_spec* spec, 
     return DPC_EINVAL;
   return by_type(elem, [&](auto tt) {
     typedef decltype(tt) T;
-    by_width(g.nexpert, [&](auto l, auto e) {
+    by_width<16>(g.nexpert, [&](auto l, auto e) {
       constexpr int LANES = decltype(l)::value, EPL = decltype(e)::value, TOKENS = kBlock / LANES;
-      const size_t lds = wave_bytes(64 / LANES, g) * (kBlock / 64);
+      Gate with = g;
+      const int lanes = g.per / EPL;
+      with.lanes = g.per % EPL == 0 && lanes <= LANES && (lanes & (lanes - 1)) == 0 ? lanes : 0;
+      const size_t lds = wave_bytes(64 / LANES, EPL, with) * (kBlock / 64);
       hipLaunchKernelGGL((gate_kernel<T, LANES, EPL>), grid_for(ntok, TOKENS), dim3(kBlock), lds,
-                         static_cast<hipStream_t>(stream), g, (const T*)logits, ldl, bias, expert,
+                         static_cast<hipStream_t>(stream), with, (const T*)logits, ldl, bias, expert,
                          (typename ElemAcc<T>::type*)weight);
     });
   });
@@ -598,7 +693,7 @@ extern "C" int dpc_gate_bwd(void* stream, dpc_elem elem, const dpc_gate_spec* sp
     return DPC_EINVAL;
   return by_type(elem, [&](auto tt) {
     typedef decltype(tt) T;
-    by_width(g.nexpert, [&](auto l, auto e) {
+    by_width<8>(g.nexpert, [&](auto l, auto e) {
       constexpr int LANES = decltype(l)::value, EPL = decltype(e)::value, TOKENS = kBlock / LANES;
       hipLaunchKernelGGL((gate_bwd_kernel<T, LANES, EPL>), grid_for(ntok, TOKENS), dim3(kBlock), 0,
                          static_cast<hipStream_t>(stream), g, (const T*)logits, ldl, expert,

@@ -101,6 +101,36 @@ def test_gradient(t, n, E, k):
         assert (np.abs(got - want) <= bound).all(), (kind, renorm, np.abs(got - want).max())
 
 
+@pytest.mark.parametrize("E,k,groups,keep,best", [(3, 2, 1, 1, 1), (12, 4, 4, 2, 2), (40, 6, 1, 1, 1), (100, 8, 10, 3, 2),
+                                                  (256, 8, 8, 4, 2), (256, 40, 1, 1, 1), (1000, 8, 8, 3, 1)])
+def test_scores_that_float32_cannot_tell_apart(E, k, groups, keep, best):
+    """Scores a few units of float32's last place apart: 2^-24 of 1 makes 2^-26 of a score, 10^7 roundings of float64."""
+    import paper_2107_02103_amd as P
+    rng = np.random.default_rng(E + k)
+    n = 200
+    z = (1.0 + 2.0 ** -23 * rng.integers(0, 40, (n, E))).astype(np.float32)
+    z[1::3] += (rng.integers(-2, 2, (len(z[1::3]), E)) * 0.25).astype(np.float32)
+    bias = (rng.integers(0, 3, E) * 2.0 ** -20).astype(np.float32)
+    for kind, b in (("sigmoid", bias), ("softmax", bias), ("sigmoid", None), ("softmax", None)):
+        e, w = P.Gate(E, k, kind, groups, keep, best, None if b is None else torch.from_numpy(b).cuda(), True)(
+            torch.from_numpy(z).cuda())
+        we, ww = og.choose(z, k, kind, b, groups, keep, best, True)
+        np.testing.assert_array_equal(e.cpu().numpy(), we)
+        _check_weights(w, ww, E, "f32")
+
+
+def test_equal_scores_of_every_expert():
+    """As a gate of zeros gives them: the lowest experts (of the lowest groups)."""
+    import paper_2107_02103_amd as P
+    for E, k, groups, keep in ((3, 2, 1, 1), (64, 8, 8, 2), (256, 8, 1, 1), (700, 64, 7, 3)):
+        z = torch.full((37, E), -0.0, device="cuda")
+        z[:, ::2] = 0.0
+        for t in (torch.float32, torch.bfloat16, torch.float64):
+            for kind in ("softmax", "sigmoid"):
+                e, w = P.Gate(E, k, kind, groups, keep, 2, renormalise=True)(z.to(t))
+                assert (e.cpu() == torch.arange(k)).all() and (w * k - 1).abs().max() < 1e-6
+
+
 def test_rows_with_nan_and_infinity():
     import paper_2107_02103_amd as P
     for E, k in ((3, 2), (20, 4), (200, 8)):
