@@ -65,6 +65,14 @@ __device__ __forceinline__ unsigned codes_of(const float (&v)[8], float scale) {
   return scale > 0.0f ? q : 0u;
 }
 
+// The scale byte of the block of these 4 lanes, and the scale as a number.
+__device__ __forceinline__ unsigned code_step(const float (&v)[8], float* factor) {
+  float a = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a = larger(a, __builtin_fabsf(v[i]));
+  return scale_byte(block_max(a), factor);
+}
+
 // 8 elements of a row of `ncols` from column c on, zeros past its end.
 template <typename T>
 __device__ __forceinline__ void take8(const T* px, int c, int ncols, float (&v)[8]) {
@@ -108,11 +116,8 @@ __global__ __launch_bounds__(kBlock) void quant_kernel(int64_t nrows_all, int nr
 #pragma unroll
   for (int k = 0; k < kQuantSteps; ++k) {
     if (s0 + k >= steps) break;
-    float a = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a = larger(a, __builtin_fabsf(v[k][i]));
     float factor;
-    const unsigned e = scale_byte(block_max(a), &factor);
+    const unsigned e = code_step(v[k], &factor);
     *reinterpret_cast<unsigned*>(q + (r * steps + s0 + k) * 128 + lane * 4) = codes_of(v[k], factor);
     if ((lane & 3) == 0) scale[((group * steps + s0 + k) * nrows + row) * 8 + (lane >> 2)] = (uint8_t)e;
   }
@@ -205,6 +210,8 @@ inline int64_t most_tiles(const Product& p, int size) {
   return t < p.m ? t : p.m;
 }
 
+inline bool few_rows(const Product& p) { return i8_few_rows(p.m, p.n, p.ngroup, p.offsets != nullptr); }
+
 // One product of 16 rows of W and 16 rows of x, 128 columns: codes a and b of this
 // lane's block, whose scale is byte K of sa and sb.
 template <int K>
@@ -220,37 +227,121 @@ __device__ __forceinline__ TY result(float sum, float bias) {
   return (TY)f;
 }
 
-// 16 rows times 16 channels of y for each wavefront.
-template <typename TY>
-__global__ __launch_bounds__(256) void product_kernel(Product p, TY* __restrict__ y, int64_t ldy) {
+// Few rows: 16 rows times 16 channels of y for each `share` wavefronts of a
+// workgroup of 8, which take the steps of K in turn and whose sums are added in
+// LDS, in order.  W is read once for each 16 rows of an expert, up to 8 KiB of it
+// under way in every wavefront: bound by that read, or for short rows by latency.
+// TX is the type of rows that the workgroup codes itself (into LDS), or uint8_t for
+// rows that are codes already.
+constexpr int kFewWaves = 8, kFewAhead = 4;
+
+template <typename TX, typename TY>
+__global__ __launch_bounds__(64 * kFewWaves) void few_product_kernel(Product p, int share, const TX* __restrict__ x,
+                                                                     int64_t ldx, TY* __restrict__ y, int64_t ldy) {
+  constexpr bool kCoded = sizeof(TX) == 1;
+  extern __shared__ __attribute__((aligned(16))) uint8_t codes[];  // codes made here [rows][steps][128], then scales [steps][rows][8]
+  __shared__ float sums[kFewWaves][256];
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Tile t = find_tile(p, 16, blockIdx.y + gridDim.y * blockIdx.z);
-  const int c0 = (blockIdx.x * 4 + wave) * 16;
-  if (t.row0 >= t.end || c0 >= p.n) return;
-  const int group = max(t.group, 0), r = t.row0 + l16;
-  const int tok = t.group < 0 ? -1 : token_of(p, min(r, t.end - 1)), tk = max(tok, 0), ch = min(c0 + l16, p.n - 1);
-  const uint8_t* pw = p.qw + ((int64_t)group * p.n + ch) * p.steps * 128 + quad * 32;
-  const uint8_t* px = p.qx + (int64_t)tk * p.steps * 128 + quad * 32;
-  const uint8_t* psw = p.sw + ((int64_t)group * p.steps * p.n + ch) * 8 + quad * 2;
-  const uint8_t* psx = p.sx + (int64_t)tk * 8 + quad * 2;
-  v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < p.steps; ++s) {
-    const v4i* w = reinterpret_cast<const v4i*>(pw + (int64_t)s * 128);
-    const v4i* x = reinterpret_cast<const v4i*>(px + (int64_t)s * 128);
-    const int sw = *reinterpret_cast<const uint16_t*>(psw + (int64_t)s * p.n * 8);
-    const int sx = *reinterpret_cast<const uint16_t*>(psx + (int64_t)s * p.ntok * 8);
-    acc = mfma4<0>(w[0], x[0], acc, sw, sx);
-    acc = mfma4<1>(w[1], x[1], acc, sw, sx);
+  if (t.row0 >= t.end) return;
+  const int tiles = kFewWaves / share;  // channel tiles of the workgroup
+  const int c0 = (blockIdx.x * tiles + wave / share) * 16, part = wave % share;
+  const int steps = p.steps, group = max(t.group, 0), high = t.end - t.row0;
+  // Codes: 4 lanes to 64 bytes of a row, moved to the lanes of a product by to_rows;
+  // in the first load of a step the even chunks, in the second the odd ones.
+  const uint8_t* pw = p.qw + ((int64_t)group * p.n + min(c0 + (lane >> 2), p.n - 1)) * steps * 128 + (lane & 3) * 32;
+  const uint8_t* psw = p.sw + ((int64_t)group * steps * p.n + min(c0 + l16, p.n - 1)) * 8 + quad * 2;
+  auto token = [&](int r) __attribute__((always_inline)) { return t.group < 0 ? -1 : token_of(p, min(t.row0 + r, t.end - 1)); };
+  const uint8_t *pq = nullptr, *psq = nullptr;
+  if (kCoded) {
+    pq = (const uint8_t*)x + (int64_t)max(token(lane >> 2), 0) * steps * 128 + (lane & 3) * 32;
+    psq = p.sx + (int64_t)max(token(l16), 0) * 8 + quad * 2;
   }
-  if (r >= t.end) return;
+  v4i w[kFewAhead][2], q[kFewAhead][2];
+  int ew[kFewAhead], eq[kFewAhead];
+  auto fetch = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = c0 + quad * 4 + i;
-    if (c >= p.n) break;
-    const float bias = p.bias ? p.bias[(int64_t)group * p.n + c] : 0.0f;
-    y[(int64_t)r * ldy + c] = tok < 0 ? (TY)0 : result<TY>(acc[i], bias);
+    for (int u = 0; u < kFewAhead; ++u) {
+      const int s = min(s0 + u * share, steps - 1);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        w[u][k] = *reinterpret_cast<const v4i*>(pw + s * 128 + k * 16);
+        if (kCoded) q[u][k] = *reinterpret_cast<const v4i*>(pq + s * 128 + k * 16);
+      }
+      ew[u] = *reinterpret_cast<const uint16_t*>(psw + (int64_t)s * p.n * 8);
+      if (kCoded) eq[u] = *reinterpret_cast<const uint16_t*>(psq + (int64_t)s * p.ntok * 8);
+    }
+  };
+  fetch(part);
+  const int held = min(high, 16);
+  const uint8_t* scales = codes + held * steps * 128;
+  if constexpr (!kCoded) {
+    // 32 lanes to a step of a row, as in quant_kernel
+    const int l32 = threadIdx.x & 31, chunk = l32 >> 2;
+    int row = 0, s = threadIdx.x >> 5;
+    for (;; s += 64 * kFewWaves / 32) {
+      for (; s >= steps && row < held; ++row) s -= steps;
+      if (row >= held) break;
+      float v[8], factor;
+      take8(x + (int64_t)max(token(row), 0) * ldx, s * 256 + l32 * 8, p.k, v);
+      const unsigned e = code_step(v, &factor);
+      *reinterpret_cast<unsigned*>(codes + (row * steps + s) * 128 + ((chunk ^ (row & 7)) << 4) + (l32 & 3) * 4) = codes_of(v, factor);
+      if ((l32 & 3) == 0) codes[held * steps * 128 + (s * held + row) * 8 + chunk] = (uint8_t)e;
+    }
+    __syncthreads();
   }
+  const int mine = min(l16, held - 1);  // rows of the tile past its end repeat its last one
+  v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s0 = part; s0 < steps; s0 += share * kFewAhead) {
+#pragma unroll
+    for (int u = 0; u < kFewAhead; ++u) {
+      const int s = s0 + u * share;
+      if (s >= steps) break;
+      v4i b[2];
+      int e;
+      if constexpr (kCoded) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) b[k] = to_rows(q[u][k]);
+        e = eq[u];
+      } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          b[k] = *reinterpret_cast<const v4i*>(codes + (mine * steps + s) * 128 + (((quad * 2 + k) ^ (mine & 7)) << 4));
+        e = *reinterpret_cast<const uint16_t*>(scales + (s * held + mine) * 8 + quad * 2);
+      }
+      acc = mfma4<0>(to_rows(w[u][0]), b[0], acc, ew[u], e);
+      acc = mfma4<1>(to_rows(w[u][1]), b[1], acc, ew[u], e);
+    }
+    if (s0 + share * kFewAhead < steps) fetch(s0 + share * kFewAhead);
+  }
+  // this lane: row l16, channels 4 quad .. 4 quad + 3
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sums[wave][l16 * 16 + quad * 4 + i] = acc[i];
+  __syncthreads();
+  for (int e = threadIdx.x; e < tiles * 256; e += 64 * kFewWaves) {
+    const int tile = e >> 8, row = e >> 4 & 15, c = (blockIdx.x * tiles + tile) * 16 + (e & 15), r = t.row0 + row;
+    if (r >= t.end || c >= p.n) continue;
+    float sum = 0.0f;
+    for (int v = 0; v < share; ++v) sum += sums[tile * share + v][e & 255];
+    y[(int64_t)r * ldy + c] = token(row) < 0 ? (TY)0 : result<TY>(sum, p.bias ? p.bias[(int64_t)group * p.n + c] : 0.0f);
+  }
+}
+
+// LDS of rows that the workgroup codes.
+inline size_t few_bytes(const Product& p) { return (size_t)(p.m < 16 ? p.m : 16) * p.steps * 136; }
+
+template <typename TX, typename TY>
+void launch_few(hipStream_t s, const Product& p, const TX* x, int64_t ldx, TY* y, int64_t ldy) {
+  const int64_t tiles = most_tiles(p, 16);
+  const unsigned gy = (unsigned)(tiles < 32768 ? tiles : 32768);
+  // wavefronts that share a tile: about 16 in all for each of 256 CUs
+  const int64_t wide = (p.n + 15) / 16;
+  int share = kFewWaves;
+  while (share > 1 && wide * tiles * share > 4096) share /= 2;
+  hipLaunchKernelGGL((few_product_kernel<TX, TY>),
+                     dim3((unsigned)((wide * share + kFewWaves - 1) / kFewWaves), gy, (unsigned)((tiles + gy - 1) / gy)),
+                     dim3(64 * kFewWaves), sizeof(TX) == 1 ? 0 : few_bytes(p), s, p, share, x, ldx, y, ldy);
 }
 
 // Tiles of BM rows times BN channels, K in steps of 256 columns: codes and scales
@@ -439,13 +530,7 @@ void launch_tiled(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
 
 template <typename TY>
 void launch_product(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
-  if (i8_few_rows(p.m, p.n, p.ngroup, p.offsets != nullptr)) {
-    const int64_t tiles = most_tiles(p, 16);
-    const unsigned gy = (unsigned)(tiles < 32768 ? tiles : 32768);
-    hipLaunchKernelGGL(product_kernel<TY>, dim3((unsigned)((p.n + 63) / 64), gy, (unsigned)((tiles + gy - 1) / gy)), dim3(256),
-                       0, s, p, y, ldy);
-    return;
-  }
+  if (few_rows(p)) return launch_few(s, p, p.qx, 0, y, ldy);
   switch (i8_tile(p.m, p.n, p.steps * 128, p.ngroup, p.offsets != nullptr)) {
     case 0: return launch_tiled<TY, 256, 256, 2, 4>(s, p, y, ldy);
     case 1: return launch_tiled<TY, 128, 128, 2, 2>(s, p, y, ldy);
@@ -457,6 +542,13 @@ void launch_product(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
 int product(hipStream_t s, dpc_elem elem_y, const Product& p, void* y, int64_t ldy) {
   return by_elem(elem_y, [&](auto t) { launch_product(s, p, (decltype(t)*)y, ldy); });
 }
+
+// Whether every workgroup codes the rows again, all of them up to 16,384 elements
+// (in steps of 256), which costs less than a launch.  Device times, us, one kernel
+// and two: 1 row of 1,600 float32 to 240 channels 3.7 and 5.9, 8 rows 4.8 and 6.1, 16
+// rows 6.4 and 6.3; 1 bfloat16 row of 4,096 to 4,096 4.2 and 6.5, 4 rows 5.4 and 6.8, 16
+// rows 10.2 and 6.9.
+inline bool coded_inside(const Product& p) { return few_rows(p) && (int64_t)p.m * p.steps <= 64; }
 
 int product_args(dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup) {
   if (!elem_ok(elem_y) || ntok < 0 || topk < 1 || n < 1 || k < 1 || ngroup < 1) return DPC_EINVAL;
@@ -542,6 +634,11 @@ extern "C" int dpc_linear_mx4(void* stream, dpc_elem elem_x, dpc_elem elem_y, in
   uint8_t* q = static_cast<uint8_t*>(workspace);
   uint8_t* scale = q + (size_t)ntok * steps * 128;
   const Product p{ntok, topk, ntok * topk, n, k, steps, ngroup, q, scale, rows, offsets, qw, sw, bias};
+  if (coded_inside(p)) {
+    return by_elem(elem_x, [&](auto tx) {
+      by_elem(elem_y, [&](auto ty) { launch_few(s, p, (const decltype(tx)*)x, ldx, (decltype(ty)*)y, ldy); });
+    });
+  }
   const int qs = quant(s, elem_x, 1, ntok, k, x, ldx, q, scale);
   if (qs != DPC_OK) return qs;
   return product(s, elem_y, p, y, ldy);

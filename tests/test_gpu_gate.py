@@ -104,11 +104,12 @@ def test_gradient(t, n, E, k):
 @pytest.mark.parametrize("E,k,groups,keep,best", [(3, 2, 1, 1, 1), (12, 4, 4, 2, 2), (40, 6, 1, 1, 1), (100, 8, 10, 3, 2),
                                                   (256, 8, 8, 4, 2), (256, 40, 1, 1, 1), (1000, 8, 8, 3, 1)])
 def test_scores_that_float32_cannot_tell_apart(E, k, groups, keep, best):
-    """Scores a few units of float32's last place apart: 2^-24 of 1 makes 2^-26 of a score, 10^7 roundings of float64."""
+    """Scores 10^-7 apart, as near as float32 may be off, and sums of two that differ in second order, by 10^-14: still a
+    hundred roundings of float64."""
     import paper_2107_02103_amd as P
     rng = np.random.default_rng(E + k)
     n = 200
-    z = (1.0 + 2.0 ** -23 * rng.integers(0, 40, (n, E))).astype(np.float32)
+    z = (1.0 + 2.0 ** -21 * rng.integers(0, 40, (n, E))).astype(np.float32)
     z[1::3] += (rng.integers(-2, 2, (len(z[1::3]), E)) * 0.25).astype(np.float32)
     bias = (rng.integers(0, 3, E) * 2.0 ** -20).astype(np.float32)
     for kind, b in (("sigmoid", bias), ("softmax", bias), ("sigmoid", None), ("softmax", None)):
