@@ -28,6 +28,7 @@ constexpr int64_t kMaxRows = (int64_t)1 << 30;      // rows of codes
 constexpr int64_t kMaxProduct = (int64_t)1 << 27;   // rows of a product (a launch has under 2^32 threads)
 constexpr int kMaxChannels = 1 << 24;
 constexpr int kBlock = 256;
+constexpr int64_t kOnceBytes = (int64_t)192 << 20;  // rows of that size are written past the caches
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -123,45 +124,53 @@ __global__ __launch_bounds__(kBlock) void quant_kernel(int64_t nrows_all, int nr
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kBlock) void values_kernel(int64_t nrows_all, int nrows, int ncols, const uint8_t* __restrict__ q,
-                                                        const uint8_t* __restrict__ scale, T* __restrict__ y, int64_t ldy) {
-  const int lane = threadIdx.x & 31, steps = DPC_MX4_LD(ncols) / 256;
-  const int64_t r = row_of_lane();
+// Values: a lane makes chunks of 16 bytes, kChunks of a row on their way; 2^lanes_log2
+// lanes to a row, so that neighbouring lanes write neighbouring chunks.
+constexpr int kChunks = 4;
+
+template <typename T, bool ONCE>
+__global__ __launch_bounds__(kBlock) void values_kernel(int64_t nrows_all, int nrows, int ncols, int lanes_log2,
+                                                        const uint8_t* __restrict__ q, const uint8_t* __restrict__ scale,
+                                                        T* __restrict__ y, int64_t ldy) {
+  constexpr int VE = Chunk<T>::kElems;
+  typedef std::conditional_t<VE == 8, unsigned, std::conditional_t<VE == 4, uint16_t, uint8_t>> Codes;
+  const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1), steps = DPC_MX4_LD(ncols) / 256;
+  const int64_t r = (blockIdx.z * (int64_t)gridDim.x + blockIdx.x) * (kBlock >> lanes_log2) + (threadIdx.x >> lanes_log2);
   if (r >= nrows_all) return;
-  const int s0 = blockIdx.y * kQuantSteps;
   const int64_t group = r / nrows, row = r - group * nrows;
-  unsigned code[kQuantSteps], e[kQuantSteps];
+  const int c0 = (int)blockIdx.y * kChunks * lanes + lane, nch = (ncols + VE - 1) / VE;
+  unsigned code[kChunks], e[kChunks];
 #pragma unroll
-  for (int k = 0; k < kQuantSteps; ++k) {
-    const int s = min(s0 + k, steps - 1);
-    code[k] = *reinterpret_cast<const unsigned*>(q + (r * steps + s) * 128 + lane * 4);
-    e[k] = scale[((group * steps + s) * nrows + row) * 8 + (lane >> 2)];
+  for (int k = 0; k < kChunks; ++k) {
+    const int at = min(c0 + k * lanes, nch - 1) * VE;  // first column
+    code[k] = *reinterpret_cast<const Codes*>(q + r * steps * 128 + at / 2);
+    e[k] = scale[((group * steps + at / 256) * nrows + row) * 8 + at / 32 % 8];
   }
 #pragma unroll
-  for (int k = 0; k < kQuantSteps; ++k) {
-    const int c = (s0 + k) * 256 + lane * 8;
-    if (c >= ncols) break;
+  for (int k = 0; k < kChunks; ++k) {
+    const int at = (c0 + k * lanes) * VE;
+    if (at >= ncols) break;
     // 2^(E - 127): in float32 a number below the least normal one for E = 0
     typename ElemAcc<T>::type f;
     if constexpr (sizeof(T) == 8) f = __longlong_as_double(e[k] == 255 ? 0x7ff8000000000000ll : (long long)(e[k] + 896) << 52);
     else f = __uint_as_float(e[k] == 0 ? 0x00400000u : e[k] == 255 ? 0x7fc00000u : e[k] << 23);
-    T out[8];
-#define DPC_PAIR(p)                                                                      \
-  {                                                                                      \
-    const v2f two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[k], 1.0f, p);          \
-    out[2 * p] = (T)(two[0] * f);                                                        \
-    out[2 * p + 1] = (T)(two[1] * f);                                                    \
+    Chunk<T> out;
+#define DPC_PAIR(p)                                                             \
+  if constexpr (2 * p < VE) {                                                   \
+    const v2f two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[k], 1.0f, p); \
+    out.v[2 * p] = (T)(two[0] * f);                                             \
+    out.v[2 * p + 1] = (T)(two[1] * f);                                         \
   }
     DPC_PAIR(0) DPC_PAIR(1) DPC_PAIR(2) DPC_PAIR(3)
 #undef DPC_PAIR
-    T* py = y + r * ldy + c;
-    if (c + 8 <= ncols) {
-      __builtin_memcpy(py, out, sizeof(out));
+    T* py = y + r * ldy + at;
+    if (at + VE <= ncols) {
+      if (ONCE) out.store_once(py);
+      else out.store(py);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (c + i < ncols) py[i] = out[i];
+      for (int i = 0; i < VE; ++i)
+        if (at + i < ncols) py[i] = out.v[i];
     }
   }
 }
@@ -592,10 +601,16 @@ extern "C" int dpc_values_mx4(void* stream, dpc_elem elem, int ngroup, int nrows
   if (ngroup == 0 || nrows == 0) return DPC_OK;
   if (!rows_ptrs(elem, ncols, y, ldy, q, scale)) return DPC_EINVAL;
   const int64_t rows = (int64_t)ngroup * nrows;
+  const int es = (int)elem_size(elem), VE = 16 / es, nch = (ncols + VE - 1) / VE;
+  int l = 0;
+  while (l < 6 && (1 << l) * kChunks < nch) ++l;
+  const int64_t blocks = (rows + (kBlock >> l) - 1) / (kBlock >> l), wide = blocks < kWide ? blocks : kWide;
+  const dim3 grid((unsigned)wide, (unsigned)((nch + (kChunks << l) - 1) / (kChunks << l)), (unsigned)((blocks + wide - 1) / wide));
+  const bool once = rows * ncols * es >= kOnceBytes && (int64_t)ncols * es % 16 == 0 && ldy * es % 16 == 0 && elem_aligned(y, 16);
   return by_elem(elem, [&](auto t) {
     typedef decltype(t) T;
-    hipLaunchKernelGGL(values_kernel<T>, rows_grid(rows, ncols), dim3(kBlock), 0, static_cast<hipStream_t>(stream), rows, nrows,
-                       ncols, q, scale, (T*)y, ldy);
+    hipLaunchKernelGGL((once ? values_kernel<T, true> : values_kernel<T, false>), grid, dim3(kBlock), 0,
+                       static_cast<hipStream_t>(stream), rows, nrows, ncols, l, q, scale, (T*)y, ldy);
   });
 }
 
