@@ -32,6 +32,7 @@ namespace {
 constexpr int kOneBlockSlots = 8192;
 constexpr int kPartSlots = 1024;       // slots of a workgroup beyond that, at least
 constexpr int kMaxBlocks = 1024;
+constexpr int kSelfCounts = 16384;     // counts that every workgroup of the last launch reads, at most
 constexpr int kPlanWaves = 4;          // wavefronts of a workgroup of the three launches
 
 inline int plan_blocks(int64_t nslot) {
@@ -196,8 +197,9 @@ __global__ __launch_bounds__(256) void plan_scan_kernel(int blocks, int* __restr
   if (threadIdx.x == 0) total[blockIdx.x] = sum;
 }
 
-// Third launch: rows of the block's part.
-template <typename Job>
+// Third launch: rows of the block's part.  SELF: there was no second one, the
+// counts are read as they are; each workgroup adds them up for itself.
+template <typename Job, bool SELF>
 __global__ __launch_bounds__(64 * kPlanWaves) void plan_place_kernel(int64_t nslot, int64_t part, int nkey, Job job,
                                                                      const int* __restrict__ hist,
                                                                      const int* __restrict__ total) {
@@ -206,9 +208,35 @@ __global__ __launch_bounds__(64 * kPlanWaves) void plan_place_kernel(int64_t nsl
   int* cnt = plan_lds;
   int* off = cnt + kPlanWaves * nkey;
   int* tmp = off + nkey;
+  int* prior = tmp + kPlanWaves;  // SELF: slots of each key in the blocks before
   const int64_t n = job.size(nslot);
   for (int i = threadIdx.x; i < kPlanWaves * nkey; i += blockDim.x) cnt[i] = 0;
-  for (int e = threadIdx.x; e < nkey; e += blockDim.x) off[e] = total[e];
+  if (SELF) {
+    int lanes = 1;  // of a key
+    while (lanes < 64 && lanes * 2 * nkey <= 64 * kPlanWaves) lanes *= 2;
+    const int lane = threadIdx.x & (lanes - 1), blocks = gridDim.x;
+    for (int e0 = 0; e0 < nkey; e0 += 64 * kPlanWaves / lanes) {  // whole wavefronts stay: sums across lanes
+      const int e = e0 + threadIdx.x / lanes;
+      int all = 0, before = 0;
+      if (e < nkey) {
+        for (int b = lane; b < blocks; b += lanes) {
+          const int h = hist[(int64_t)e * blocks + b];
+          all += h;
+          before += b < (int)blockIdx.x ? h : 0;
+        }
+      }
+      for (int m = lanes >> 1; m; m >>= 1) {
+        all += __shfl_xor(all, m);
+        before += __shfl_xor(before, m);
+      }
+      if (e < nkey && lane == 0) {
+        off[e] = all;
+        prior[e] = before;
+      }
+    }
+  } else {
+    for (int e = threadIdx.x; e < nkey; e += blockDim.x) off[e] = total[e];
+  }
   __syncthreads();
   const int kept = block_scan(off, nkey, tmp);
   const int64_t first = blockIdx.x * part + wave * (part / kPlanWaves);
@@ -217,7 +245,7 @@ __global__ __launch_bounds__(64 * kPlanWaves) void plan_place_kernel(int64_t nsl
   count(job, lo, hi, nkey, cnt + wave * nkey);
   __syncthreads();
   for (int e = threadIdx.x; e < nkey; e += blockDim.x) {
-    int run = off[e] + hist[(int64_t)e * gridDim.x + blockIdx.x];
+    int run = off[e] + (SELF ? prior[e] : hist[(int64_t)e * gridDim.x + blockIdx.x]);
     for (int w = 0; w < kPlanWaves; ++w) {
       const int c = cnt[w * nkey + e];
       cnt[w * nkey + e] = run;
@@ -254,9 +282,15 @@ void launch_sort(hipStream_t s, int64_t nslot, int nkey, const Job& job, void* w
   const dim3 block(64 * kPlanWaves);
   hipLaunchKernelGGL(plan_count_kernel<Job>, dim3(blocks), block, (size_t)kPlanWaves * nkey * sizeof(int), s, nslot, part,
                      nkey, job, hist);
+  const size_t lds = ((size_t)(kPlanWaves + 1) * nkey + kPlanWaves) * sizeof(int);
+  // Few counts: every workgroup adds them up, which takes less than a launch.
+  if ((int64_t)blocks * nkey <= kSelfCounts) {
+    hipLaunchKernelGGL((plan_place_kernel<Job, true>), dim3(blocks), block, lds + nkey * sizeof(int), s, nslot, part, nkey,
+                       job, hist, total);
+    return;
+  }
   hipLaunchKernelGGL(plan_scan_kernel, dim3(nkey), dim3(256), 0, s, blocks, hist, total);
-  hipLaunchKernelGGL(plan_place_kernel<Job>, dim3(blocks), block,
-                     ((size_t)(kPlanWaves + 1) * nkey + kPlanWaves) * sizeof(int), s, nslot, part, nkey, job, hist, total);
+  hipLaunchKernelGGL((plan_place_kernel<Job, false>), dim3(blocks), block, lds, s, nslot, part, nkey, job, hist, total);
 }
 
 }  // namespace
