@@ -552,6 +552,173 @@ int product(hipStream_t s, dpc_elem elem_y, const Product& p, void* y, int64_t l
   return by_elem(elem_y, [&](auto t) { launch_product(s, p, (decltype(t)*)y, ldy); });
 }
 
+// Codes and product in one, for layers of few channels over many rows: the codes
+// of kCodedRows rows pass through LDS step by step and never see memory.  While a
+// step is coded and multiplied, the next one's elements are on their way to
+// registers.  Wavefront w makes channels 32 w .. 32 w + 31, with W's rows straight
+// from L2 (every workgroup reads all of W).  Chunks of codes lie as in the tiles above.
+constexpr int kCodedRows = 32, kCodedWaves = 8;
+
+// A lane's 8 results of a row in the type of y, runs at c, c + 4 VE, ... of n.
+template <typename TY>
+__device__ __forceinline__ void put_row(TY* y, int c, int n, const v4f (&acc)[2], const float (&bias)[8], bool exists, bool owned) {
+  constexpr int VE = 16 / sizeof(TY);
+#pragma unroll
+  for (int g = 0; g < 8 / VE; ++g) {
+    TY out[VE];
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const int at = g * VE + e;
+      out[e] = owned ? result<TY>(acc[at / 4][at % 4], bias[at]) : (TY)0;
+    }
+    put_run(y + c + g * 4 * VE, out, exists ? n - c - g * 4 * VE : 0);
+  }
+}
+
+template <typename TX>
+__global__ __launch_bounds__(64 * kCodedWaves, 4) void coded_product_kernel(Product p, dpc_elem elem_y, const TX* __restrict__ x,
+                                                                            int64_t ldx, void* __restrict__ y, int64_t ldy) {
+  constexpr int kRows = kCodedRows, MI = kRows / 16, kPass = kRows * 32 / (64 * kCodedWaves);  // rows that 32 lanes code
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2][kRows * 136];          // codes, then scales
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Tile t = find_tile(p, kRows, blockIdx.x);
+  if (t.row0 >= t.end) return;
+  const int steps = p.steps, group = max(t.group, 0);
+  const int ve = elem_y == DPC_ELEM_F64 ? 2 : elem_y == DPC_ELEM_F32 ? 4 : 8;
+  auto channel = [&](int j, int r) __attribute__((always_inline)) {
+    return ve == 2 ? channel_of<2>(j, r) : ve == 4 ? channel_of<4>(j, r) : channel_of<8>(j, r);
+  };
+  // 32 lanes to a row: rows half, half + 16, ...
+  const int half = threadIdx.x >> 5, l32 = threadIdx.x & 31;
+  const TX* px[kPass];
+#pragma unroll
+  for (int a = 0; a < kPass; ++a) {
+    const int tok = t.group < 0 ? -1 : token_of(p, min(t.row0 + half + 16 * a, t.end - 1));
+    px[a] = x + (int64_t)max(tok, 0) * ldx + l32 * 8;
+  }
+  const uint8_t *pw[2], *psw[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    pw[j] = p.qw + ((int64_t)group * p.n + min(wave * 32 + channel(j, lane >> 2), p.n - 1)) * steps * 128 + (lane & 3) * 32;
+    psw[j] = p.sw + ((int64_t)group * steps * p.n + min(wave * 32 + channel(j, l16), p.n - 1)) * 8 + quad * 2;
+  }
+  const bool work = wave * 32 < p.n;  // this wavefront has channels
+  auto take = [&](int s, TX (&held)[kPass][8]) __attribute__((always_inline)) {
+    if (s * 256 + 256 <= p.k) {
+#pragma unroll
+      for (int a = 0; a < kPass; ++a)
+#pragma unroll
+        for (int c = 0; c < 8; c += Chunk<TX>::kElems) {
+          Chunk<TX> ch;
+          ch.load_once(px[a] + s * 256 + c);
+#pragma unroll
+          for (int i = 0; i < Chunk<TX>::kElems; ++i) held[a][c + i] = ch.v[i];
+        }
+    } else {
+#pragma unroll
+      for (int a = 0; a < kPass; ++a)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int c = s * 256 + l32 * 8 + i;
+          const TX v = px[a][min(c, p.k - 1) - l32 * 8];
+          held[a][i] = c < p.k ? v : (TX)0;
+        }
+    }
+  };
+  v4f acc[MI][2];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  TX held[kPass][8];
+  take(0, held);
+  for (int s = 0; s < steps; ++s) {
+    uint8_t* to = lds[s & 1];
+    v4i w[2][2];
+    int ew[2];
+    if (work) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) w[k][j] = *reinterpret_cast<const v4i*>(pw[j] + s * 128 + k * 16);
+        ew[j] = *reinterpret_cast<const uint16_t*>(psw[j] + (int64_t)s * p.n * 8);
+      }
+    }
+#pragma unroll
+    for (int a = 0; a < kPass; ++a) {
+      const int row = half + 16 * a, chunk = l32 >> 2;
+      float v[8], factor;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = (float)held[a][i];
+      const unsigned e = code_step(v, &factor);
+      *reinterpret_cast<unsigned*>(to + row * 128 + ((chunk ^ (row & 7)) << 4) + (l32 & 3) * 4) = codes_of(v, factor);
+      if ((l32 & 3) == 0) to[kRows * 128 + row * 8 + chunk] = (uint8_t)e;
+    }
+    if (s + 1 < steps) take(s + 1, held);
+    // the codes of this step are written (its buffer was read two steps ago, before
+    // the barrier in between); loads stay under way
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (!work) continue;
+    v4i a[2][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) a[k][j] = to_rows(w[k][j]);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int row = i * 16 + l16;
+      const int ex = *reinterpret_cast<const uint16_t*>(to + kRows * 128 + row * 8 + quad * 2);
+      const v4i b0 = *reinterpret_cast<const v4i*>(to + row * 128 + (((quad * 2) ^ (l16 & 7)) << 4));
+      const v4i b1 = *reinterpret_cast<const v4i*>(to + row * 128 + (((quad * 2 + 1) ^ (l16 & 7)) << 4));
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        acc[i][j] = mfma4<0>(a[0][j], b0, acc[i][j], ew[j], ex);
+        acc[i][j] = mfma4<1>(a[1][j], b1, acc[i][j], ew[j], ex);
+      }
+    }
+  }
+  if (!work) return;
+  float bias[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const int c = min(wave * 32 + channel(q / 4, quad * 4 + q % 4), p.n - 1);
+    bias[q] = p.bias ? p.bias[(int64_t)group * p.n + c] : 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int r = t.row0 + i * 16 + l16, c = wave * 32 + quad * ve;
+    const bool exists = r < t.end, owned = exists && t.group >= 0 && token_of(p, r) >= 0;
+    auto put = [&](auto* py) __attribute__((always_inline)) {
+      put_row(py + (int64_t)r * ldy, c, p.n, acc[i], bias, exists, owned);
+    };
+    switch (elem_y) {
+      case DPC_ELEM_F64: put((double*)y); break;
+      case DPC_ELEM_F32: put((float*)y); break;
+      case DPC_ELEM_F16: put((_Float16*)y); break;
+      default: put((__bf16*)y); break;
+    }
+  }
+}
+
+// Whether that kernel takes a layer: rows of 1,024 elements or more, so many of them
+// that in two kernels the codes would leave the caches in between.  Times, us, 240
+// channels, one kernel and two:
+//   float32, 1,600 columns     8,192 rows 17.6 18.3, 32,768 60.1 52.0, 131,072 223 259, 1,048,576 1,824 2,025
+//   bfloat16, 1,600 columns    8,192 rows 14.7 15.4, 32,768 40.7 39.7, 131,072 147 161, 1,048,576 1,138 1,223
+//   bfloat16, 8,192 columns    8,192 rows 53.1 46.0, 16,384 75.6 107, 131,072 551 786
+//   bfloat16, 240 columns      8,192 rows 7.1 7.7, 131,072 56.3 44.0, 1,048,576 465 342
+//   float64, 1,600 columns     16,384 rows 74.7 46.4, 131,072 605 458
+// Coding takes most of its instructions: with 64 rows to a workgroup (W moved to the
+// lanes of a product half as often) registers spill (2,563 us in the first line), with
+// two steps of elements under way it is no faster (1,920).
+inline bool one_kernel(const Product& p, dpc_elem elem_x) {
+  return p.topk == 1 && p.n <= 256 && p.k >= 1024 && (int64_t)p.m * p.k >= (int64_t)1 << 27 && elem_x != DPC_ELEM_F64 &&
+         !few_rows(p);
+}
+
 // Whether every workgroup codes the rows again, all of them up to 16,384 elements
 // (in steps of 256), which costs less than a launch.  Device times, us, one kernel
 // and two: 1 row of 1,600 float32 to 240 channels 3.7 and 5.9, 8 rows 4.8 and 6.1, 16
@@ -652,6 +819,13 @@ extern "C" int dpc_linear_mx4(void* stream, dpc_elem elem_x, dpc_elem elem_y, in
   if (coded_inside(p)) {
     return by_elem(elem_x, [&](auto tx) {
       by_elem(elem_y, [&](auto ty) { launch_few(s, p, (const decltype(tx)*)x, ldx, (decltype(ty)*)y, ldy); });
+    });
+  }
+  if (one_kernel(p, elem_x)) {
+    return by_elem(elem_x, [&](auto tx) {
+      typedef std::conditional_t<sizeof(tx) == 8, float, decltype(tx)> TX;  // never float64
+      hipLaunchKernelGGL(coded_product_kernel<TX>, dim3((unsigned)most_tiles(p, kCodedRows)), dim3(64 * kCodedWaves), 0, s, p,
+                         elem_y, (const TX*)x, ldx, y, ldy);
     });
   }
   const int qs = quant(s, elem_x, 1, ntok, k, x, ldx, q, scale);

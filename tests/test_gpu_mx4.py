@@ -237,3 +237,45 @@ def test_no_rows():
     lin = P.Mx4Linear.from_weight(torch.randn(7, 40, device="cuda"))
     assert lin(torch.empty(0, 40, device="cuda")).shape == (0, 7)
     assert P.Mx4Rows.from_rows(torch.empty(0, 40, device="cuda")).values().shape == (0, 40)
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("m,n,k,G", [(131109, 250, 1030, 1), (131072, 33, 1024, 1), (131105, 256, 1024, 3), (66000, 17, 2049, 2)])
+def test_narrow_layers_over_many_rows(t, m, n, k, G):
+    """Rows that are coded and multiplied in one kernel: the same as in two (up to the order of a sum), and sampled
+    rows against the plain layer."""
+    import paper_2107_02103_amd as P
+    rng = np.random.default_rng(m + n)
+    codes, scales, w, bias = layer(rng, G, n, k)
+    x = torch.empty(m, k + 3, dtype=TYPES[t], device="cuda")[:, :k]
+    x.normal_(generator=torch.Generator("cuda").manual_seed(n))
+    x[7] = 0.0
+    x[m - 2, k - 1] = float("inf")
+    lin = P.Mx4Linear(codes, scales, k, torch.from_numpy(bias).cuda())
+    route, rows = None, np.arange(m)
+    if G > 1:
+        e = rng.integers(-1, G, (m, 1)).astype(np.int32)
+        route = P.Route(torch.from_numpy(e).cuda(), G)
+        rows = route.rows.cpu().numpy()
+    for ty in (t, "f32", "f64"):
+        out = torch.full((m, n + 1), 9.0, dtype=TYPES[ty], device="cuda")
+        y = lin(x, route=route, dtype=TYPES[ty], out=out[:, :n])
+        two = lin(P.Mx4Rows.from_rows(x), route=route, dtype=TYPES[ty])
+        assert (out[:, n] == 9.0).all()
+        assert torch.equal(y.isnan(), two.isnan())
+        some = np.unique(np.concatenate([rng.integers(0, m, 60), [0, 31, 32, m - 1], np.flatnonzero(rows == 7),
+                                         np.flatnonzero(rows == m - 2)]))
+        off = [0, m] if route is None else route.offsets.tolist()
+        expert = np.searchsorted(np.array(off[1:]), some, side="right")
+        at = torch.from_numpy(some).cuda()
+        plain = om.values(*om.quantise(x[torch.from_numpy(np.maximum(rows[some], 0)).cuda().long()].cpu().double().numpy()))[:, :k]
+        want, mag = np.zeros((len(some), n)), np.zeros((len(some), n))
+        for g in range(G):
+            r = np.flatnonzero(expert == g)
+            want[r], mag[r] = om.product(plain[r], w[g], bias[g])
+        check(y[at], want, mag, k, ty)
+        d = (y.double() - two.double()).abs().nan_to_num()
+        # every row: twice the bound of one sum, of magnitudes under 8 sigma of k products, and a rounding
+        top = 8.0 * np.sqrt(k) * float(np.abs(w).max()) * 6
+        assert float(d.max()) <= 2 * (k / 128 + 12) * 2.0 ** -23 * top * np.sqrt(k) + 2.002 * STEP[ty] * float(two.nan_to_num().abs().max())
+        del out, y, two, d
