@@ -26,8 +26,11 @@ _OBJECTS = {"SeATab": "descriptor", "Route": "experts", "Int8Linear": "experts",
 def __getattr__(name):
     if name in _BINDING:
         from . import binding
-        return getattr(binding, name)
-    if name in _OBJECTS:
+        value = getattr(binding, name)
+    elif name in _OBJECTS:
         from importlib import import_module
-        return getattr(import_module("." + _OBJECTS[name], __name__), name)
-    raise AttributeError(name)
+        value = getattr(import_module("." + _OBJECTS[name], __name__), name)
+    else:
+        raise AttributeError(name)
+    globals()[name] = value              # found without this function from now on (it takes microseconds)
+    return value

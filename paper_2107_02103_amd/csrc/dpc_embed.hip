@@ -413,7 +413,7 @@ Layout layout_for(dpc_elem elem, int ntok, int nid, int width) {
   l.slabs = (int)(((int64_t)nch + (1 << l.lanes_log2) - 1) >> l.lanes_log2);
   // about 4,096 groups of lanes in all
   const int64_t part = ((int64_t)ntok * l.slabs + 4095) / 4096;
-  l.part = (int)(part < 16 ? 16 : part > 1024 ? 1024 : part);
+  l.part = (int)(part < 32 ? 32 : part > 1024 ? 1024 : part);
   l.parts = (int)(((int64_t)ntok + l.part - 1) / l.part);
   size_t at = 0;
   const auto take = [&](size_t bytes) {

@@ -719,12 +719,17 @@ inline bool one_kernel(const Product& p, dpc_elem elem_x) {
          !few_rows(p);
 }
 
-// Whether every workgroup codes the rows again, all of them up to 16,384 elements
-// (in steps of 256), which costs less than a launch.  Device times, us, one kernel
-// and two: 1 row of 1,600 float32 to 240 channels 3.7 and 5.9, 8 rows 4.8 and 6.1, 16
-// rows 6.4 and 6.3; 1 bfloat16 row of 4,096 to 4,096 4.2 and 6.5, 4 rows 5.4 and 6.8, 16
-// rows 10.2 and 6.9.
-inline bool coded_inside(const Product& p) { return few_rows(p) && (int64_t)p.m * p.steps <= 64; }
+// Whether every workgroup codes its rows itself, up to 16,384 elements of them (in
+// steps of 256), which costs less than a launch.  Of experts the host knows the
+// average alone: a tile is taken to have twice as many rows.  Device times, us, one
+// kernel and two: 1 row of 1,600 float32 to 240 channels 3.7 and 5.9, 8 rows 4.8 and
+// 6.1, 16 rows 6.4 and 6.3; 1 bfloat16 row of 4,096 to 4,096 4.2 and 6.5, 4 rows 5.4 and
+// 6.8, 16 rows 10.2 and 6.9.
+inline bool coded_inside(const Product& p) {
+  const int most = p.m < 16 ? p.m : 16, likely = (2 * p.m + p.ngroup - 1) / p.ngroup;
+  const int rows = p.offsets && likely < most ? likely : most;
+  return few_rows(p) && rows * p.steps <= 64 && few_bytes(p) <= 65536;
+}
 
 int product_args(dpc_elem elem_y, int ntok, int topk, int n, int k, int ngroup) {
   if (!elem_ok(elem_y) || ntok < 0 || topk < 1 || n < 1 || k < 1 || ngroup < 1) return DPC_EINVAL;

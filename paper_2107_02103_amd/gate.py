@@ -9,6 +9,7 @@ import torch
 from . import binding as B
 from .experts import (_MOST, _check, _current_device, _elem_of, _enter, _lib, _on, _raw_stream, _rows, _too_large)
 
+_Spec = B.dpc_gate_spec
 _SCORES = {"softmax": B.DPC_SCORE_SOFTMAX, "sigmoid": B.DPC_SCORE_SIGMOID}
 
 
@@ -30,17 +31,16 @@ class Gate:
     def __init__(self, nexpert, topk, score="softmax", groups=1, keep=1, best=1, bias=None, renormalise=False, scale=1.0):
         if score not in _SCORES:
             raise ValueError(f"score is softmax or sigmoid, not {score!r}")
-        sizes = [int(v) for v in (nexpert, topk, groups, keep, best)]
-        if max(map(abs, sizes)) > _MOST:
-            _too_large("dpc_gate")
-        self.nexpert, self.topk = sizes[:2]
+        for v in (nexpert, topk, groups, keep, best):
+            if not -_MOST <= v <= _MOST:
+                _too_large("dpc_gate")
+        self.nexpert, self.topk = int(nexpert), int(topk)
         if bias is not None:
             if bias.dtype != torch.float32 or bias.shape != (self.nexpert,) or not bias.is_contiguous():
                 raise ValueError("bias must be contiguous float32 [nexpert]")
             _on(bias, None, "bias")
         self.bias = bias
-        self.spec = B.dpc_gate_spec(self.nexpert, self.topk, _SCORES[score], sizes[2], sizes[3], sizes[4], bool(renormalise),
-                                    float(scale))
+        self.spec = _Spec(self.nexpert, self.topk, _SCORES[score], int(groups), int(keep), int(best), bool(renormalise), scale)
         self._spec = C.byref(self.spec)
 
     def _logits(self, logits, dev):
@@ -65,8 +65,7 @@ class Gate:
             bias = bias.data_ptr()
         n, elem = logits.shape[0], _elem_of(logits.dtype)
         shape = (n, max(self.topk, 0))
-        expert = torch.empty(shape, dtype=torch.int32, device=logits.device)
-        weight = torch.empty(shape, dtype=wt, device=logits.device)
+        expert, weight = logits.new_empty(shape, dtype=torch.int32), logits.new_empty(shape, dtype=wt)
         _check(_lib.dpc_gate(_raw_stream(dev), elem, self._spec, n, logits.data_ptr(), ld, bias, expert.data_ptr(),
                              weight.data_ptr()), "dpc_gate")
         return expert, weight
@@ -86,7 +85,7 @@ class Gate:
                 raise ValueError(f"{name} must be contiguous {dt} [tokens, topk]")
             _on(t, dev, name)
         if out is None:
-            out, ldo = torch.empty((n, self.nexpert), dtype=logits.dtype, device=logits.device), self.nexpert
+            out, ldo = logits.new_empty((n, self.nexpert)), self.nexpert
         else:
             ldo = _rows(out, "out", n, self.nexpert, logits.dtype, dev)
         _check(_lib.dpc_gate_bwd(_raw_stream(dev), elem, self._spec, n, logits.data_ptr(), ld, expert.data_ptr(),
@@ -160,7 +159,7 @@ class Embedding:
         else:
             ldo = _rows(out, "out", nid, width, dtype, dev)
         nb = _lib.dpc_embed_bwd_workspace_bytes(elem, n, nid, width)
-        ws = torch.empty(nb, dtype=torch.uint8, device=dy.device)
+        ws = dy.new_empty(nb, dtype=torch.uint8)
         _check(_lib.dpc_embed_bwd(_raw_stream(dev), elem, elem_d, n, nid, width, ids.data_ptr(), dy.data_ptr(), lddy,
                                   float(scale), ws.data_ptr(), nb, out.data_ptr(), ldo), "dpc_embed_bwd")
         return out

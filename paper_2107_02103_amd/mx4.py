@@ -7,8 +7,11 @@ from . import binding as B
 from .experts import (_MOST, _check, _current_device, _elem_of, _enter, _lib, _on, _raw_stream, _rows, _too_large)
 
 
+_U8 = torch.uint8
+
+
 def _bytes(t, shape, name, device):
-    if t.dtype != torch.uint8 or t.shape != shape or not t.is_contiguous():
+    if t.dtype != _U8 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous uint8 {list(shape)}")
     _on(t, device, name)
 
@@ -20,8 +23,8 @@ def _quantise(x, groups):
     if rows > _MOST or cols > _MOST:
         _too_large("dpc_quant_mx4")
     ld, n = B.mx4_ld(cols), rows // groups if groups else 0
-    codes = torch.empty((groups, n, ld // 2), dtype=torch.uint8, device=x.device)
-    scales = torch.empty((groups, ld // 256, n, 8), dtype=torch.uint8, device=x.device)
+    codes = x.new_empty((groups, n, ld // 2), dtype=torch.uint8)
+    scales = x.new_empty((groups, ld // 256, n, 8), dtype=torch.uint8)
     _check(_lib.dpc_quant_mx4(_raw_stream(dev), _elem_of(x.dtype), groups, n, cols, x.data_ptr(), ldx, codes.data_ptr(),
                               scales.data_ptr()), "dpc_quant_mx4")
     return codes, scales
@@ -31,7 +34,7 @@ def _values(codes, scales, cols, dtype, out, dev):
     """Rows that codes [groups, n, .] and scales [groups, ., n, 8] stand for."""
     groups, n = codes.shape[:2]
     if out is None:
-        out, ldy = torch.empty((groups * n, cols), dtype=dtype, device=codes.device), cols
+        out, ldy = codes.new_empty((groups * n, cols), dtype=dtype), cols
     else:
         ldy = _rows(out, "out", groups * n, cols, dtype, dev)
     _check(_lib.dpc_values_mx4(_raw_stream(dev), _elem_of(dtype), groups, n, cols, codes.data_ptr(), scales.data_ptr(),
@@ -170,7 +173,7 @@ class Mx4Linear:
         if dtype is None:
             dtype = torch.float32 if coded else x.dtype
         if out is None:
-            out, ldy = torch.empty((ntok * topk, self.outer), dtype=dtype, device=self.codes.device), self.outer
+            out, ldy = self.codes.new_empty((ntok * topk, self.outer), dtype=dtype), self.outer
         else:
             ldy = _rows(out, "out", ntok * topk, self.outer, dtype, dev)
         tail = (rows, offsets, self.codes.data_ptr(), self.scales.data_ptr(),
