@@ -19,8 +19,8 @@
 #include "dpc.h"
 #include "dpc_elem.h"
 #include "dpc_groups.h"
-#include "dpc_i8_tiles.h"
 #include "dpc_internal.h"
+#include "dpc_mx4_tiles.h"
 
 namespace {
 
@@ -213,13 +213,9 @@ struct Product {
 };
 
 // Tiles of `size` rows that find_tile can be asked for.
-inline int64_t most_tiles(const Product& p, int size) {
-  if (!p.offsets) return ((int64_t)p.m + size - 1) / size;
-  const int64_t t = (int64_t)p.m / size + p.ngroup + 1;
-  return t < p.m ? t : p.m;
-}
+inline int64_t most_tiles(const Product& p, int size) { return mx4_most_tiles(p.m, p.ngroup, p.offsets != nullptr, size); }
 
-inline bool few_rows(const Product& p) { return i8_few_rows(p.m, p.n, p.ngroup, p.offsets != nullptr); }
+inline bool few_rows(const Product& p) { return mx4_few_rows(p.m, p.n, p.ngroup, p.offsets != nullptr); }
 
 // One product of 16 rows of W and 16 rows of x, 128 columns: codes a and b of this
 // lane's block, whose scale is byte K of sa and sb.
@@ -540,7 +536,7 @@ void launch_tiled(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
 template <typename TY>
 void launch_product(hipStream_t s, const Product& p, TY* y, int64_t ldy) {
   if (few_rows(p)) return launch_few(s, p, p.qx, 0, y, ldy);
-  switch (i8_tile(p.m, p.n, p.steps * 128, p.ngroup, p.offsets != nullptr)) {
+  switch (mx4_tile(p.m, p.n, p.steps, p.ngroup, p.offsets != nullptr)) {
     case 0: return launch_tiled<TY, 256, 256, 2, 4>(s, p, y, ldy);
     case 1: return launch_tiled<TY, 128, 128, 2, 2>(s, p, y, ldy);
     case 2: return launch_tiled<TY, 128, 64, 2, 2>(s, p, y, ldy);
