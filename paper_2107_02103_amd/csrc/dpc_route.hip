@@ -30,6 +30,7 @@ constexpr int kMaxWidth = INT32_MAX - 127;  // a lane's next element (64 on) and
 // plan
 // ---------------------------------------------------------------------------
 struct PlanJob {
+  static constexpr int kPart = 1024;  // with 4,096 331,776 slots take twice as long
   const int* __restrict__ expert;
   int* __restrict__ offsets;
   int* __restrict__ rows;
@@ -292,7 +293,7 @@ extern "C" size_t dpc_route_workspace_bytes(int ntok, int topk, int nexpert) {
   if (ntok < 0 || topk < 1 || topk > DPC_MAX_TOPK || nexpert < 1 || nexpert > DPC_MAX_EXPERTS) return 0;
   const int64_t nslot = (int64_t)ntok * topk;
   if (nslot > kMaxSlots) return 0;
-  return sort_workspace_bytes(nslot, nexpert);
+  return sort_workspace_bytes<PlanJob>(nslot, nexpert);
 }
 
 extern "C" int dpc_route_plan(void* stream, int ntok, int topk, int nexpert, const int* expert, void* workspace,

@@ -7,10 +7,11 @@
 // A part is what one wavefront walks, 64 slots at a time: lanes with the same
 // key find each other by one ballot per bit of the key, and their rank is the
 // number of such lanes below.  No atomics: the order is the same on every call.
-// Bound by latency: 3 us for a few slots, 12 to 16 us for 331,776 in three
-// launches of 1,024 slots to a workgroup (with 4,096 31 us).
+// Bound by latency: 3 us for a few slots, 14 us for 331,776 of 2 keys in two
+// launches, 17 us for 16,384 of 256 keys.
 //
 // A job has
+//   kPart                            slots of a workgroup, at least (constexpr int)
 //   int key(int64_t s)               key of slot s; none of [0, nkey): dropped
 //   int64_t size(int64_t n)          slots that exist, at most n
 //   void put(int64_t s, int e, int row)   slot s goes to row (-1: dropped)
@@ -30,13 +31,13 @@ namespace {
 // 13.6 in three launches, 8,192 14.4 and 14.1, 16,384 24.3 and 14.1 (2 keys
 // 6.9, 10.5; 9.5, 10.6; 14.8, 10.9).
 constexpr int kOneBlockSlots = 8192;
-constexpr int kPartSlots = 1024;       // slots of a workgroup beyond that, at least
 constexpr int kMaxBlocks = 1024;
 constexpr int kSelfCounts = 16384;     // counts that every workgroup of the last launch reads, at most
 constexpr int kPlanWaves = 4;          // wavefronts of a workgroup of the three launches
 
-inline int plan_blocks(int64_t nslot) {
-  const int64_t b = (nslot + kPartSlots - 1) / kPartSlots;
+// Beyond, a workgroup takes a job's kPart slots at least.
+inline int plan_blocks(int64_t nslot, int part) {
+  const int64_t b = (nslot + part - 1) / part;
   return (int)(b < kMaxBlocks ? b : kMaxBlocks);
 }
 // slots of a workgroup: every wavefront gets whole groups of 64
@@ -261,8 +262,9 @@ __global__ __launch_bounds__(64 * kPlanWaves) void plan_place_kernel(int64_t nsl
 }
 
 // Bytes of workspace that a sort of nslot slots needs.
-inline size_t sort_workspace_bytes(int64_t nslot, int nkey) {
-  const size_t blocks = nslot <= kOneBlockSlots ? 0 : plan_blocks(nslot);
+template <typename Job>
+size_t sort_workspace_bytes(int64_t nslot, int nkey) {
+  const size_t blocks = nslot <= kOneBlockSlots ? 0 : plan_blocks(nslot, Job::kPart);
   return ((blocks + 1) * nkey * sizeof(int) + 255) / 256 * 256;
 }
 
@@ -275,7 +277,7 @@ void launch_sort(hipStream_t s, int64_t nslot, int nkey, const Job& job, void* w
     hipLaunchKernelGGL(plan_one_kernel<Job>, dim3(1), dim3(64 * waves), lds, s, (int)nslot, nkey, job);
     return;
   }
-  const int blocks = plan_blocks(nslot);
+  const int blocks = plan_blocks(nslot, Job::kPart);
   const int64_t part = plan_part(nslot, blocks);
   int* hist = static_cast<int*>(workspace);
   int* total = hist + (size_t)blocks * nkey;
