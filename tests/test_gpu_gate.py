@@ -230,3 +230,50 @@ def test_chain_with_route_and_gradient_of_a_mixture():
             assert torch.equal(ea, base) and torch.equal(eb, base)
             # third derivatives of order 10 n times h^2, roundings n 2^-52 / h
             assert abs((a - b) / (2 * h) - d[v, e]) < 10 * n * h * h + n * 2.0 ** -50 / h
+
+
+@pytest.mark.parametrize("E,groups,k", [(4, 4, 4), (8, 8, 8), (16, 16, 16), (32, 32, 32), (64, 64, 64), (48, 16, 30)])
+def test_as_many_groups_as_experts(E, groups, k):
+    """The most LDS that a wavefront takes, and groups of one expert."""
+    import paper_2107_02103_amd as P
+    rng = np.random.default_rng(E)
+    z = rng.standard_normal((130, E)).astype(np.float32)
+    z[5::7] = -np.inf
+    bias = rng.standard_normal(E).astype(np.float32)
+    for keep in (groups, max(1, groups // 2)):
+        kk = min(k, keep * (E // groups))
+        for t in (torch.float32, torch.float64):
+            e, w = P.Gate(E, kk, "softmax", groups, keep, 2, torch.from_numpy(bias).cuda())(torch.from_numpy(z).cuda().to(t))
+            we, ww = og.choose(z, kk, "softmax", bias, groups, keep, 2)
+            np.testing.assert_array_equal(e.cpu().numpy(), we)
+            _check_weights(w, ww, E, "f64" if t == torch.float64 else "f32")
+
+
+def test_tokens_past_32_bits():
+    """Rows of logits that start behind 2^31 elements, read and written."""
+    import paper_2107_02103_amd as P
+    far = torch.empty((1 << 31) + 4096, dtype=torch.bfloat16, device="cuda")
+    z = torch.as_strided(far, (3, 64), ((1 << 30) + 512, 1))
+    z.copy_(torch.randn(3, 64))
+    gate = P.Gate(64, 4, "softmax")
+    e, w = gate(z)
+    near = z.clone()
+    e2, w2 = gate(near)
+    assert torch.equal(e, e2) and torch.equal(w, w2)
+    dw = torch.randn(3, 4, device="cuda")
+    out = torch.as_strided(far, (3, 64), ((1 << 30) + 512, 1), 128)
+    gate.backward(z, e, dw, out=out)
+    assert torch.equal(out, gate.backward(near, e, dw))
+
+
+def test_many_tokens():
+    """More than one dimension of a launch takes at once, in workgroups of 256 tokens: checked by what is known."""
+    import paper_2107_02103_amd as P
+    n = (1 << 30) + 300
+    z = torch.zeros(n, 1, dtype=torch.bfloat16, device="cuda")
+    z[-1] = -float("inf")
+    with pytest.raises(P.DpcError):
+        P.Gate(1, 1)(z)
+    z = z[-(1 << 30):]
+    e, w = P.Gate(1, 1, "sigmoid", scale=4.0)(z)
+    assert e[-1] == -1 and w[-1] == 0 and not e[:-1].any() and bool((w[:-1] == 2.0).all())
