@@ -555,10 +555,11 @@ int dpc_embed_bwd(void* stream, dpc_elem elem, dpc_elem elem_d, int ntok, int ni
  *           one in the low half
  *   scales  uint8 [DPC_MX4_LD(cols) / 256][rows][8]: byte E of a block stands for
  *           2^(E - 127), 255 for NaN
- * A code is off by up to a sixth of its block's largest magnitude where that is
- * large and a quarter of itself elsewhere: a product of normally distributed rows
- * is off by 13 to 17% of the norm.  That is for searches and for weights trained
- * with it; forces of nets that were not are wrong.                           */
+ * A code is off by up to a fifth of itself from one scale on, and by up to a
+ * quarter of the scale (a 14th of the block's largest magnitude) below: a product of
+ * normally distributed rows is off by 16% of the norm, and by up to 19% where
+ * channels of x differ in size.  That is for searches and for weights trained
+ * with such codes; forces of nets that were not are wrong.                   */
 #define DPC_MX4_LD(cols) (((cols) + 255) / 256 * 256)
 #define DPC_MAX_MX4_COLS (1 << 20)
 
