@@ -169,24 +169,30 @@ __device__ __forceinline__ float number(unsigned key) {
 }
 
 // LDS of a wavefront: chosen experts [tokens][topk], groups' values [tokens][groups]
-// as doubles, and, one after the other, values [tokens][nexpert] of groups that are
-// no whole lanes, as doubles, and keys [EPL][64].
+// as doubles, and, one after the other, values of groups that are no whole lanes
+// ([tokens][nexpert], of the type that chooses), keys [EPL][64] and the values of one
+// token as doubles.
 __host__ __device__ constexpr size_t chosen_bytes(int tokens, const Gate& g) { return ((size_t)tokens * g.topk * 4 + 15) / 16 * 16; }
 __host__ __device__ constexpr size_t group_bytes(int tokens, const Gate& g) {
   return g.groups > 1 ? ((size_t)tokens * g.groups * 8 + 15) / 16 * 16 : 0;
 }
+template <typename T>
 __host__ __device__ constexpr size_t wave_bytes(int tokens, int epl, const Gate& g) {
-  const size_t keys = (size_t)epl * 256, values = g.groups > 1 && !g.lanes ? (size_t)tokens * g.nexpert * 8 : 0;
-  return chosen_bytes(tokens, g) + group_bytes(tokens, g) + ((keys > values ? keys : values) + 15) / 16 * 16;
+  const size_t keys = (size_t)epl * 256, one = (size_t)g.nexpert * 8;  // keys: as many bytes as float32 values
+  const size_t values = sizeof(T) == 8 ? tokens * one : keys > one ? keys : one;
+  return chosen_bytes(tokens, g) + group_bytes(tokens, g) +
+         (sizeof(T) == 8 && g.groups == 1 ? 0 : g.groups == 1 ? keys : (values + 15) / 16 * 16);
 }
 
-// Which groups stay (bit by bit) of values c, -infinity where an expert cannot be
-// chosen; *near: two at the border are closer than what float32 can tell apart.
+// Which groups stay (bit by bit).  Of a group that is whole lanes (g.lanes) each
+// lane has its two best, first and second, -infinity where there is none; else c
+// are the lane's values, -infinity where an expert cannot be chosen.  *near: two
+// groups at the border are closer than what float32 can tell apart.
 template <int LANES, int EPL, typename V>
-__device__ __forceinline__ unsigned long long kept_groups(const Gate& g, const V (&c)[EPL], int lane, V* values, V* group,
-                                                          bool* near) {
+__device__ __forceinline__ unsigned long long kept_groups(const Gate& g, V first, V second, const V (&c)[EPL], int lane,
+                                                          V* values, V* group, bool* near) {
   const int e0 = lane * EPL;
-  V first, second, size = (V)0;  // the two best of a group; their magnitudes, largest of all groups
+  V size = (V)0;  // magnitudes of a group's best, largest of all groups
   auto put = [&](int q) __attribute__((always_inline)) {
     const bool two = g.best == 2 && second != -(V)INFINITY;
     group[q] = two ? first + second : first;
@@ -211,10 +217,7 @@ __device__ __forceinline__ unsigned long long kept_groups(const Gate& g, const V
     if constexpr (LANES > 8) { if (some > 8) step(std::integral_constant<int, 8>{}); }
     if constexpr (LANES > 16) { if (some > 16) step(std::integral_constant<int, 16>{}); }
   };
-  if (g.lanes) {  // a group is a whole number of lanes, 1, 2, 4, ...
-    first = second = -(V)INFINITY;
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) take(c[i]);
+  if (g.lanes) {
     merge(g.lanes);
     if (!(lane & (g.lanes - 1)) && e0 < g.nexpert) put(g.group_of(e0));
   } else {
@@ -254,8 +257,8 @@ __device__ __forceinline__ unsigned long long kept_groups(const Gate& g, const V
     low = across<LANES>(low, Smaller());
     high = across<LANES>(high, Larger());
     size = across<LANES>(size, Larger());
-    // a value is off by its terms' errors, a rounding of each and one of its own
-    *near = high != -(V)INFINITY && !(low - high > 4 * score_off_by(g.sigmoid) + 0x1p-21f * size);
+    // a value is off by its terms' errors, what their keys have lost and a rounding
+    *near = high != -(V)INFINITY && !(low - high > 4 * score_off_by(g.sigmoid) + (EPL + 4) * 0x1p-22f * size);
   }
   return kept;
 }
@@ -285,10 +288,22 @@ __device__ __forceinline__ bool close(bool plain, bool sigmoid, unsigned high, u
   return !(a - b > off_by<EPL>(sigmoid, a) + off_by<EPL>(sigmoid, b));
 }
 
-// The order in float64, one expert after the other.
+// The choice in float64, one expert after the other.
 template <int LANES, int EPL>
-__device__ __forceinline__ void choose64(const Gate& g, double (&c)[EPL], int lane, int* chosen) {
+__device__ __forceinline__ void choose64(const Gate& g, double (&c)[EPL], int lane, double* values, double* group, int* chosen) {
   const int e0 = lane * EPL;
+  if (g.groups > 1) {
+    double first = -INFINITY, second = -INFINITY;
+    if (g.lanes) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        second = Larger()(second, Smaller()(c[i], first));
+        first = Larger()(first, c[i]);
+      }
+    }
+    const unsigned long long kept = kept_groups<LANES>(g, first, second, c, lane, values, group, (bool*)nullptr);
+    drop(g, kept, e0, c);
+  }
   for (int j = 0; j < g.topk; ++j) {
     double top = -INFINITY;
     int at = INT32_MAX;
@@ -307,6 +322,33 @@ __device__ __forceinline__ void choose64(const Gate& g, double (&c)[EPL], int la
   }
 }
 
+// The same for one token by a whole wavefront, from its logits.
+template <typename T, int EPL>
+__device__ __forceinline__ void settle(Gate g, const T* pz, const float* bias, double* values, double* group, int* chosen) {
+  const int lane = threadIdx.x & 63, e0 = lane * EPL;
+  double c[EPL], top = 0.0, inverse = 1.0;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) c[i] = e0 + i < g.nexpert ? (double)pz[e0 + i] : -INFINITY;
+  if (bias || g.groups > 1) {
+    if (!g.sigmoid) {
+      top = c[0];
+#pragma unroll
+      for (int i = 1; i < EPL; ++i) top = Larger()(top, c[i]);
+      top = across<64>(top, Larger());
+      double sum = 0.0;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) sum += exp64(c[i] - top);
+      inverse = 1.0 / across<64>(sum, Sum());
+    }
+#pragma unroll
+    for (int i = 0; i < EPL; ++i)
+      if (c[i] != -INFINITY)
+        c[i] = (g.sigmoid ? sigmoid64(c[i]) : exp64(c[i] - top) * inverse) + (bias ? (double)bias[e0 + i] : 0.0);
+  }
+  g.lanes = 0;
+  choose64<64>(g, c, lane, values, group, chosen);
+}
+
 template <typename T, int LANES, int EPL>
 __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restrict__ logits, int64_t ldl,
                                                       const float* __restrict__ bias, int* __restrict__ expert,
@@ -318,13 +360,13 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
   const int64_t t = (blockIdx.y * (int64_t)gridDim.x + blockIdx.x) * (kBlock / LANES) + threadIdx.x / LANES;
   const bool in = t < g.ntok;
   const int e0 = lane * EPL;
-  char* lds = gate_lds + (threadIdx.x >> 6) * wave_bytes(kTokens, EPL, g);
+  char* lds = gate_lds + (threadIdx.x >> 6) * wave_bytes<T>(kTokens, EPL, g);
   int* chosen = reinterpret_cast<int*>(lds) + mine * g.topk;
   lds += chosen_bytes(kTokens, g);
   double* group = reinterpret_cast<double*>(lds) + mine * g.groups;
   lds += group_bytes(kTokens, g);
   unsigned* keys = reinterpret_cast<unsigned*>(lds);
-  double* values = reinterpret_cast<double*>(lds) + mine * g.nexpert;
+  A* values = reinterpret_cast<A*>(lds) + mine * g.nexpert;
   const T* pz = logits + (in ? t : 0) * ldl;
   // with neither bias nor groups the order is that of the logits
   const bool plain = !bias && g.groups == 1;
@@ -370,8 +412,10 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
   if (__any(bad)) bad = across<LANES>((int)bad, Or());
 
   bool unsure = sizeof(T) == 8;
+  unsigned mine_key = 0;   // with fewer than LANES slots: the key of slot `lane`, and its expert
+  int mine_expert = -1;
   if constexpr (sizeof(T) != 8) {
-    unsigned key[EPL];  // 0 for what cannot be chosen
+    unsigned key[EPL];
     constexpr unsigned kLow = EPL - 1;  // a key's last bits say which expert of the lane it is
     float c[EPL];
     if (!plain) {
@@ -392,11 +436,8 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
       }
 #pragma unroll
       for (int i = 0; i < EPL; ++i) c[i] = z[i] == -INFINITY ? -INFINITY : c[i] + b[i];
-      if (g.groups > 1) {
-        bool near = false;
-        const unsigned long long kept = kept_groups<LANES>(g, c, lane, reinterpret_cast<float*>(values),
-                                                                    reinterpret_cast<float*>(group), &near);
-        unsure = near;
+      if (g.groups > 1 && !g.lanes) {
+        const unsigned long long kept = kept_groups<LANES>(g, 0.0f, 0.0f, c, lane, values, reinterpret_cast<float*>(group), &unsure);
         drop(g, kept, e0, c);
       }
     } else {
@@ -415,13 +456,14 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
           __builtin_memcpy(&h, &v, 2);
           u = h & 0x8000u ? (unsigned)(unsigned short)~h : h | 0x8000u;
         }
-        key[i] = c[i] == -INFINITY ? 0u : u << 16 | (0xffffu - (unsigned)(e0 + i));
+        key[i] = u << 16 | (0xffffu - (unsigned)(e0 + i));
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < EPL; ++i)
-        key[i] = c[i] == -INFINITY ? 0u : (ordered(c[i]) & ~kLow) | (kLow - (unsigned)i);
+      for (int i = 0; i < EPL; ++i) key[i] = (ordered(c[i]) & ~kLow) | (kLow - (unsigned)i);
     }
+    // keys up to this are those of -infinity
+    const unsigned none = whole && std::is_same_v<T, _Float16> ? 0x03ffffffu : 0x007fffffu;
     // each lane's keys in descending order (exchanges of an odd-even merge sort)
 #pragma unroll
     for (int p = 1; p < EPL; p *= 2)
@@ -436,51 +478,69 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
               key[i + j] = max(x, y);
               key[i + j + k] = min(x, y);
             }
-    // they wait in LDS: key j of this lane in place j * 64 + lane, 0 behind the last
-    unsigned* mykeys = keys + (threadIdx.x & 63);
+    unsigned head = key[0];
+    if (g.groups > 1 && g.lanes) {  // a lane's two best are its first two keys; all of it stays or none
+      const float first = key[0] > none ? number(key[0] & ~kLow) : -INFINITY;
+      const float second = key[1] > none ? number(key[1] & ~kLow) : -INFINITY;
+      const unsigned long long kept = kept_groups<LANES>(g, first, second, c, lane, values, reinterpret_cast<float*>(group), &unsure);
+      if (!(kept >> g.group_of(e0) & 1)) head = 0u;
+    }
+    // The others wait in LDS: key j + 1 of this lane in place j * 64 + lane, 0 behind
+    // the last.  The largest of all heads is the next: its lane notes whose it is and
+    // goes on to its next key.  Lane j keeps the j-th, if there are as many lanes.
+    unsigned* next = keys + (threadIdx.x & 63);
 #pragma unroll
-    for (int i = 1; i < EPL; ++i) mykeys[(i - 1) * 64] = key[i];
-    mykeys[(EPL - 1) * 64] = 0u;
-    // The largest of all heads is the next: its lane goes on to its next key.  Lane
-    // j keeps the j-th for what follows, if there are as many.
+    for (int i = 1; i < EPL; ++i) next[(i - 1) * 64] = key[i];
+    next[(EPL - 1) * 64] = 0u;
     const bool few = g.topk < LANES;
-    unsigned head = key[0], before = 0, kept = 0;
+    unsigned before = 0;
     int taken = 0, rounds = 0;
     for (int j = 0; j <= g.topk; ++j) {
       const unsigned best = across<LANES>(head, Larger());
-      if (few) kept = lane == j ? best : kept;
-      else if (!whole && j > 0) unsure |= best != 0 && close<EPL>(plain, g.sigmoid, before, best);
+      if (few) {
+        mine_key = lane == j ? best : mine_key;
+      } else if (!whole) {
+        unsure |= j > 0 && best > none && close<EPL>(plain, g.sigmoid, before, best);
+        before = best;
+      }
       if (j == g.topk) break;
-      if (head == best) {
-        chosen[j] = best == 0 ? -1 : whole ? (int)(0xffffu - (best & 0xffffu)) : e0 + (int)(kLow - (best & kLow));
-        head = mykeys[min(taken, EPL - 1) * 64];
-        taken += best != 0;
+      if (!few) {
+        rounds += best > none;
+        if (best <= none && lane == 0) chosen[j] = -1;
       }
-      rounds += best != 0;
-      before = best;
-    }
-    if (!whole) {
-      if (few && LANES > 1) {
-        const unsigned next = (unsigned)__shfl_down((int)kept, 1);
-        unsure |= lane < g.topk && next != 0 && close<EPL>(plain, g.sigmoid, kept, next);
+      if (head == best && best > none) {
+        chosen[j] = few ? e0 : whole ? (int)(0xffffu - (best & 0xffffu)) : e0 + (int)(kLow - (best & kLow));
+        head = *next;
+        next += 64;
+        ++taken;
       }
-      // equal ones in two lanes were taken at once
-      if (LANES > 1) unsure |= across<LANES>(taken, Sum()) != rounds;
     }
+    if (few) {
+      const bool live = lane < g.topk && mine_key > none;
+      wave_sync();
+      mine_expert = !live ? -1 : whole ? (int)(0xffffu - (mine_key & 0xffffu)) : chosen[lane] + (int)(kLow - (mine_key & kLow));
+      if (!whole) {
+        const unsigned after = (unsigned)__shfl_down((int)mine_key, 1);
+        unsure |= lane < g.topk && after > none && close<EPL>(plain, g.sigmoid, mine_key, after);
+        rounds = live;
+      }
+    }
+    // equal ones in two lanes were taken at once
+    if (!whole && LANES > 1) unsure |= across<LANES>(few ? taken - rounds : taken, Sum()) != (few ? 0 : rounds);
   }
 
-  // Exactly, where that did not settle it.
-  const bool all = !g.sigmoid && !g.renorm;  // the sum of all exponentials counts
+  // Exactly, where that did not settle it: the whole wavefront does such tokens one
+  // by one.  (All of the wavefront's tokens at once takes as many registers as to cost
+  // the float32 code a third of its wavefronts.)
   double inverse = 1.0;
-  const bool again = __any(unsure && in && !bad);
-  if (all || (again && !plain && !g.sigmoid)) {
+  if (!g.sigmoid && (!g.renorm || (sizeof(T) == 8 && !plain))) {  // the sum of all exponentials counts
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) sum += exp64((double)z[i] - (double)top);
     sum = across<LANES>(sum, Sum());
     inverse = sum == 0.0 ? 0.0 : 1.0 / sum;
   }
-  if (again) {
+  if constexpr (sizeof(T) == 8) {
     double c[EPL];
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
@@ -488,14 +548,27 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
       if (!plain && z[i] != -(A)INFINITY)
         c[i] = (g.sigmoid ? sigmoid64((double)z[i]) : exp64((double)z[i] - (double)top) * inverse) + (double)b[i];
     }
-    wave_sync();
-    if (g.groups > 1) {
-      const unsigned long long kept = kept_groups<LANES>(g, c, lane, values, group, nullptr);
-      drop(g, kept, e0, c);
+    choose64<LANES>(g, c, lane, values, group, chosen);
+  } else {
+    unsigned long long left = __ballot(unsure && in && !bad);
+    if (left) {
+      constexpr int WIDE = LANES * EPL > 64 ? LANES * EPL / 64 : 1;
+      wave_sync();  // keys have been read
+      const int64_t t0 = t - mine;
+      int* first_chosen = chosen - mine * g.topk;
+      do {
+        const int token = (__ffsll(left) - 1) / LANES;
+        left &= ~((~0ull >> (64 - LANES)) << token * LANES);
+        settle<T, WIDE>(g, logits + (t0 + token) * ldl, bias, reinterpret_cast<double*>(keys), group - mine * g.groups,
+                        first_chosen + token * g.topk);
+      } while (left);
+      wave_sync();
+      const bool again = across<LANES>((int)(unsure && in && !bad), Or());
+      if (again && g.topk < LANES) mine_expert = lane < g.topk ? chosen[lane] : -1;
     }
-    choose64<LANES>(g, c, lane, chosen);
   }
   wave_sync();
+  const bool few = sizeof(T) != 8 && g.topk < LANES;
 
   // weights of the chosen, a slot to a lane (and further ones if there are more)
   auto score = [&](int e) __attribute__((always_inline)) {
@@ -503,7 +576,7 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
     const double v = (double)pz[e];
     return g.sigmoid ? sigmoid64(v) : exp64(v - (double)top) * inverse;
   };
-  const int e1 = lane < g.topk ? chosen[lane] : -1;
+  const int e1 = few ? mine_expert : lane < g.topk ? chosen[lane] : -1;
   const double s1 = score(e1);
   double total = s1;
   for (int j = lane + LANES; j < g.topk; j += LANES) total += score(chosen[j]);
@@ -672,7 +745,7 @@ extern "C" int dpc_gate(void* stream, dpc_elem elem, const dpc_gate_spec* spec, 
       Gate with = g;
       const int lanes = g.per / EPL;
       with.lanes = g.per % EPL == 0 && lanes <= LANES && (lanes & (lanes - 1)) == 0 ? lanes : 0;
-      const size_t lds = wave_bytes(64 / LANES, EPL, with) * (kBlock / 64);
+      const size_t lds = wave_bytes<T>(64 / LANES, EPL, with) * (kBlock / 64);
       hipLaunchKernelGGL((gate_kernel<T, LANES, EPL>), grid_for(ntok, TOKENS), dim3(kBlock), lds,
                          static_cast<hipStream_t>(stream), with, (const T*)logits, ldl, bias, expert,
                          (typename ElemAcc<T>::type*)weight);
