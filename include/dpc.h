@@ -513,7 +513,8 @@ int dpc_gate(void* stream, dpc_elem elem, const dpc_gate_spec* spec, int ntok, c
  *   S = sum_j s_j,  ds_j = scale dw_j  or (renorm)  scale / S (dw_j - sum_i dw_i s_i / S)
  *   softmax  dz_e = s_e (ds_e - sum_j ds_j s_j),   sigmoid  dz_e = ds_e s_e (1 - s_e)
  * with ds_e summed over the slots that hold e; 0 for closed experts, and
- * everywhere where S is 0.  Slots whose expert is outside [0, nexpert), and what
+ * everywhere where S is 0 (in float64).  A token with a NaN among its z (or, in a
+ * softmax, z = +infinity) gets NaN at its open experts.  Slots whose expert is outside [0, nexpert), and what
  * dweight holds there, do not count.  Arithmetic is float32 (float64 for
  * DPC_ELEM_F64), rounded once; sums have a fixed order.
  *   dlogits  device out [ntok] rows, lddl elements apart, of logits' type

@@ -638,7 +638,10 @@ __global__ __launch_bounds__(kBlock) void gate_bwd_kernel(Gate g, const T* __res
   int slots[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) z[i] = in && e0 + i < g.nexpert ? (A)pz[e0 + i] : -(A)INFINITY;
-  scores<LANES>(g, z, s);
+  bool bad = false;  // a NaN, or in a softmax +infinity
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) bad |= __builtin_isunordered(z[i], z[i]) || (!g.sigmoid && z[i] == (A)INFINITY);
+  bad = across<LANES>((int)bad, Or());
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
     ds[i] = (A)0;
@@ -654,30 +657,56 @@ __global__ __launch_bounds__(kBlock) void gate_bwd_kernel(Gate g, const T* __res
         slots[i] += 1;
       }
   }
-  A total = (A)0, dot = (A)0;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i)
-    if (slots[i]) {
-      total += (A)slots[i] * s[i];
-      dot += ds[i] * s[i];
-    }
-  total = across<LANES>(total, Sum());
-  dot = across<LANES>(dot, Sum());
   const A scale = (A)g.scale;
-  A rest = scale * dot;  // sum of ds s
+  A rest = (A)0;  // sum of ds s
   if (g.renorm) {
-    const A mean = total == (A)0 ? (A)0 : dot / total;
+    // The shares of the chosen, from scores taken against the largest of theirs: that
+    // may be the smallest number of float32 itself, or below, where a bias or a group
+    // made the choice.
+    A top = -(A)INFINITY, high = -(A)INFINITY;  // of all and of the chosen
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) ds[i] = total == (A)0 || !slots[i] ? (A)0 : scale * ((ds[i] - (A)slots[i] * mean) / total);
-    rest = (A)0;
+    for (int i = 0; i < EPL; ++i) {
+      top = fmax(top, z[i]);
+      if (slots[i]) high = fmax(high, z[i]);
+    }
+    if (!g.sigmoid) top = across<LANES>(top, Larger());
+    high = across<LANES>(high, Larger());
+    // exp(-745.13) is where float64 ends: below, and where none is open, the sum is 0
+    const bool none = !((g.sigmoid ? high : high - top) >= (A)-745.13);
+    const A shift = g.sigmoid ? fmin(high, (A)0) : high, unit = exp(shift);
+    A share[EPL], total = (A)0, dot = (A)0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      share[i] = !slots[i] || none ? (A)0 : g.sigmoid ? (A)1 / (unit + exp(shift - z[i])) : exp(z[i] - shift);
+      if (slots[i]) {
+        total += (A)slots[i] * share[i];
+        dot += ds[i] * share[i];
+      }
+    }
+    total = across<LANES>(total, Sum());
+    dot = across<LANES>(dot, Sum());
+    const A mean = none ? (A)0 : dot / total;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      ds[i] = !slots[i] || none ? (A)0 : scale * (ds[i] - (A)slots[i] * mean);
+      s[i] = none ? (A)0 : share[i] / total;
+    }
   } else {
+    scores<LANES>(g, z, s);
+    A dot = (A)0;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) ds[i] *= scale;
+    for (int i = 0; i < EPL; ++i) {
+      if (slots[i]) dot += ds[i] * s[i];
+      ds[i] *= scale;
+    }
+    rest = scale * across<LANES>(dot, Sum());
   }
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
     if (!in || e0 + i >= g.nexpert) continue;
-    A d = g.sigmoid ? ds[i] * s[i] * ((A)1 - s[i]) : s[i] * (ds[i] - rest);
+    // 1 - sigmoid(z) is sigmoid(-z)
+    A d = g.sigmoid ? ds[i] * s[i] * ((A)1 / ((A)1 + exp(z[i]))) : s[i] * (ds[i] - rest);
+    if (bad) d = (A)NAN;
     if (z[i] == -(A)INFINITY) d = (A)0;
     dlogits[t * lddl + e0 + i] = (T)d;
   }

@@ -277,3 +277,58 @@ def test_many_tokens():
     z = z[-(1 << 30):]
     e, w = P.Gate(1, 1, "sigmoid", scale=4.0)(z)
     assert e[-1] == -1 and w[-1] == 0 and not e[:-1].any() and bool((w[:-1] == 2.0).all())
+
+
+@pytest.mark.parametrize("t", ["f64", "f32", "bf16"])
+@pytest.mark.parametrize("E,k", [(3, 2), (7, 3), (40, 6), (200, 8), (900, 8)])
+def test_gradient_where_scores_are_tiny(t, E, k):
+    """Chosen experts (a bias can choose any) whose scores are e^-90 to e^-600, below float32's smallest number: their
+    shares, and the gradient, are of order 1 all the same; and scores within e^-30 of 1."""
+    import paper_2107_02103_amd as P
+    rng = np.random.default_rng(E)
+    n = 41
+    far = rng.choice([0.0, 60.0, 90.0, 150.0, 600.0], n)[:, None]
+    base = rng.standard_normal((n, E))
+    e = np.stack([rng.permutation(E)[:k] for _ in range(n)])
+    for kind, z in (("sigmoid", base - far), ("sigmoid", base + np.minimum(far, 30.0)), ("softmax", base.copy())):
+        if kind == "softmax":
+            for i in range(n):
+                z[i, e[i]] -= far[i]                        # the others hold nearly all of the sum
+        z[5], z[6] = -2000.0, -np.inf                       # no share: the sum is 0 in float64
+        if kind == "softmax" and E > k:
+            z[5, np.setdiff1d(np.arange(E), e[5])] = 0.0
+        x = torch.from_numpy(z).to(TYPES[t]).cuda()
+        plain = x.cpu().double().numpy()
+        wt = torch.float64 if t == "f64" else torch.float32
+        dw = torch.from_numpy(rng.standard_normal((n, k))).to(wt).cuda()
+        for renorm in (True, False):
+            got = P.Gate(E, k, kind, renormalise=renorm).backward(x, torch.from_numpy(e.astype(np.int32)).cuda(), dw)
+            got = got.cpu().double().numpy()
+            want, mag = og.choose_backward(plain, e, dw.cpu().double().numpy(), kind, renorm)
+            unit = STEP["f64" if t == "f64" else "f32"]
+            size = np.abs(np.where(np.isfinite(plain), plain, 0)).max(1, keepdims=True)
+            bound = 1.001 * STEP[t] * np.abs(want) + (E + k + 64 + 2 * size) * unit * mag + LEAST[t]
+            assert (np.abs(got - want) <= bound).all(), (kind, renorm, np.abs(got - want).max())
+            if renorm and E > 3:
+                assert np.abs(want).max() > 1e-2
+
+
+def test_gradient_of_rows_with_nan_and_infinity():
+    """NaN at all open experts where the weights are NaN, zeros where there is none."""
+    import paper_2107_02103_amd as P
+    for E, k in ((3, 2), (20, 4), (200, 8)):
+        z = torch.randn(5, E, device="cuda")
+        z[:, 1] = -float("inf")
+        z[1, E // 2 + 1] = float("nan")
+        z[2, 0] = float("inf")
+        z[3] = -float("inf")
+        e = torch.tensor([[0] + list(range(2, k + 1))] * 5, dtype=torch.int32, device="cuda")
+        dw = torch.randn(5, k, device="cuda")
+        for kind in ("softmax", "sigmoid"):
+            for renorm in (True, False):
+                d = P.Gate(E, k, kind, renormalise=renorm).backward(z, e, dw)
+                assert not d[:, 1].any() and not d[3].any()
+                rest = torch.arange(E, device="cuda") != 1
+                assert d[1, rest].isnan().all()
+                assert d[2, rest].isnan().all() if kind == "softmax" else d[2].isfinite().all()
+                assert d[0].isfinite().all() and d[4].isfinite().all()
