@@ -39,6 +39,12 @@ int log2_lanes(int width, size_t es) {
 // ---------------------------------------------------------------------------
 // lookup
 // ---------------------------------------------------------------------------
+// One dimension of a launch has under 2^32 threads.
+inline dim3 rows_grid(int64_t blocks) {
+  const int64_t wide = 1 << 23;
+  return blocks <= wide ? dim3((unsigned)blocks) : dim3((unsigned)wide, (unsigned)((blocks + wide - 1) / wide));
+}
+
 constexpr int kRowsAtOnce = 4;  // rows whose loads a group of lanes has under way
 
 // Results of 192 MiB and more (with addresses and strides multiples of 16 bytes)
@@ -52,7 +58,8 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(int ntok, int nid, int wi
   constexpr int VE = Chunk<T>::kElems, R = kRowsAtOnce;
   const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1);
   const int nch = (width + VE - 1) / VE;
-  const int64_t t0 = ((((int64_t)blockIdx.x * kBlock + threadIdx.x) >> lanes_log2)) * R;
+  const int64_t block = blockIdx.y * (int64_t)gridDim.x + blockIdx.x;
+  const int64_t t0 = ((block * kBlock + threadIdx.x) >> lanes_log2) * R;
   if (t0 >= ntok) return;
   const T* px[R];
   bool live[R];
@@ -487,7 +494,7 @@ extern "C" int dpc_embed(void* stream, dpc_elem elem, int ntok, int nid, int wid
   }
   by_elem(elem, [&](auto tt) {
     typedef decltype(tt) T;
-    hipLaunchKernelGGL((once ? embed_kernel<T, true> : embed_kernel<T, false>), dim3((unsigned)((ntok + per - 1) / per)),
+    hipLaunchKernelGGL((once ? embed_kernel<T, true> : embed_kernel<T, false>), rows_grid((ntok + per - 1) / per),
                        dim3(kBlock), 0, static_cast<hipStream_t>(stream), ntok, nid, width, l, ids, (const T*)table, ldt,
                        (typename ElemAcc<T>::type)scale, (T*)y, ldy);
   });

@@ -159,3 +159,25 @@ def test_rows_past_32_bits():
     rows = torch.arange(24.0).view(3, 8) + 1
     want[2], want[0] = rows[0] + rows[1], rows[2]
     assert torch.equal(back.float().cpu(), want)
+
+
+def test_more_than_one_dimension_of_a_launch_takes():
+    """2^28 rows of 528 bytes and a gap, a wavefront to four rows: 2^32 threads and more.  (142 GB: every row is looked at.)"""
+    import paper_2107_02103_amd as P
+    torch.cuda.empty_cache()
+    n, W = (1 << 28) + 5, 264
+    if torch.cuda.mem_get_info()[0] < 190 << 30:
+        pytest.skip("needs 190 GB of free memory")
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    ids[-3], ids[n // 2] = 1, -1
+    table = torch.arange(1.0, 2 * W + 1, device="cuda").view(2, W).bfloat16()
+    y = torch.empty(n, W, dtype=torch.bfloat16, device="cuda").fill_(-1.0)
+    P.Embedding(table)(ids, out=y)
+    want, odd = table[0].view(torch.int64), []
+    for a in range(0, n, 1 << 23):
+        rows = y[a:a + (1 << 23)].view(torch.int64)
+        odd += (a + (rows != want).any(1).nonzero().flatten()).tolist()
+    assert odd == [n // 2, n - 3]
+    assert not y[n // 2].any() and torch.equal(y[n - 3], table[1])
+    del y, ids
+    torch.cuda.empty_cache()
