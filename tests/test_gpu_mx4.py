@@ -279,3 +279,11 @@ def test_narrow_layers_over_many_rows(t, m, n, k, G):
         top = 8.0 * np.sqrt(k) * float(np.abs(w).max()) * 6
         assert float(d.max()) <= 2 * (k / 128 + 12) * 2.0 ** -23 * top * np.sqrt(k) + 2.002 * STEP[ty] * float(two.nan_to_num().abs().max())
         del out, y, two, d
+
+
+@pytest.mark.parametrize("K", [7680, 7681])
+def test_long_rows_of_many_experts(K):
+    """The longest rows that a workgroup codes itself where most experts have one (the LDS of 16 of them is 64 KiB and more
+    with the sums), and longer ones."""
+    test_layers_of_experts("f32", 16, 1, 64, 40, K)
+    test_layers_of_experts("bf16", 16, 1, 64, 40, K)
