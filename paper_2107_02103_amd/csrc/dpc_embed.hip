@@ -173,6 +173,7 @@ struct Runs {
   const int* __restrict__ tok;
   const int* __restrict__ kept; // positions
   int nid, width, part, parts, slabs, lanes_log2, join_slabs, join_log2;
+  int zero_slabs, zero_wide;    // columns of the zeros of a wavefront: chunks zero_wide s and more of slab s
 };
 
 // First element of chunk c, or -1.  Widths under a chunk: element c.
@@ -202,10 +203,10 @@ __device__ __forceinline__ int64_t reaches(const int* id, int64_t n, int64_t v) 
   return lo;
 }
 
-// Zeros in the rows of the ids of [64 k, 64 k + 64) that have no token, by one
-// wavefront: each lane looks for one id.
+// Zeros in chunks [c0, c1) of the rows of the ids of [64 k, 64 k + 64) that have no
+// token, by one wavefront: each lane looks for one id.
 template <typename TD>
-__device__ __forceinline__ void absent(const Runs& r, int64_t k, int64_t n, TD* dtable, int64_t ldt) {
+__device__ __forceinline__ void absent(const Runs& r, int64_t k, int c0, int c1, int64_t n, TD* dtable, int64_t ldt) {
   constexpr int VE = Chunk<TD>::kElems;
   const int lane = threadIdx.x & 63;
   const int64_t v = k * 64 + lane;
@@ -219,8 +220,7 @@ __device__ __forceinline__ void absent(const Runs& r, int64_t k, int64_t n, TD* 
     if (r.width < VE) {
       if (lane < r.width) p[lane] = (TD)0;
     } else {
-      const int nch = (r.width + VE - 1) / VE;
-      for (int c = lane; c < nch; c += 64) zero.store(p + (c * VE < r.width - VE ? c * VE : r.width - VE));
+      for (int c = c0 + lane; c < c1; c += 64) zero.store(p + (c * VE < r.width - VE ? c * VE : r.width - VE));
     }
   }
 }
@@ -232,6 +232,7 @@ __device__ __forceinline__ void absent(const Runs& r, int64_t k, int64_t n, TD* 
 // kAtOnce rows of a part are under way at a time, whichever ids they belong to.
 // WIDE: a row takes a whole wavefront, and what is known of positions is scalar.
 constexpr int kAtOnce = 8;
+constexpr int kZeroWaves = 4096;
 
 template <typename T, typename TD, bool WIDE>
 __global__ __launch_bounds__(kBlock) void runs_kernel(Runs r, unsigned run_blocks, const T* __restrict__ dy, int64_t lddy,
@@ -240,8 +241,10 @@ __global__ __launch_bounds__(kBlock) void runs_kernel(Runs r, unsigned run_block
   constexpr int VE = Chunk<T>::kElems;
   const int64_t n = *r.kept;
   if (blockIdx.x >= run_blocks) {
-    const int64_t k = (int64_t)(blockIdx.x - run_blocks) * (kBlock / 64) + threadIdx.x / 64;
-    if (k * 64 < r.nid) absent<TD>(r, k, n, dtable, ldt);
+    const int64_t item = (int64_t)(blockIdx.x - run_blocks) * (kBlock / 64) + threadIdx.x / 64, k = item / r.zero_slabs;
+    const int nch = (r.width + Chunk<TD>::kElems - 1) / Chunk<TD>::kElems;
+    const int c0 = (int)(item % r.zero_slabs) * r.zero_wide;
+    if (k * 64 < r.nid) absent<TD>(r, k, c0, min(nch - c0, r.zero_wide) + c0, n, dtable, ldt);
     return;
   }
   const int lane = threadIdx.x & ((1 << r.lanes_log2) - 1);
@@ -534,10 +537,17 @@ extern "C" int dpc_embed_bwd(void* stream, dpc_elem elem, dpc_elem elem_d, int n
   }
   const int join_log2 = l.lanes_log2 < 3 ? l.lanes_log2 : 3;
   const int64_t join_slabs = (int64_t)l.slabs << (l.lanes_log2 - join_log2);
-  const Runs r{id, tok, left, nid, width, l.part, l.parts, l.slabs, l.lanes_log2, (int)join_slabs, join_log2};
+  // Zeros: 64 rows of ids to a wavefront, and as many of their columns as makes about
+  // kZeroWaves of them (21 float32 rows of 6,920 for 258 ids 15 us; whole rows 68).
+  const int64_t id_waves = ((int64_t)nid + 63) / 64, VE = 16 / (int64_t)elem_size(elem_d), units = (width + 64 * VE - 1) / (64 * VE);
+  const int64_t cuts = id_waves < kZeroWaves ? kZeroWaves / id_waves : 1;
+  const int64_t zero_units = (units + cuts - 1) / cuts;
+  const int zero_slabs = (int)((units + zero_units - 1) / zero_units);
+  const Runs r{id, tok, left, nid, width, l.part, l.parts, l.slabs, l.lanes_log2, (int)join_slabs, join_log2, zero_slabs,
+               (int)(zero_units * 64)};
   const int64_t threads = ((int64_t)l.parts * l.slabs) << l.lanes_log2;
   const unsigned run_blocks = (unsigned)((threads + kBlock - 1) / kBlock);
-  const unsigned absent_blocks = (unsigned)((nid + 255) / 256);
+  const unsigned absent_blocks = (unsigned)((id_waves * zero_slabs + kBlock / 64 - 1) / (kBlock / 64));
   by_elem(elem, [&](auto tt) {
     typedef decltype(tt) T;
     const auto go = [&](auto dd) {

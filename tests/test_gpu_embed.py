@@ -181,3 +181,18 @@ def test_more_than_one_dimension_of_a_launch_takes():
     assert not y[n // 2].any() and torch.equal(y[n - 3], table[1])
     del y, ids
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n,V,W", [(21, 258, 6920), (1, 64, 5003), (3, 65, 2051), (200, 130, 257), (5, 3000, 1029), (2, 70000, 260)])
+def test_wide_rows_of_ids_without_tokens(n, V, W):
+    """Rows of zeros that several wavefronts write, in every pair of types, with a gap behind each row."""
+    import paper_2107_02103_amd as P
+    rng = np.random.default_rng(V)
+    ids = torch.from_numpy(rng.integers(0, V, n).astype(np.int32)).cuda()
+    for t, td in ((torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32),
+                  (torch.float64, torch.float64), (torch.float64, torch.float32)):
+        dy = torch.from_numpy(rng.integers(-4, 5, (n, W))).cuda().to(t)         # sums are exact
+        out = torch.full((V, W + 1), 7.0, dtype=td, device="cuda")
+        P.Embedding.gradient(ids, dy, V, dtype=td, out=out[:, :W])
+        want = torch.zeros(V, W, dtype=torch.float64, device="cuda").index_add_(0, ids.long(), dy.double())
+        assert torch.equal(out[:, :W].double(), want) and (out[:, W] == 7.0).all()
