@@ -272,27 +272,45 @@ __global__ __launch_bounds__(kBlock) void runs_kernel(Runs r, unsigned run_block
       write_row<double>(partial + ((int64_t)part * 2 + (open_left ? 0 : 1)) * r.width, at, narrow, sum, 1.0);
     }
   };
-  for (int64_t p = p0; p < p1; p += kAtOnce) {
+  // The rows behind these are on their way while these are added, and the ids behind
+  // those while they are.
+  struct Ids {
     int id[kAtOnce], tok[kAtOnce];
+  };
+  auto look = [&](int64_t p, Ids& to) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
       const int64_t q = p + k < p1 ? p + k : p1 - 1;
-      id[k] = r.id[q];
-      tok[k] = r.tok[q];
+      to.id[k] = r.id[q];
+      to.tok[k] = r.tok[q];
     }
-    Chunk<T> ch[kAtOnce];
+  };
+  auto fetch = [&](const Ids& of, Chunk<T> (&to)[kAtOnce]) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      const T* px = dy + (int64_t)tok[k] * lddy + max(at, 0);
-      if (narrow) ch[k].v[0] = px[0];
-      else ch[k].load(px);
+      const T* px = dy + (int64_t)of.tok[k] * lddy + max(at, 0);
+      if (narrow) to[k].v[0] = px[0];
+      else to[k].load(px);
+    }
+  };
+  Ids now, next;
+  Chunk<T> ch[kAtOnce], behind[kAtOnce];
+  look(p0, now);
+  fetch(now, ch);
+  if (p0 + kAtOnce < p1) look(p0 + kAtOnce, next);
+  for (int64_t p = p0; p < p1; p += kAtOnce) {
+    const bool more = p + kAtOnce < p1;
+    Ids later;
+    if (more) {
+      fetch(next, behind);
+      look(min(p + 2 * kAtOnce, p1 - 1), later);
     }
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
       if (p + k >= p1) break;
-      if (id[k] != cur) {
+      if (now.id[k] != cur) {
         flush(p + k);
-        cur = id[k];
+        cur = now.id[k];
 #pragma unroll
         for (int i = 0; i < VE; ++i) sum[i] = 0.0;
       }
@@ -300,16 +318,23 @@ __global__ __launch_bounds__(kBlock) void runs_kernel(Runs r, unsigned run_block
       for (int i = 0; i < VE; ++i)
         if (i == 0 || !narrow) sum[i] += (double)ch[k].v[i];
     }
+    if (more) {
+      now = next;
+      next = later;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) ch[k] = behind[k];
+    }
   }
   flush(p1);
 }
 
 // Sums of the runs that cross parts, 2^join_log2 chunks of a row at a time.  A
 // group of lanes looks at the part where such a run starts; of up to kAlone parts
-// it joins them itself, longer ones are joined by the whole workgroup, one after
-// the other.  Few columns to a workgroup: a run of hundreds of parts would take the
-// CU's whole bandwidth else (331,776 rows of 960 bytes for 2 ids: whole rows 56 us).
-constexpr int kJoinBlock = 1024, kAlone = 64;
+// it joins them itself, of up to kLong all groups of its wavefront do, longer ones
+// are joined by the whole workgroup, one after the other.  Few columns to a
+// workgroup: a run of hundreds of parts would take the CU's whole bandwidth else
+// (331,776 rows of 960 bytes for 2 ids: whole rows 56 us).
+constexpr int kJoinBlock = 1024, kAlone = 8, kLong = 512;
 
 // Partial sums of parts first, first + step, ... up to last; the run starts in `part`.
 template <int VE, bool NARROW>
@@ -354,6 +379,7 @@ __global__ __launch_bounds__(kJoinBlock) void join_kernel(Runs r, double scale, 
   const int slab = (int)(item / r.parts), part = (int)(item % r.parts);
   const int at = slab < r.join_slabs ? chunk_at<T>(r, (slab << r.join_log2) + lane) : -1;
   const int64_t p0 = (int64_t)part * r.part, p1 = p0 + r.part;
+  int mine = part;  // last part of the run that starts in `part` and goes on, if one does
   if (slab < r.join_slabs && p1 < n) {
     const int v = r.id[p1 - 1];
     if (r.id[p1] == v && (p0 == 0 || r.id[p0 - 1] != v)) {  // starts here and goes on
@@ -375,19 +401,36 @@ __global__ __launch_bounds__(kJoinBlock) void join_kernel(Runs r, double scale, 
         past = yes < lanes ? cut(yes) : past;
         last = yes > 0 ? cut(yes - 1) : last;
       }
-      if (last - part >= kAlone) {
+      mine = last;
+      if (last - part >= kLong) {
         if (lane == 0) {
           int* entry = list[atomicAdd(&listed, 1)];
           entry[0] = sub;
           entry[1] = last;
           entry[2] = v;
         }
-      } else if (at >= 0) {
+      } else if (at >= 0 && last - part < kAlone) {
         double sum[VE];
         add(part, part, 1, last, at, sum);
         write_row<TD>(dtable + v * ldt, at, narrow, sum, scale);
       }
     }
+  }
+  // runs of some length: every group of the wavefront, one after the other
+  const int wave_subs = 64 >> r.join_log2;
+  for (unsigned long long left = __ballot(lane == 0 && mine - part >= kAlone && mine - part < kLong); left; left &= left - 1) {
+    const int from = __ffsll(left) - 1;
+    const int first = __shfl(part, from), last = __shfl(mine, from), at_it = __shfl(at, from + lane);
+    double sum[VE];
+    if (at_it >= 0) add(first, first + ((threadIdx.x & 63) >> r.join_log2), wave_subs, last, at_it, sum);
+    else
+#pragma unroll
+      for (int i = 0; i < VE; ++i) sum[i] = 0.0;
+    for (int m = 1 << r.join_log2; m < 64; m <<= 1)
+#pragma unroll
+      for (int i = 0; i < VE; ++i) sum[i] += __shfl_xor(sum[i], m);
+    if ((int)(threadIdx.x & 63) < 1 << r.join_log2 && at_it >= 0)
+      write_row<TD>(dtable + (int64_t)r.id[(int64_t)last * r.part] * ldt, at_it, narrow, sum, scale);
   }
   __syncthreads();
   for (int l = 0; l < listed; ++l) {
@@ -536,7 +579,8 @@ extern "C" int dpc_embed_bwd(void* stream, dpc_elem elem, dpc_elem elem_d, int n
     left = kept;
   }
   const int join_log2 = l.lanes_log2 < 3 ? l.lanes_log2 : 3;
-  const int64_t join_slabs = (int64_t)l.slabs << (l.lanes_log2 - join_log2);
+  const int chunk = (int)(16 / elem_size(elem)), nch = width < chunk ? width : (width + chunk - 1) / chunk;
+  const int64_t join_slabs = ((int64_t)nch + (1 << join_log2) - 1) >> join_log2;
   // Zeros: 64 rows of ids to a wavefront, and as many of their columns as makes about
   // kZeroWaves of them (21 float32 rows of 6,920 for 258 ids 15 us; whole rows 68).
   const int64_t id_waves = ((int64_t)nid + 63) / 64, VE = 16 / (int64_t)elem_size(elem_d), units = (width + 64 * VE - 1) / (64 * VE);
@@ -557,7 +601,7 @@ extern "C" int dpc_embed_bwd(void* stream, dpc_elem elem, dpc_elem elem_d, int n
                          dim3(run_blocks + absent_blocks), dim3(kBlock), 0, s, r, run_blocks, (const T*)dy, lddy, scale,
                          partial, (TD*)dtable, lddt);
       if (l.parts > 1)
-        hipLaunchKernelGGL((join_kernel<T, TD>), dim3((unsigned)((threads + kJoinBlock - 1) / kJoinBlock)), dim3(kJoinBlock),
+        hipLaunchKernelGGL((join_kernel<T, TD>), dim3((unsigned)((((l.parts * join_slabs) << join_log2) + kJoinBlock - 1) / kJoinBlock)), dim3(kJoinBlock),
                            0, s, r, scale, partial, (TD*)dtable, lddt);
     };
     if (elem_d == elem) go(T{});

@@ -196,3 +196,26 @@ def test_wide_rows_of_ids_without_tokens(n, V, W):
         P.Embedding.gradient(ids, dy, V, dtype=td, out=out[:, :W])
         want = torch.zeros(V, W, dtype=torch.float64, device="cuda").index_add_(0, ids.long(), dy.double())
         assert torch.equal(out[:, :W].double(), want) and (out[:, W] == 7.0).all()
+
+
+@pytest.mark.parametrize("t", ["f64", "f32", "bf16"])
+@pytest.mark.parametrize("W", [1, 3, 9, 40, 240, 500, 1600])
+def test_runs_of_every_length(t, W):
+    """Ids with as many tokens as end in the middle of one part, or cross 2 to 600 of them (parts are 8 to 1,024 rows
+    long): whoever joins their sums."""
+    import paper_2107_02103_amd as P
+    for seed, longest, n in ((0, 40, 3000), (1, 600, 20000), (2, 9000, 60000), (3, 70000, 150000)):
+        if n * W > 100_000_000:
+            continue
+        rng = np.random.default_rng(seed + W)
+        lengths = []
+        while sum(lengths) < n:
+            lengths.append(int(np.exp(rng.uniform(0, np.log(longest)))))
+        ids = np.repeat(np.arange(len(lengths)), lengths)[:n].astype(np.int32)
+        V = int(ids[-1]) + 1
+        keep = rng.permutation(n)
+        ids = torch.from_numpy(ids[keep]).cuda()
+        dy = torch.from_numpy(rng.integers(-1, 2, (n, W)).astype(np.float32)).cuda().to(TYPES[t])   # sums are exact
+        out = P.Embedding.gradient(ids, dy, V, dtype=torch.float32 if t == "bf16" else None)
+        want = torch.zeros(V, W, dtype=torch.float64, device="cuda").index_add_(0, ids.long(), dy.double())
+        assert torch.equal(out.double(), want), (seed, (out.double() != want).any(1).nonzero()[:4])
