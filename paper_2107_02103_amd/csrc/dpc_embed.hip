@@ -9,9 +9,9 @@
 // parts.  A group of lanes sums the runs of its part, in order and in float64; a
 // run inside one part is written out, of a run that crosses into another part both
 // keep the sum of their piece, which a second kernel joins.  331,776 float32 rows of
-// 240 for 2 ids 86 us: sort 13, runs 63 (the rows at 5 TB/s), joins 10; 16,384 bfloat16
-// rows of 4,096 for 65,536 ids 193: sort 31, runs and zeros 144 (671 MB at 4.7 TB/s),
-// joins 18.
+// 240 for 2 ids 76 us: sort 11, runs 61 (the rows at 5.2 TB/s), joins 11 (the kernels
+// one by one); 16,384 bfloat16 rows of 4,096 for 65,536 ids 174: sort 29, runs and zeros
+// 132 (671 MB at 5.1 TB/s), joins 14.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -230,15 +230,19 @@ __device__ __forceinline__ void absent(const Runs& r, int64_t k, int c0, int c1,
 // partial sums: [parts][2][width], 0: the run that comes from the part before,
 // 1: a run that starts here and goes on.
 // kAtOnce rows of a part are under way at a time, whichever ids they belong to.
-// WIDE: a row takes a whole wavefront, and what is known of positions is scalar.
+// KIND kNarrow: rows of less than a chunk, an element to a lane (a branch inside would
+// cut the loads of chunks in pieces: 494,073 float16 rows of 240 take 133 us for 58 then); kWide:
+// a row takes a whole wavefront, and what is known of positions is scalar.
+enum Kind { kNarrow, kChunks, kWide };
 constexpr int kAtOnce = 8;
 constexpr int kZeroWaves = 4096;
 
-template <typename T, typename TD, bool WIDE>
+template <typename T, typename TD, Kind KIND>
 __global__ __launch_bounds__(kBlock) void runs_kernel(Runs r, unsigned run_blocks, const T* __restrict__ dy, int64_t lddy,
                                                       double scale, double* __restrict__ partial,
                                                       TD* __restrict__ dtable, int64_t ldt) {
   constexpr int VE = Chunk<T>::kElems;
+  constexpr bool WIDE = KIND == kWide, narrow = KIND == kNarrow;
   const int64_t n = *r.kept;
   if (blockIdx.x >= run_blocks) {
     const int64_t item = (int64_t)(blockIdx.x - run_blocks) * (kBlock / 64) + threadIdx.x / 64, k = item / r.zero_slabs;
@@ -256,7 +260,6 @@ __global__ __launch_bounds__(kBlock) void runs_kernel(Runs r, unsigned run_block
   const int64_t p0 = (int64_t)part * r.part, p1 = min(n, p0 + r.part);
   const int at = chunk_at<T>(r, (slab << r.lanes_log2) + lane);
   if (p0 >= p1 || (!WIDE && at < 0)) return;
-  const bool narrow = r.width < VE;
   const int before = p0 > 0 ? r.id[p0 - 1] : -1, after = p1 < n ? r.id[p1] : -1;
   double sum[VE];
 #pragma unroll
@@ -289,7 +292,7 @@ __global__ __launch_bounds__(kBlock) void runs_kernel(Runs r, unsigned run_block
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
       const T* px = dy + (int64_t)of.tok[k] * lddy + max(at, 0);
-      if (narrow) to[k].v[0] = px[0];
+      if constexpr (narrow) to[k].v[0] = px[0];
       else to[k].load(px);
     }
   };
@@ -334,7 +337,7 @@ __global__ __launch_bounds__(kBlock) void runs_kernel(Runs r, unsigned run_block
 // are joined by the whole workgroup, one after the other.  Few columns to a
 // workgroup: a run of hundreds of parts would take the CU's whole bandwidth else
 // (331,776 rows of 960 bytes for 2 ids: whole rows 56 us).
-constexpr int kJoinBlock = 1024, kAlone = 8, kLong = 512;
+constexpr int kJoinBlock = 512, kAlone = 8, kLong = 512;
 
 // Partial sums of parts first, first + step, ... up to last; the run starts in `part`.
 template <int VE, bool NARROW>
@@ -469,11 +472,12 @@ Layout layout_for(dpc_elem elem, int ntok, int nid, int width) {
   l.lanes_log2 = log2_lanes(width, elem_size(elem));
   const int VE = (int)(16 / elem_size(elem)), nch = width < VE ? width : (width + VE - 1) / VE;
   l.slabs = (int)(((int64_t)nch + (1 << l.lanes_log2) - 1) >> l.lanes_log2);
-  // About 4,096 wavefronts in all; 1,536 where ids have many tokens, since of long
-  // runs every part is read again when they are joined (331,776 rows of 960 bytes
-  // of 2 ids 95 and 89 us).  8 to 1,024 rows to a part, 32 and more where a row takes a wavefront.
+  // About 4,096 wavefronts in all; 2,048, two to a SIMD, where ids have many tokens,
+  // since of long runs every part is read again when they are joined (runs and joins
+  // of 494,073 float16 rows of 240 for 21 ids 85 us; with 1,536 wavefronts 93, with 3,072
+  // 88).  8 to 1,024 rows to a part, 32 and more where a row takes a wavefront.
   const int lanes = 1 << l.lanes_log2, least = lanes / 2 < 8 ? 8 : lanes / 2;
-  const int64_t all = (int64_t)(ntok / nid >= 256 ? 1536 : 4096) * 64;
+  const int64_t all = (int64_t)(ntok / nid >= 256 ? 2048 : 4096) * 64;
   const int64_t part = ((int64_t)ntok * l.slabs * lanes + all - 1) / all;
   l.part = (int)(part < least ? least : part > 1024 ? 1024 : part);
   l.parts = (int)(((int64_t)ntok + l.part - 1) / l.part);
@@ -578,7 +582,8 @@ extern "C" int dpc_embed_bwd(void* stream, dpc_elem elem, dpc_elem elem_d, int n
     tok = job.to_tok;
     left = kept;
   }
-  const int join_log2 = l.lanes_log2 < 3 ? l.lanes_log2 : 3;
+  const int most_log2 = elem_size(elem) == 8 ? 3 : 2;
+  const int join_log2 = l.lanes_log2 < most_log2 ? l.lanes_log2 : most_log2;
   const int chunk = (int)(16 / elem_size(elem)), nch = width < chunk ? width : (width + chunk - 1) / chunk;
   const int64_t join_slabs = ((int64_t)nch + (1 << join_log2) - 1) >> join_log2;
   // Zeros: 64 rows of ids to a wavefront, and as many of their columns as makes about
@@ -597,7 +602,9 @@ extern "C" int dpc_embed_bwd(void* stream, dpc_elem elem, dpc_elem elem_d, int n
     const auto go = [&](auto dd) {
       typedef decltype(dd) TD;
       double* partial = reinterpret_cast<double*>(ws + l.partial);
-      hipLaunchKernelGGL((l.lanes_log2 == 6 ? runs_kernel<T, TD, true> : runs_kernel<T, TD, false>),
+      hipLaunchKernelGGL((width < Chunk<T>::kElems ? runs_kernel<T, TD, kNarrow>
+                          : l.lanes_log2 == 6        ? runs_kernel<T, TD, kWide>
+                                                     : runs_kernel<T, TD, kChunks>),
                          dim3(run_blocks + absent_blocks), dim3(kBlock), 0, s, r, run_blocks, (const T*)dy, lddy, scale,
                          partial, (TD*)dtable, lddt);
       if (l.parts > 1)

@@ -7,8 +7,8 @@
 // A part is what one wavefront walks, 64 slots at a time: lanes with the same
 // key find each other by one ballot per bit of the key, and their rank is the
 // number of such lanes below.  No atomics: the order is the same on every call.
-// Bound by latency: 3 us for a few slots, 14 us for 331,776 of 2 keys in two
-// launches, 17 us for 16,384 of 256 keys.
+// Bound by latency: 3 us for a few slots, 11 us for 331,776 of 2 keys in two
+// launches, 15 us for 16,384 of 256 keys.
 //
 // A job has
 //   kPart                            slots of a workgroup, at least (constexpr int)
@@ -220,10 +220,16 @@ __global__ __launch_bounds__(64 * kPlanWaves) void plan_place_kernel(int64_t nsl
       const int e = e0 + threadIdx.x / lanes;
       int all = 0, before = 0;
       if (e < nkey) {
-        for (int b = lane; b < blocks; b += lanes) {
-          const int h = hist[(int64_t)e * blocks + b];
-          all += h;
-          before += b < (int)blockIdx.x ? h : 0;
+        for (int b0 = lane; b0 < blocks; b0 += 8 * lanes) {
+          int h[8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) h[u] = hist[(int64_t)e * blocks + min(b0 + u * lanes, blocks - 1)];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const int b = b0 + u * lanes;
+            all += b < blocks ? h[u] : 0;
+            before += b < (int)blockIdx.x ? h[u] : 0;  // one of the blocks
+          }
         }
       }
       for (int m = lanes >> 1; m; m >>= 1) {
