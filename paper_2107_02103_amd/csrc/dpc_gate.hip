@@ -657,49 +657,56 @@ __global__ __launch_bounds__(kBlock) void gate_bwd_kernel(Gate g, const T* __res
         slots[i] += 1;
       }
   }
-  const A scale = (A)g.scale;
-  A rest = (A)0;  // sum of ds s
+  scores<LANES>(g, z, s);
+  A total = (A)0, dot = (A)0;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    ds[i] *= (A)g.scale;
+    if (!slots[i]) continue;
+    total += (A)slots[i] * s[i];
+    dot += ds[i] * s[i];
+  }
+  dot = across<LANES>(dot, Sum());
+  A rest = dot;  // sum of ds s
   if (g.renorm) {
-    // The shares of the chosen, from scores taken against the largest of theirs: that
-    // may be the smallest number of float32 itself, or below, where a bias or a group
-    // made the choice.
-    A top = -(A)INFINITY, high = -(A)INFINITY;  // of all and of the chosen
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      top = fmax(top, z[i]);
-      if (slots[i]) high = fmax(high, z[i]);
-    }
-    if (!g.sigmoid) top = across<LANES>(top, Larger());
-    high = across<LANES>(high, Larger());
-    // exp(-745.13) is where float64 ends: below, and where none is open, the sum is 0
-    const bool none = !((g.sigmoid ? high : high - top) >= (A)-745.13);
-    const A shift = g.sigmoid ? fmin(high, (A)0) : high, unit = exp(shift);
-    A share[EPL], total = (A)0, dot = (A)0;
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      share[i] = !slots[i] || none ? (A)0 : g.sigmoid ? (A)1 / (unit + exp(shift - z[i])) : exp(z[i] - shift);
-      if (slots[i]) {
-        total += (A)slots[i] * share[i];
-        dot += ds[i] * share[i];
-      }
-    }
     total = across<LANES>(total, Sum());
-    dot = across<LANES>(dot, Sum());
+    const bool tiny = total < (A)(sizeof(A) == 8 ? 0x1p-900 : 0x1p-100);
+    if (__any(tiny)) {
+      // Scores at the smallest numbers or below, as a bias or a group may choose
+      // them: taken against the largest of theirs, since shares are all that counts.
+      A top = -(A)INFINITY, high = -(A)INFINITY;  // of all and of the chosen
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        top = fmax(top, z[i]);
+        if (slots[i]) high = fmax(high, z[i]);
+      }
+      if (!g.sigmoid) top = across<LANES>(top, Larger());
+      high = across<LANES>(high, Larger());
+      // exp(-745.13) is where float64 ends: below, and where none is open, the sum is 0
+      const bool some = (g.sigmoid ? high : high - top) >= (A)-745.13;
+      const A unit = exp(g.sigmoid ? high : (A)0);
+      A sum = (A)0, part = (A)0;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        if (!slots[i]) continue;
+        if (tiny) s[i] = !some ? (A)0 : g.sigmoid ? (A)1 / (unit + exp(high - z[i])) : exp(z[i] - high);
+        sum += (A)slots[i] * s[i];
+        part += ds[i] * s[i];
+      }
+      sum = across<LANES>(sum, Sum());
+      part = across<LANES>(part, Sum());
+      total = tiny ? sum : total;
+      dot = tiny ? part : dot;
+    }
+    const bool none = total == (A)0;
     const A mean = none ? (A)0 : dot / total;
+    rest = (A)0;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
-      ds[i] = !slots[i] || none ? (A)0 : scale * (ds[i] - (A)slots[i] * mean);
-      s[i] = none ? (A)0 : share[i] / total;
+      ds[i] = none || !slots[i] ? (A)0 : (ds[i] - (A)slots[i] * mean) / total;
+      if (slots[i]) rest += ds[i] * s[i];
     }
-  } else {
-    scores<LANES>(g, z, s);
-    A dot = (A)0;
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      if (slots[i]) dot += ds[i] * s[i];
-      ds[i] *= scale;
-    }
-    rest = scale * across<LANES>(dot, Sum());
+    rest = tiny ? (A)0 : across<LANES>(rest, Sum());  // 0 but for roundings
   }
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
