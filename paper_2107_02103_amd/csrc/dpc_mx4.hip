@@ -374,7 +374,8 @@ void launch_few(hipStream_t s, const Product& p, const TX* x, int64_t ldx, TY* y
 // the reads 140, with their loads 176: the largest tile's reads (1,536 clocks a step),
 // loads (512) and products (2,048) overlap in part.  Tried without gain: reads in the
 // order of use one to three fragments ahead (287 to 292), the next half step's while
-// this one is multiplied (451: spills), four wavefronts of 128 x 128 (297), 64 x 128 (398).
+// this one is multiplied (451: spills), four wavefronts of 128 x 128 (297), 64 x 128 (398),
+// workgroups that go on to their next tile with its first step under way (298: spills).
 template <typename TY, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, int col_tiles, TY* __restrict__ y,
                                                                      int64_t ldy) {
