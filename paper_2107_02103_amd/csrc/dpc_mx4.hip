@@ -370,9 +370,8 @@ void launch_few(hipStream_t s, const Product& p, const TX* x, int64_t ldx, TY* y
 //
 // 8192 x 8192 x 8192 in 254 to 290 us (3.8 to 4.3e15 operations a second, the more the
 // cooler the card; random codes in registers alone 7.2e15), 32,768 rows for 16 experts'
-// 4096 x 4096 in 345 to 400.  Of 285 us the products alone take 196, with LDS reads 240;
-// the reads 140, with their loads 176: the largest tile's reads (1,536 clocks a step),
-// loads (512) and products (2,048) overlap in part.  Tried without gain: reads in the
+// 4096 x 4096 in 345 to 400.  Of 285 us the products alone take 196: the largest tile's
+// reads (1,024 clocks a step), loads (512) and products (2,048) overlap in part.  Tried without gain: reads in the
 // order of use one to three fragments ahead (287 to 292), the next half step's while
 // this one is multiplied (451: spills), four wavefronts of 128 x 128 (297), 64 x 128 (398),
 // workgroups that go on to their next tile with its first step under way (298: spills).
