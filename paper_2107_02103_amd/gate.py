@@ -105,40 +105,57 @@ def _ids(ids):
 class Embedding:
     """A vector for each id (the species of an atom, a token), times a scale.
 
-    table  [ids, width], rows of any stride
+    table  [ids, width], rows of any stride; another one may take its place
     An id outside [0, ids) stands for nothing: its vector is zeros, and it has no
     part in the gradient."""
 
     def __init__(self, table, scale=1.0):
-        self._ld = _rows(table, "table")
         self.table, self.scale = table, float(scale)
-        self.ids, self.width = table.shape
-        self._device, self._elem = table.get_device(), _elem_of(table.dtype)
-        if self.ids > _MOST or self.width > _MOST:
+        self._read(table)
+
+    @staticmethod
+    def _read(table):
+        """Device, element type and row stride of a table, as it is now: a table may be
+        exchanged, or changed in place (as .data of a parameter is)."""
+        ld, elem = _rows(table, "table"), _elem_of(table.dtype)
+        ids, width = table.shape
+        if ids > _MOST or width > _MOST:
             _too_large("dpc_embed")
+        return table.get_device(), elem, ld, ids, width
+
+    @property
+    def ids(self):
+        return self.table.shape[0]
+
+    @property
+    def width(self):
+        return self.table.shape[1]
 
     def __call__(self, ids, out=None, stream=None):
         """[tokens, width] of ids int32 [tokens]."""
-        if stream is not None or _current_device() != self._device:
-            with _enter(self._device, stream):
+        table = self.table
+        dev, elem, ld, nid, width = self._read(table)
+        if stream is not None or _current_device() != dev:
+            with _enter(dev, stream):
                 return self(ids, out)
-        if _ids(ids) != self._device:
-            _on(ids, self._device, "ids")
+        if _ids(ids) != dev:
+            _on(ids, dev, "ids")
         n = ids.shape[0]
         if out is None:
-            out, ldy = self.table.new_empty((n, self.width)), self.width or 1
+            out, ldy = table.new_empty((n, width)), width or 1
         else:
-            ldy = _rows(out, "out", n, self.width, self.table.dtype, self._device)
-        _check(_lib.dpc_embed(_raw_stream(self._device), self._elem, n, self.ids, self.width, ids.data_ptr(),
-                              self.table.data_ptr(), self._ld, self.scale, out.data_ptr(), ldy), "dpc_embed")
+            ldy = _rows(out, "out", n, width, table.dtype, dev)
+        _check(_lib.dpc_embed(_raw_stream(dev), elem, n, nid, width, ids.data_ptr(), table.data_ptr(), ld, self.scale,
+                              out.data_ptr(), ldy), "dpc_embed")
         return out
 
     def backward(self, ids, dy, dtype=None, out=None, stream=None):
         """dE/dtable from dE/dy (see gradient)."""
-        if dy.dim() != 2 or dy.shape[1] != self.width:
-            raise ValueError(f"dy has shape {tuple(dy.shape)}, expected [tokens, {self.width}]")
-        _on(dy, self._device, "dy")
-        return Embedding.gradient(ids, dy, self.ids, self.scale, dtype, out, stream)
+        nid, width = self.table.shape
+        if dy.dim() != 2 or dy.shape[1] != width:
+            raise ValueError(f"dy has shape {tuple(dy.shape)}, expected [tokens, {width}]")
+        _on(dy, self.table.get_device(), "dy")
+        return Embedding.gradient(ids, dy, nid, self.scale, dtype, out, stream)
 
     @staticmethod
     def gradient(ids, dy, nid, scale=1.0, dtype=None, out=None, stream=None):

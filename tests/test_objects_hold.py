@@ -1,0 +1,92 @@
+"""What an object was given may be replaced or changed afterwards: a call goes by what
+is there when it is made, or refuses it.  Without a GPU: descriptions of tensors, and
+a recorder for a library."""
+import contextlib
+
+import pytest
+
+import paper_2107_02103_amd as P
+from paper_2107_02103_amd import binding as B
+from tests.test_experts_device import GPU, Tensor
+
+torch = pytest.importorskip("torch")
+I32, F16, F64 = torch.int32, torch.float16, torch.float64
+
+
+class Rows(Tensor):
+    """Rows with a gap behind each, or (contiguous=False) an array that is not in one piece."""
+
+    def __init__(self, shape, dtype=torch.float32, gpu=GPU, gap=0, contiguous=True):
+        super().__init__(shape, dtype, gpu)
+        self.gap, self.contiguous_ = gap, contiguous
+
+    def stride(self):
+        return (self.shape[1] + self.gap, 1)
+
+    def is_contiguous(self):
+        return self.contiguous_
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The calls that reach the library, with their arguments."""
+    import paper_2107_02103_amd.gate as G
+    made, current = [], [GPU]
+
+    @contextlib.contextmanager
+    def device(d):
+        before, current[0] = current[0], d
+        try:
+            yield
+        finally:
+            current[0] = before
+
+    class Lib:
+        def __getattr__(self, name):
+            def call(*args):
+                if name.endswith("workspace_bytes"):
+                    return 256
+                made.append((name,) + args)
+                return 0
+            return call
+
+    for module in (G,):
+        monkeypatch.setattr(module, "_lib", Lib())
+        monkeypatch.setattr(module, "_raw_stream", lambda d: 0)
+        monkeypatch.setattr(module, "_current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", device)
+    return made
+
+
+def test_an_embedding_reads_the_table_that_it_has(calls):
+    """The library is told the shape, type and stride of the table in place, not those of the first."""
+    emb, ids = P.Embedding(Rows((300, 64))), Tensor((4,), I32)
+    for table in (Rows((3, 64)), Rows((300, 64), F16), Rows((300, 8)), Rows((300, 64), gap=8), Rows((7, 5), F64)):
+        emb.table = table
+        calls.clear()
+        out = emb(ids)
+        name, _, elem, n, nid, width, _, _, ldt = calls[0][:9]
+        assert (name, n, nid, width, elem, ldt) == ("dpc_embed", 4, *table.shape, B.elem_of(table.dtype), table.stride()[0])
+        assert out.shape == (4, table.shape[1]) and out.dtype == table.dtype
+        assert (emb.ids, emb.width) == table.shape
+        emb.backward(ids, Tensor((4, emb.width), table.dtype))
+        assert calls[1][4:7] == (4, *table.shape)
+
+
+def test_an_embedding_refuses_a_table_that_no_constructor_takes(calls):
+    emb, ids = P.Embedding(Rows((300, 64))), Tensor((4,), I32)
+    for table, error in ((Rows((300, 64), I32), TypeError), (Tensor((300,)), ValueError), (Rows((300, 64), gap=-1), ValueError),
+                         (torch.zeros(300, 64), ValueError), (Rows((300, 64), gpu=0), ValueError)):
+        emb.table = table
+        with pytest.raises(error):
+            emb(ids)                                # the ids are on GPU 1
+    assert not calls
+
+
+def test_an_embedding_sees_a_table_changed_in_place(calls):
+    """As .data of a parameter is exchanged when its module goes to another type."""
+    table = Rows((300, 64))
+    emb = P.Embedding(table)
+    table.shape, table.dtype = (10, 6), F16
+    emb(Tensor((4,), I32))
+    assert calls[0][2] == B.DPC_ELEM_F16 and calls[0][4:6] == (10, 6) and calls[0][8] == 6
