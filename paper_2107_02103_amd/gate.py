@@ -2,8 +2,6 @@
 vectors of ids.  As Route's, their methods check arguments and allocate outputs;
 all arithmetic happens in libdpc, and no call is recorded for torch's autograd:
 gradients are methods of their own."""
-import ctypes as C
-
 import torch
 
 from . import binding as B
@@ -19,7 +17,8 @@ class Gate:
     nexpert, topk  experts, and how many of them a token is sent to
     score          "softmax" or "sigmoid" of the logits
     bias           float32 [nexpert] or None: added to the scores for the choice
-                   alone, as what balances the experts' loads
+                   alone, as what balances the experts' loads; another one may
+                   take its place between calls
     groups, keep, best  the experts stand in `groups` groups of equal size, of
                    which a token keeps the `keep` with the largest sum of their
                    `best` (1 or 2) largest biased scores
@@ -34,17 +33,25 @@ class Gate:
         for v in (nexpert, topk, groups, keep, best):
             if not -_MOST <= v <= _MOST:
                 _too_large("dpc_gate")
-        self.nexpert, self.topk = int(nexpert), int(topk)
-        if bias is not None:
-            if bias.dtype != torch.float32 or bias.shape != (self.nexpert,) or not bias.is_contiguous():
-                raise ValueError("bias must be contiguous float32 [nexpert]")
-            _on(bias, None, "bias")
+        self.spec = _Spec(int(nexpert), int(topk), _SCORES[score], int(groups), int(keep), int(best), bool(renormalise), scale)
         self.bias = bias
-        self.spec = _Spec(self.nexpert, self.topk, _SCORES[score], int(groups), int(keep), int(best), bool(renormalise), scale)
-        self._spec = C.byref(self.spec)
+        self._bias(None)
+
+    nexpert = property(lambda self: self.spec.nexpert)
+    topk = property(lambda self: self.spec.topk)
+
+    def _bias(self, dev):
+        """Address of the bias, which may be another than the constructor's."""
+        bias = self.bias
+        if bias is None:
+            return None
+        if bias.dtype != torch.float32 or bias.shape != (self.spec.nexpert,) or not bias.is_contiguous():
+            raise ValueError("bias must be contiguous float32 [nexpert]")
+        _on(bias, dev, "bias")
+        return bias.data_ptr()
 
     def _logits(self, logits, dev):
-        ld = _rows(logits, "logits", None, self.nexpert, None, dev)
+        ld = _rows(logits, "logits", None, self.spec.nexpert, None, dev)
         if logits.shape[0] > _MOST:
             _too_large("dpc_gate")
         return ld, torch.float64 if logits.dtype == torch.float64 else torch.float32
@@ -59,14 +66,11 @@ class Gate:
             with _enter(dev, stream):
                 return self(logits)
         ld, wt = self._logits(logits, None)
-        bias = self.bias
-        if bias is not None:
-            _on(bias, dev, "bias")
-            bias = bias.data_ptr()
+        bias, spec = self._bias(dev), self.spec
         n, elem = logits.shape[0], _elem_of(logits.dtype)
-        shape = (n, max(self.topk, 0))
+        shape = (n, max(spec.topk, 0))
         expert, weight = logits.new_empty(shape, dtype=torch.int32), logits.new_empty(shape, dtype=wt)
-        _check(_lib.dpc_gate(_raw_stream(dev), elem, self._spec, n, logits.data_ptr(), ld, bias, expert.data_ptr(),
+        _check(_lib.dpc_gate(_raw_stream(dev), elem, spec, n, logits.data_ptr(), ld, bias, expert.data_ptr(),
                              weight.data_ptr()), "dpc_gate")
         return expert, weight
 
@@ -79,16 +83,16 @@ class Gate:
             with _enter(dev, stream):
                 return self.backward(logits, expert, dweight, out)
         ld, wt = self._logits(logits, None)
-        n, elem = logits.shape[0], _elem_of(logits.dtype)
+        n, elem, spec = logits.shape[0], _elem_of(logits.dtype), self.spec
         for name, t, dt in (("expert", expert, torch.int32), ("dweight", dweight, wt)):
-            if t.dtype != dt or t.shape != (n, self.topk) or not t.is_contiguous():
+            if t.dtype != dt or t.shape != (n, spec.topk) or not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous {dt} [tokens, topk]")
             _on(t, dev, name)
         if out is None:
-            out, ldo = logits.new_empty((n, self.nexpert)), self.nexpert
+            out, ldo = logits.new_empty((n, spec.nexpert)), spec.nexpert
         else:
-            ldo = _rows(out, "out", n, self.nexpert, logits.dtype, dev)
-        _check(_lib.dpc_gate_bwd(_raw_stream(dev), elem, self._spec, n, logits.data_ptr(), ld, expert.data_ptr(),
+            ldo = _rows(out, "out", n, spec.nexpert, logits.dtype, dev)
+        _check(_lib.dpc_gate_bwd(_raw_stream(dev), elem, spec, n, logits.data_ptr(), ld, expert.data_ptr(),
                                  dweight.data_ptr(), out.data_ptr(), ldo), "dpc_gate_bwd")
         return out
 

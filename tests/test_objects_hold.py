@@ -90,3 +90,53 @@ def test_an_embedding_sees_a_table_changed_in_place(calls):
     table.shape, table.dtype = (10, 6), F16
     emb(Tensor((4,), I32))
     assert calls[0][2] == B.DPC_ELEM_F16 and calls[0][4:6] == (10, 6) and calls[0][8] == 6
+
+
+BIAS = {"float64": lambda: Tensor((6,), F64), "shorter": lambda: Tensor((5,)), "a row": lambda: Tensor((1, 6)),
+        "in pieces": lambda: Rows((6,), contiguous=False), "on the CPU": lambda: torch.zeros(6)}
+
+
+@pytest.mark.parametrize("what", list(BIAS))
+def test_a_gate_refuses_a_bias_that_no_constructor_takes(calls, what):
+    gate = P.Gate(6, 2, bias=Tensor((6,)))
+    gate(Tensor((4, 6)))
+    gate.bias = None
+    gate(Tensor((4, 6)))
+    gate.bias = Tensor((6,))                        # a balancing step's new one
+    gate(Tensor((4, 6)))
+    assert len(calls) == 3
+    gate.bias = BIAS[what]()
+    with pytest.raises(ValueError, match="bias"):
+        gate(Tensor((4, 6)))
+    assert len(calls) == 3
+
+
+def test_a_gate_sees_a_bias_changed_in_place(calls):
+    gate = P.Gate(6, 2, bias=Tensor((6,)))
+    gate.bias.dtype = F16
+    with pytest.raises(ValueError, match="bias"):
+        gate(Tensor((4, 6)))
+    assert not calls
+
+
+def test_a_gate_allocates_what_the_library_is_told(calls):
+    """Outputs have the sizes that the specification has when the call is made."""
+    gate = P.Gate(6, 2)
+    gate.spec.topk = 5
+    expert, weight = gate(Tensor((4, 6)))
+    assert expert.shape == weight.shape == (4, 5) and (gate.nexpert, gate.topk) == (6, 5)
+    with pytest.raises(ValueError, match="expert"):
+        gate.backward(Tensor((4, 6)), Tensor((4, 2), I32), Tensor((4, 2)))
+    gate.spec.nexpert = 7
+    for call in (lambda: gate(Tensor((4, 6))), lambda: gate.backward(Tensor((4, 6)), Tensor((4, 5), I32), Tensor((4, 5)))):
+        with pytest.raises(ValueError, match="logits"):
+            call()
+    gate.spec = B.dpc_gate_spec(8, 3, B.DPC_SCORE_SOFTMAX, 1, 1, 1, 0, 1.0)
+    calls.clear()
+    assert gate(Tensor((4, 8)))[0].shape == (4, 3)
+    given = calls[0][3]
+    given = getattr(given, "_obj", given)           # by reference
+    assert (given.nexpert, given.topk) == (8, 3)
+    for name in ("nexpert", "topk"):
+        with pytest.raises(AttributeError):
+            setattr(gate, name, 2)
