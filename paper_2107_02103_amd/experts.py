@@ -7,6 +7,8 @@ gradient do not.  Gradients are calls of their own, named at each method.
 A call with few rows is over in microseconds, so these methods check what they
 are given once and call the library by address, without the checks of the
 binding's functions of the same names."""
+import operator
+
 import torch
 
 from . import binding as B
@@ -50,6 +52,22 @@ def _on(x, device, name):
         raise ValueError(f"{name} must be a tensor on a GPU device, not {x.device}")
     if device is not None and at != device:
         raise ValueError(f"{name} is on {x.device}, the others are on cuda:{device}")
+
+
+def _fixed(name):
+    """An attribute that stays what the constructor has checked: sizes and addresses
+    of later calls follow from it."""
+    return property(operator.attrgetter("_" + name))
+
+
+def _layer_bias(bias, shape, device):
+    """Address of the bias of layers, which may be another than the constructor's."""
+    if bias is None:
+        return None
+    if bias.dtype != torch.float32 or bias.shape != shape or not bias.is_contiguous():
+        raise ValueError("bias must be contiguous float32 [experts, outer]")
+    _on(bias, device, "bias")
+    return bias.data_ptr()
 
 
 def _enter(device, stream):

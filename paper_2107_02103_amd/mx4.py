@@ -4,7 +4,8 @@ libdpc.  No call is recorded for torch's autograd."""
 import torch
 
 from . import binding as B
-from .experts import (_MOST, _check, _current_device, _elem_of, _enter, _lib, _on, _raw_stream, _rows, _too_large)
+from .experts import (_MOST, _check, _current_device, _elem_of, _enter, _fixed, _layer_bias, _lib, _on, _raw_stream, _rows,
+                      _too_large)
 
 
 _U8 = torch.uint8
@@ -43,18 +44,21 @@ class Mx4Rows:
     """Rows in 4-bit floating-point codes with a power of two for every 32 columns.
 
     codes   uint8 [rows, mx4_ld(cols) / 2]: two columns in a byte
-    scales  uint8 [mx4_ld(cols) / 256, rows, 8]: exponents, plus 127"""
+    scales  uint8 [mx4_ld(cols) / 256, rows, 8]: exponents, plus 127
+    Both may be written into; others in their place take another object."""
+
+    codes, scales, cols = _fixed("codes"), _fixed("scales"), _fixed("cols")
 
     def __init__(self, codes, scales, cols):
-        self.cols = int(cols)
-        if self.cols < 1 or codes.dim() != 2:
+        self._cols = cols = int(cols)
+        if cols < 1 or codes.dim() != 2:
             raise ValueError("codes must be contiguous uint8 [rows, mx4_ld(cols) / 2]")
-        self._device, n, ld = codes.get_device(), codes.shape[0], B.mx4_ld(self.cols)
-        if n > _MOST or self.cols > _MOST:
+        self._device, n, ld = codes.get_device(), codes.shape[0], B.mx4_ld(cols)
+        if n > _MOST or cols > _MOST:
             _too_large("dpc_values_mx4")
         _bytes(codes, (n, ld // 2), "codes", None)
         _bytes(scales, (ld // 256, n, 8), "scales", self._device)
-        self.codes, self.scales = codes, scales
+        self._codes, self._scales = codes, scales
 
     @classmethod
     def from_rows(cls, x, stream=None):
@@ -64,8 +68,8 @@ class Mx4Rows:
             with _enter(dev, stream):
                 return cls.from_rows(x)
         r = cls.__new__(cls)
-        r.cols, r._device = x.shape[1], dev
-        r.codes, r.scales = _quantise(x, ldx, 1, x.shape[0], dev)
+        r._cols, r._device = x.shape[1], dev
+        r._codes, r._scales = _quantise(x, ldx, 1, x.shape[0], dev)
         return r
 
     def values(self, dtype=torch.float32, out=None, stream=None):
@@ -86,26 +90,26 @@ class Mx4Linear:
 
     codes   uint8 [experts, outer, mx4_ld(inner) / 2] (or [outer, ...] for one)
     scales  uint8 [experts, mx4_ld(inner) / 256, outer, 8]
-    bias    float32 [experts, outer] or None"""
+    bias    float32 [experts, outer] or None
+    All may be written into, and another bias may take the place of the first."""
+
+    codes, scales, inner, outer, experts = (_fixed(name) for name in ("codes", "scales", "inner", "outer", "experts"))
 
     def __init__(self, codes, scales, inner, bias=None):
         if codes.dim() == 2:
             codes, scales = codes[None], scales[None]
             bias = None if bias is None else bias[None]
-        self.inner = int(inner)
-        if codes.dim() != 3 or self.inner < 1:
+        self._inner = inner = int(inner)
+        if codes.dim() != 3 or inner < 1:
             raise ValueError("codes must be contiguous uint8 [experts, outer, mx4_ld(inner) / 2]")
-        self.experts, self.outer = codes.shape[:2]
-        if self.inner > _MOST or self.experts > _MOST or self.outer > _MOST:
+        self._experts, self._outer = experts, outer = codes.shape[:2]
+        if inner > _MOST or experts > _MOST or outer > _MOST:
             _too_large("dpc_linear_mx4")
-        ld, self._device = B.mx4_ld(self.inner), codes.get_device()
-        _bytes(codes, (self.experts, self.outer, ld // 2), "codes", None)
-        _bytes(scales, (self.experts, ld // 256, self.outer, 8), "scales", self._device)
-        if bias is not None:
-            if bias.dtype != torch.float32 or bias.shape != codes.shape[:2] or not bias.is_contiguous():
-                raise ValueError("bias must be contiguous float32 [experts, outer]")
-            _on(bias, self._device, "bias")
-        self.codes, self.scales, self.bias = codes, scales, bias
+        ld, self._device = B.mx4_ld(inner), codes.get_device()
+        _bytes(codes, (experts, outer, ld // 2), "codes", None)
+        _bytes(scales, (experts, ld // 256, outer, 8), "scales", self._device)
+        _layer_bias(bias, (experts, outer), self._device)
+        self._codes, self._scales, self.bias = codes, scales, bias
 
     @classmethod
     def from_weight(cls, weight, bias=None, stream=None):
@@ -129,8 +133,8 @@ class Mx4Linear:
         if stream is not None or _current_device() != self._device:
             with _enter(self._device, stream):
                 return self.weight(dtype)
-        return _values(self.codes, self.scales, self.experts, self.outer, self.inner, dtype, None, self._device).view(
-            self.experts, self.outer, self.inner)
+        return _values(self._codes, self._scales, self._experts, self._outer, self._inner, dtype, None, self._device).view(
+            self._experts, self._outer, self._inner)
 
     def __call__(self, x, route=None, offsets=None, dtype=None, out=None, stream=None):
         """y [tokens, outer] of x [tokens, inner], or of Mx4Rows (rows coded once for
@@ -145,11 +149,11 @@ class Mx4Linear:
         ntok, topk, rows = x.codes.shape[0] if coded else x.shape[0], 1, None
         if coded:
             _on(x.codes, dev, "x")
-            if x.cols != self.inner or (route is not None and ntok != route.ntok):
+            if x.cols != self._inner or (route is not None and ntok != route.ntok):
                 raise ValueError(f"x has {ntok} rows of {x.cols} columns, expected "
-                                 f"{'rows' if route is None else route.ntok} of {self.inner}")
+                                 f"{'rows' if route is None else route.ntok} of {self._inner}")
         else:
-            ldx = _rows(x, "x", None if route is None else route.ntok, self.inner, None, dev)
+            ldx = _rows(x, "x", None if route is None else route.ntok, self._inner, None, dev)
         if ntok > _MOST:
             _too_large("dpc_linear_mx4")
         if route is not None:
@@ -160,27 +164,27 @@ class Mx4Linear:
         if offsets is not None:
             if offsets.dtype != torch.int32 or not offsets.is_contiguous():
                 raise TypeError("offsets must be contiguous int32")
-            if len(offsets) != self.experts + 1:
-                raise ValueError(f"offsets for {len(offsets) - 1} experts, layers for {self.experts}")
+            if len(offsets) != self._experts + 1:
+                raise ValueError(f"offsets for {len(offsets) - 1} experts, layers for {self._experts}")
             _on(offsets, dev, "offsets")
             offsets = offsets.data_ptr()
-        elif self.experts != 1:
+        elif self._experts != 1:
             raise ValueError("layers of several experts need a route or offsets")
         if dtype is None:
             dtype = torch.float32 if coded else x.dtype
         if out is None:
-            out, ldy = self.codes.new_empty((ntok * topk, self.outer), dtype=dtype), self.outer
+            out, ldy = self._codes.new_empty((ntok * topk, self._outer), dtype=dtype), self._outer
         else:
-            ldy = _rows(out, "out", ntok * topk, self.outer, dtype, dev)
-        tail = (rows, offsets, self.codes.data_ptr(), self.scales.data_ptr(),
-                None if self.bias is None else self.bias.data_ptr())
+            ldy = _rows(out, "out", ntok * topk, self._outer, dtype, dev)
+        tail = (rows, offsets, self._codes.data_ptr(), self._scales.data_ptr(),
+                _layer_bias(self.bias, (self._experts, self._outer), dev))
         if coded:
-            _check(_lib.dpc_matmul_mx4(_raw_stream(dev), _elem_of(dtype), ntok, topk, self.outer, self.inner, self.experts,
+            _check(_lib.dpc_matmul_mx4(_raw_stream(dev), _elem_of(dtype), ntok, topk, self._outer, self._inner, self._experts,
                                        x.codes.data_ptr(), x.scales.data_ptr(), *tail, out.data_ptr(), ldy), "dpc_matmul_mx4")
             return out
-        nb = _lib.dpc_linear_mx4_workspace_bytes(ntok, self.inner)
-        ws = self.codes.new_empty(nb)
-        _check(_lib.dpc_linear_mx4(_raw_stream(dev), _elem_of(x.dtype), _elem_of(dtype), ntok, topk, self.outer, self.inner,
-                                   self.experts, x.data_ptr(), ldx, *tail, ws.data_ptr(), nb, out.data_ptr(), ldy),
+        nb = _lib.dpc_linear_mx4_workspace_bytes(ntok, self._inner)
+        ws = self._codes.new_empty(nb)
+        _check(_lib.dpc_linear_mx4(_raw_stream(dev), _elem_of(x.dtype), _elem_of(dtype), ntok, topk, self._outer, self._inner,
+                                   self._experts, x.data_ptr(), ldx, *tail, ws.data_ptr(), nb, out.data_ptr(), ldy),
                "dpc_linear_mx4")
         return out

@@ -31,6 +31,7 @@ class Rows(Tensor):
 def calls(monkeypatch):
     """The calls that reach the library, with their arguments."""
     import paper_2107_02103_amd.gate as G
+    import paper_2107_02103_amd.mx4 as M
     made, current = [], [GPU]
 
     @contextlib.contextmanager
@@ -50,7 +51,7 @@ def calls(monkeypatch):
                 return 0
             return call
 
-    for module in (G,):
+    for module in (G, M):
         monkeypatch.setattr(module, "_lib", Lib())
         monkeypatch.setattr(module, "_raw_stream", lambda d: 0)
         monkeypatch.setattr(module, "_current_device", lambda: current[0])
@@ -140,3 +141,60 @@ def test_a_gate_allocates_what_the_library_is_told(calls):
     for name in ("nexpert", "topk"):
         with pytest.raises(AttributeError):
             setattr(gate, name, 2)
+
+
+class Codes(Tensor):
+    """Codes and what is cut from them."""
+
+    def __getitem__(self, i):
+        return Codes(((1,) + self.shape) if i is None else self.shape[1:], self.dtype, self.gpu)
+
+    def new_empty(self, shape, dtype=None):
+        return Codes((shape,) if isinstance(shape, int) else shape, dtype or self.dtype, self.gpu)
+
+
+U8 = torch.uint8
+
+
+def _rows4():
+    return P.Mx4Rows(Codes((4, 128), U8), Codes((1, 4, 8), U8), 100)
+
+
+def _layer4():
+    return P.Mx4Linear(Codes((1, 5, 128), U8), Codes((1, 1, 5, 8), U8), 100, Tensor((1, 5)))
+
+
+def _refuses_others(made, names):
+    """Attributes that sizes and addresses of a call follow from cannot be exchanged one by one."""
+    for name in names:
+        before = getattr(made, name)
+        with pytest.raises(AttributeError):
+            setattr(made, name, before)
+        assert getattr(made, name) is before
+
+
+def test_rows_and_layers_of_4_bits_keep_their_codes(calls):
+    _refuses_others(_rows4(), ("codes", "scales", "cols"))
+    _refuses_others(P.Mx4Rows.from_rows(Codes((4, 100))), ("codes", "scales", "cols"))
+    _refuses_others(_layer4(), ("codes", "scales", "inner", "outer", "experts"))
+
+
+LAYER_BIAS = {"float64": lambda: Tensor((1, 5), F64), "longer": lambda: Tensor((1, 6)), "flat": lambda: Tensor((5,)),
+              "in pieces": lambda: Rows((1, 5), contiguous=False), "on the CPU": lambda: torch.zeros(1, 5),
+              "elsewhere": lambda: Tensor((1, 5), gpu=0)}
+
+
+@pytest.mark.parametrize("what", list(LAYER_BIAS))
+def test_a_layer_of_4_bits_refuses_a_bias_that_no_constructor_takes(calls, what):
+    layer = _layer4()
+    layer.bias = Tensor((1, 5))
+    layer(Tensor((4, 100)))
+    layer(_rows4())
+    layer.bias = None
+    layer(Tensor((4, 100)))
+    assert len(calls) == 3
+    layer.bias = LAYER_BIAS[what]()
+    for x in (Tensor((4, 100)), _rows4()):
+        with pytest.raises(ValueError, match="bias"):
+            layer(x)
+    assert len(calls) == 3
