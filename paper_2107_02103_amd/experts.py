@@ -91,9 +91,13 @@ class Route:
              empty rows at the end
     pos      int32 [tokens, topk]: row of each choice, -1 if it is dropped
 
+    The three may be written into; others in their place take another object.
+
     A call runs on the GPU of its tensors, whichever is current.
     stream: a torch stream of that GPU that the call runs on, and for which its
     outputs are allocated (default: the current one)."""
+
+    offsets, rows, pos, ntok, topk, nexpert = (_fixed(name) for name in ("offsets", "rows", "pos", "ntok", "topk", "nexpert"))
 
     def __init__(self, expert, nexpert, stream=None):
         if expert.dtype != torch.int32 or expert.dim() not in (1, 2) or not expert.is_contiguous():
@@ -103,19 +107,19 @@ class Route:
         if stream is not None or _current_device() != dev:
             with _enter(dev, stream):
                 return Route.__init__(self, expert, nexpert)
-        self.ntok, self.topk = expert.shape if expert.dim() == 2 else (expert.shape[0], 1)
-        self.nexpert = int(nexpert)
-        m, head = self.ntok * self.topk, max(self.nexpert, 0) + 1
-        if m > _MOST or abs(self.nexpert) > _MOST:
+        self._ntok, self._topk = expert.shape if expert.dim() == 2 else (expert.shape[0], 1)
+        self._nexpert = int(nexpert)
+        m, head = self._ntok * self._topk, max(self._nexpert, 0) + 1
+        if m > _MOST or abs(self._nexpert) > _MOST:
             _too_large("dpc_route_plan")
-        nb = _lib.dpc_route_workspace_bytes(self.ntok, self.topk, self.nexpert)
+        nb = _lib.dpc_route_workspace_bytes(self._ntok, self._topk, self._nexpert)
         # the three of the plan in one allocation
         buf = expert.new_empty(head + 2 * m)
         ws = expert.new_empty((nb + 3) // 4)
-        self.offsets, self.rows, pos = buf.split_with_sizes((head, m, m))
-        self.pos = pos.view(self.ntok, self.topk)
+        self._offsets, self._rows, pos = buf.split_with_sizes((head, m, m))
+        self._pos = pos.view(self._ntok, self._topk)
         first = buf.data_ptr()
-        _check(_lib.dpc_route_plan(_raw_stream(dev), self.ntok, self.topk, self.nexpert, expert.data_ptr(),
+        _check(_lib.dpc_route_plan(_raw_stream(dev), self._ntok, self._topk, self._nexpert, expert.data_ptr(),
                                    ws.data_ptr(), nb, first, first + 4 * head, first + 4 * (head + m)), "dpc_route_plan")
 
     @classmethod
@@ -129,10 +133,10 @@ class Route:
             if t.dtype != torch.int32 or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous int32 tensor")
             _on(t, r._device, name)
-        r.offsets, r.rows, r.pos = offsets, rows, pos
-        r.ntok, r.topk = pos.shape
-        r.nexpert = len(offsets) - 1
-        if r.ntok > _MOST or r.topk > _MOST or r.nexpert > _MOST:
+        r._offsets, r._rows, r._pos = offsets, rows, pos
+        r._ntok, r._topk = pos.shape
+        r._nexpert = len(offsets) - 1
+        if r._ntok > _MOST or r._topk > _MOST or r._nexpert > _MOST:
             _too_large("dpc_route_plan")
         return r
 
@@ -141,7 +145,7 @@ class Route:
         if weight is None:
             return None
         want = torch.float64 if x.dtype == torch.float64 else torch.float32
-        if weight.dtype != want or weight.shape != self.pos.shape or not weight.is_contiguous():
+        if weight.dtype != want or weight.shape != self._pos.shape or not weight.is_contiguous():
             raise ValueError(f"weight must be contiguous {want} [tokens, topk]")
         _on(weight, self._device, "weight")
         return weight.data_ptr()
@@ -152,16 +156,16 @@ class Route:
         if stream is not None or _current_device() != self._device:
             with _enter(self._device, stream):
                 return self.gather(x, weight, out)
-        dev, m = self._device, self.ntok * self.topk
-        ldx, width = _rows(x, "x", self.ntok, None, None, dev), x.shape[1]
+        dev, m = self._device, self._ntok * self._topk
+        ldx, width = _rows(x, "x", self._ntok, None, None, dev), x.shape[1]
         if width > _MOST:
             _too_large("dpc_route_gather")
         if out is None:
             out, ldy = x.new_empty((m, width)), width or 1
         else:
             ldy = _rows(out, "out", m, width, x.dtype, dev)
-        _check(_lib.dpc_route_gather(_raw_stream(dev), _elem_of(x.dtype), self.ntok, self.topk, width, x.data_ptr(), ldx,
-                                     self._weight(weight, x), self.rows.data_ptr(), self.pos.data_ptr(),
+        _check(_lib.dpc_route_gather(_raw_stream(dev), _elem_of(x.dtype), self._ntok, self._topk, width, x.data_ptr(), ldx,
+                                     self._weight(weight, x), self._rows.data_ptr(), self._pos.data_ptr(),
                                      out.data_ptr(), ldy), "dpc_route_gather")
         return out
 
@@ -172,15 +176,15 @@ class Route:
             with _enter(self._device, stream):
                 return self.combine(x, weight, out)
         dev = self._device
-        ldx, width = _rows(x, "rows", self.ntok * self.topk, None, None, dev), x.shape[1]
+        ldx, width = _rows(x, "rows", self._ntok * self._topk, None, None, dev), x.shape[1]
         if width > _MOST:
             _too_large("dpc_route_combine")
         if out is None:
-            out, ldy = x.new_empty((self.ntok, width)), width or 1
+            out, ldy = x.new_empty((self._ntok, width)), width or 1
         else:
-            ldy = _rows(out, "out", self.ntok, width, x.dtype, dev)
-        _check(_lib.dpc_route_combine(_raw_stream(dev), _elem_of(x.dtype), self.ntok, self.topk, width, x.data_ptr(), ldx,
-                                      self._weight(weight, x), self.pos.data_ptr(), out.data_ptr(), ldy),
+            ldy = _rows(out, "out", self._ntok, width, x.dtype, dev)
+        _check(_lib.dpc_route_combine(_raw_stream(dev), _elem_of(x.dtype), self._ntok, self._topk, width, x.data_ptr(), ldx,
+                                      self._weight(weight, x), self._pos.data_ptr(), out.data_ptr(), ldy),
                "dpc_route_combine")
         return out
 
@@ -190,18 +194,18 @@ class Route:
         if stream is not None or _current_device() != self._device:
             with _enter(self._device, stream):
                 return self.combine_backward(x, dy, weight, need_rows)
-        dev, m = self._device, self.ntok * self.topk
+        dev, m = self._device, self._ntok * self._topk
         ldx, width = _rows(x, "rows", m, None, None, dev), x.shape[1]
         if width > _MOST:
             _too_large("dpc_route_combine_bwd")
-        lddy = _rows(dy, "dy", self.ntok, width, x.dtype, dev)
+        lddy = _rows(dy, "dy", self._ntok, width, x.dtype, dev)
         w = self._weight(weight, x)
         if weight is None and not need_rows:
             return None, None
         dx = x.new_empty((m, width)) if need_rows else None
         dw = None if weight is None else weight.new_empty(weight.shape)
-        _check(_lib.dpc_route_combine_bwd(_raw_stream(dev), _elem_of(x.dtype), self.ntok, self.topk, width, x.data_ptr(),
-                                          ldx, w, self.rows.data_ptr(), self.pos.data_ptr(), dy.data_ptr(), lddy,
+        _check(_lib.dpc_route_combine_bwd(_raw_stream(dev), _elem_of(x.dtype), self._ntok, self._topk, width, x.data_ptr(),
+                                          ldx, w, self._rows.data_ptr(), self._pos.data_ptr(), dy.data_ptr(), lddy,
                                           None if dx is None else dx.data_ptr(), width or 1,
                                           None if dw is None else dw.data_ptr()), "dpc_route_combine_bwd")
         return dx, dw
@@ -216,28 +220,29 @@ class Int8Linear:
     W^T approximates the gradient in x; it is not the derivative of y.
 
     codes   int8 [experts, outer, i8_ld(inner)] (or [outer, ...] for one layer)
-    scales  float32 [experts, outer];  bias float32 [experts, outer] or None"""
+    scales  float32 [experts, outer];  bias float32 [experts, outer] or None
+    All may be written into, and another bias may take the place of the first."""
+
+    codes, scales, inner, outer, experts = (_fixed(name) for name in ("codes", "scales", "inner", "outer", "experts"))
 
     def __init__(self, codes, scales, inner, bias=None):
         if codes.dim() == 2:
             codes, scales = codes[None], scales[None]
             bias = None if bias is None else bias[None]
-        self.inner = int(inner)
+        self._inner = int(inner)
         shape = codes.shape
-        if len(shape) != 3 or codes.dtype != torch.int8 or shape[2] != B.i8_ld(self.inner) or not codes.is_contiguous():
+        if len(shape) != 3 or codes.dtype != torch.int8 or shape[2] != B.i8_ld(self._inner) or not codes.is_contiguous():
             raise ValueError("codes must be contiguous int8 [experts, outer, i8_ld(inner)]")
         self._device = codes.get_device()
         _on(codes, None, "codes")
-        self.experts, self.outer = shape[:2]
-        if self.inner > _MOST or self.experts > _MOST or self.outer > _MOST:
+        self._experts, self._outer = shape[:2]
+        if self._inner > _MOST or self._experts > _MOST or self._outer > _MOST:
             _too_large("dpc_linear_i8")
-        for name, t in (("scales", scales), ("bias", bias)):
-            if t is None:
-                continue
-            if t.dtype != torch.float32 or t.shape != shape[:2] or not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous float32 [experts, outer]")
-            _on(t, self._device, name)
-        self.codes, self.scales, self.bias = codes, scales, bias
+        if scales.dtype != torch.float32 or scales.shape != shape[:2] or not scales.is_contiguous():
+            raise ValueError("scales must be contiguous float32 [experts, outer]")
+        _on(scales, self._device, "scales")
+        _layer_bias(bias, shape[:2], self._device)
+        self._codes, self._scales, self.bias = codes, scales, bias
 
     @classmethod
     def from_weight(cls, weight, bias=None, stream=None):
@@ -271,7 +276,7 @@ class Int8Linear:
             with _enter(self._device, stream):
                 return self(x, route, offsets, dtype, out)
         dev = self._device
-        ldx = _rows(x, "x", None if route is None else route.ntok, self.inner, None, dev)
+        ldx = _rows(x, "x", None if route is None else route.ntok, self._inner, None, dev)
         ntok, topk, rows = x.shape[0], 1, None
         if ntok > _MOST:
             _too_large("dpc_linear_i8")
@@ -282,22 +287,22 @@ class Int8Linear:
         if offsets is not None:
             if offsets.dtype != torch.int32 or not offsets.is_contiguous():
                 raise TypeError("offsets must be contiguous int32")
-            if len(offsets) != self.experts + 1:
-                raise ValueError(f"offsets for {len(offsets) - 1} experts, layers for {self.experts}")
+            if len(offsets) != self._experts + 1:
+                raise ValueError(f"offsets for {len(offsets) - 1} experts, layers for {self._experts}")
             _on(offsets, dev, "offsets")
             offsets = offsets.data_ptr()
-        elif self.experts != 1:
+        elif self._experts != 1:
             raise ValueError("layers of several experts need a route or offsets")
         if dtype is None:
             dtype = x.dtype
         if out is None:
-            out, ldy = torch.empty((ntok * topk, self.outer), dtype=dtype, device=x.device), self.outer
+            out, ldy = torch.empty((ntok * topk, self._outer), dtype=dtype, device=x.device), self._outer
         else:
-            ldy = _rows(out, "out", ntok * topk, self.outer, dtype, dev)
-        nb = _lib.dpc_linear_i8_workspace_bytes(ntok, self.inner)
-        ws = self.codes.new_empty(nb)
-        _check(_lib.dpc_linear_i8(_raw_stream(dev), _elem_of(x.dtype), _elem_of(dtype), ntok, topk, self.outer,
-                                  self.inner, self.experts, x.data_ptr(), ldx, rows, offsets, self.codes.data_ptr(),
-                                  self.scales.data_ptr(), None if self.bias is None else self.bias.data_ptr(),
+            ldy = _rows(out, "out", ntok * topk, self._outer, dtype, dev)
+        nb = _lib.dpc_linear_i8_workspace_bytes(ntok, self._inner)
+        ws = self._codes.new_empty(nb)
+        _check(_lib.dpc_linear_i8(_raw_stream(dev), _elem_of(x.dtype), _elem_of(dtype), ntok, topk, self._outer,
+                                  self._inner, self._experts, x.data_ptr(), ldx, rows, offsets, self._codes.data_ptr(),
+                                  self._scales.data_ptr(), _layer_bias(self.bias, (self._experts, self._outer), dev),
                                   ws.data_ptr(), nb, out.data_ptr(), ldy), "dpc_linear_i8")
         return out

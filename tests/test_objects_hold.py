@@ -30,6 +30,7 @@ class Rows(Tensor):
 @pytest.fixture
 def calls(monkeypatch):
     """The calls that reach the library, with their arguments."""
+    import paper_2107_02103_amd.experts as E
     import paper_2107_02103_amd.gate as G
     import paper_2107_02103_amd.mx4 as M
     made, current = [], [GPU]
@@ -51,7 +52,7 @@ def calls(monkeypatch):
                 return 0
             return call
 
-    for module in (G, M):
+    for module in (E, G, M):
         monkeypatch.setattr(module, "_lib", Lib())
         monkeypatch.setattr(module, "_raw_stream", lambda d: 0)
         monkeypatch.setattr(module, "_current_device", lambda: current[0])
@@ -198,3 +199,30 @@ def test_a_layer_of_4_bits_refuses_a_bias_that_no_constructor_takes(calls, what)
         with pytest.raises(ValueError, match="bias"):
             layer(x)
     assert len(calls) == 3
+
+
+def test_a_route_keeps_its_plan(calls):
+    plan = Tensor((3,), I32), Tensor((8,), I32), Tensor((4, 2), I32)
+    for route in (P.Route.from_plan(*plan), P.Route(Tensor((4, 2), I32), 2)):
+        _refuses_others(route, ("offsets", "rows", "pos", "ntok", "topk", "nexpert"))
+        route.name = "mine"                         # what a program notes at a plan is its own matter
+
+
+def test_a_layer_of_8_bits_keeps_its_codes(calls):
+    layer = P.Int8Linear(Tensor((2, 5, 128), torch.int8), Tensor((2, 5)), 100, Tensor((2, 5)))
+    _refuses_others(layer, ("codes", "scales", "inner", "outer", "experts"))
+
+
+@pytest.mark.parametrize("what", list(LAYER_BIAS))
+def test_a_layer_of_8_bits_refuses_a_bias_that_no_constructor_takes(calls, what):
+    layer = P.Int8Linear(Tensor((1, 5, 128), torch.int8), Tensor((1, 5)), 100, Tensor((1, 5)))
+    out = Tensor((4, 5))
+    layer.bias = Tensor((1, 5))
+    layer(Tensor((4, 100)), out=out)
+    layer.bias = None
+    layer(Tensor((4, 100)), out=out)
+    assert len(calls) == 2
+    layer.bias = LAYER_BIAS[what]()
+    with pytest.raises(ValueError, match="bias"):
+        layer(Tensor((4, 100)), out=out)
+    assert len(calls) == 2
