@@ -117,15 +117,13 @@ class Embedding:
         self.table, self.scale = table, float(scale)
         self._read(table)
 
-    @staticmethod
-    def _read(table):
-        """Device, element type and row stride of a table, as it is now: a table may be
-        exchanged, or changed in place (as .data of a parameter is)."""
+    def _read(self, table):
+        """What a table is, its element type and the stride of its rows, checked."""
         ld, elem = _rows(table, "table"), _elem_of(table.dtype)
-        ids, width = table.shape
-        if ids > _MOST or width > _MOST:
+        if table.shape[0] > _MOST or table.shape[1] > _MOST:
             _too_large("dpc_embed")
-        return table.get_device(), elem, ld, ids, width
+        self._seen = seen = (table.shape, table.stride(), table.dtype, table.get_device()), elem, ld
+        return seen
 
     @property
     def ids(self):
@@ -137,14 +135,16 @@ class Embedding:
 
     def __call__(self, ids, out=None, stream=None):
         """[tokens, width] of ids int32 [tokens]."""
-        table = self.table
-        dev, elem, ld, nid, width = self._read(table)
+        table, seen = self.table, self._seen
+        dev = table.get_device()
+        if (table.shape, table.stride(), table.dtype, dev) != seen[0]:  # another one, or changed as .data of a parameter is
+            seen = self._read(table)
         if stream is not None or _current_device() != dev:
             with _enter(dev, stream):
                 return self(ids, out)
         if _ids(ids) != dev:
             _on(ids, dev, "ids")
-        n = ids.shape[0]
+        (nid, width), (_, elem, ld), n = table.shape, seen, ids.shape[0]
         if out is None:
             out, ldy = table.new_empty((n, width)), width or 1
         else:

@@ -85,6 +85,18 @@ def test_an_embedding_refuses_a_table_that_no_constructor_takes(calls):
     assert not calls
 
 
+def test_an_embedding_goes_on_after_a_refused_table(calls):
+    first = Rows((300, 64), gap=3)
+    emb, ids = P.Embedding(first), Tensor((4,), I32)
+    for table in (Rows((2 ** 32, 64), gap=9), Rows((300, 64), I32)):
+        emb.table = table
+        with pytest.raises((P.DpcError, TypeError)):
+            emb(ids)
+        emb.table = first
+        emb(ids)
+        assert calls.pop()[2:9:2] == (B.DPC_ELEM_F32, 300, 4096, 67) and not calls
+
+
 def test_an_embedding_sees_a_table_changed_in_place(calls):
     """As .data of a parameter is exchanged when its module goes to another type."""
     table = Rows((300, 64))
