@@ -2,7 +2,8 @@
 //
 // Lookup: a copy of rows with one product per element; the table of a few ids
 // stays in the caches, and the call is bound by what it writes: 1,048,576 float32 rows
-// of 240 for 3 ids 174 us (5.8 TB/s).
+// of 240 for 3 ids 174 us (5.8 TB/s).  A vocabulary's rows are read, too: 16,384 bfloat16
+// rows of 4,096 for 65,536 ids 54 us (a copy of the bytes 56), 131,072 of them 308 (335).
 //
 // Gradient: tokens are sorted by id (dpc_sort.h, up to 10 bits of the id a
 // pass), so that an id's tokens are a run of positions.  The positions are cut into

@@ -7,13 +7,26 @@
 // instructions for every score.  So it is made in float32 first, whose error is
 // bounded: where every two neighbours in the order of the best topk + 1 scores,
 // and the groups at the border, are further apart than that, the float64 order is
-// the same.  Where not (a token in 300 of 256 experts, or exact ties), the wavefront
-// does the token again in float64.  The weights are float64 arithmetic on the chosen.
+// the same.  Where not, the wavefront does the token again in float64, one token after
+// the other.  The weights are float64 arithmetic on the chosen.
 //
 // Bound by vector issue: 65,536 tokens of 256 bfloat16 scores, 8 of 256 chosen, from 4
-// of 8 groups, 36 us where a copy of the bytes takes 8; without groups 30, without
-// bias 22 (all float64: 88, a 16-lane float64 loop for the choice: 247).  One token
-// 3.2 us.  The gradient: 331,776 tokens of 3 float32 scores 5.7 us (13 MB).
+// of 8 groups, 36 us where a copy of the bytes takes 8; without groups 30, with neither
+// groups nor bias 22 (all float64: 88, a 16-lane float64 loop for the choice: 247).  One
+// token 3.2 us.  The gradient: 331,776 tokens of 3 float32 scores 5.7 us (13 MB); 65,536
+// of 256, 8 chosen, 50 to 58 in bfloat16 (a copy of the bytes 15) and 79 to 82 in float32
+// (29), of 1,024 274 to 296 (57), of 64 18 to 22 (4): elements are loaded and stored one
+// by one, and every slot is compared with all of a lane's experts.
+//
+// How many tokens float32 does not settle is up to the scores: under one in 100 of 256
+// experts with a bias of normally distributed numbers, all of them where scores tie or
+// all but tie, as without a bias in 16 bits and where sigmoids are near 1.  65,536
+// tokens, us:
+//   8 of 256, sigmoid, bias 0, logits of spread 1.5, 3, 5.4   float32 34 50 127, bfloat16 82 82 125
+//   the same from 4 of 8 groups                               float32 40 56 152, bfloat16 95 95 153
+//   16 of 1,024, softmax, spread 1.5; bias normal and 0       float32 167 254, bfloat16 191 490
+//   all scores equal, float32, without and with a bias        3 experts 47 79, 16 80 110, 256 106 145
+//                                       (scores that differ:  3 experts 8 8, 16 10 13, 256 38 55)
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -536,8 +549,9 @@ __global__ __launch_bounds__(kBlock) void gate_kernel(Gate g, const T* __restric
   }
 
   // Exactly, where that did not settle it: the whole wavefront does such tokens one
-  // by one.  (All of the wavefront's tokens at once takes as many registers as to cost
-  // the float32 code a third of its wavefronts.)
+  // by one, 64 at worst (equal scores of up to 16 experts).  (All of the wavefront's
+  // tokens at once takes as many registers as to cost the float32 code a third of its
+  // wavefronts.)
   double inverse = 1.0;
   if (!g.sigmoid && (!g.renorm || (sizeof(T) == 8 && !plain))) {  // the sum of all exponentials counts
     double sum = 0.0;

@@ -368,13 +368,15 @@ void launch_few(hipStream_t s, const Product& p, const TX* x, int64_t ldx, TY* y
 // 16 bytes, one block each; where each lies, place_of says.  The scales of a
 // row are 8 bytes in a row, of which a lane reads the two of its chunks.
 //
-// 8192 x 8192 x 8192 in 254 to 290 us (3.8 to 4.3e15 operations a second, the more the
-// cooler the card; random codes in registers alone 7.2e15), 32,768 rows for 16 experts'
-// 4096 x 4096 in 345 to 400.  Of 285 us the products alone take 196: the largest tile's
-// reads (1,024 clocks a step), loads (512) and products (2,048) overlap in part.  Tried without gain: reads in the
-// order of use one to three fragments ahead (287 to 292), the next half step's while
-// this one is multiplied (451: spills), four wavefronts of 128 x 128 (297), 64 x 128 (398),
-// workgroups that go on to their next tile with its first step under way (298: spills).
+// 8192 x 8192 x 8192 in 257 to 276 us late in a row of 3,000 (4.0 to 4.3e15 operations a
+// second; random codes in registers alone 7.2e15: 153 us), 269 to 374 in the first 23 of
+// a row, 274 to 298 one by one with pauses; 32,768 rows for 16 experts' 4096 x 4096 333
+// to 378 past the first 50, 364 to 486 in the first 23, 383 to 408 with pauses.  Of 285
+// us the products alone take 196: the largest tile's reads (1,024 clocks a step), loads
+// (512) and products (2,048) overlap in part.  Tried without gain: reads in the order of
+// use one to three fragments ahead (287 to 292), the next half step's while this one is
+// multiplied (451: spills), four wavefronts of 128 x 128 (297), 64 x 128 (398), workgroups
+// that go on to their next tile with its first step under way (298: spills).
 template <typename TY, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void product_tiled_kernel(Product p, int col_tiles, TY* __restrict__ y,
                                                                      int64_t ldy) {

@@ -32,7 +32,12 @@ namespace {
 // 6.9, 10.5; 9.5, 10.6; 14.8, 10.9).
 constexpr int kOneBlockSlots = 8192;
 constexpr int kMaxBlocks = 1024;
-constexpr int kSelfCounts = 16384;     // counts that every workgroup of the last launch reads, at most
+// Counts (one for each key and workgroup) up to which every workgroup of the last launch
+// adds them up for itself, which saves a launch and costs reads by the square of the
+// workgroups.  Plans, us, so and with the launch between:
+//   262,144 slots of 32 keys 13.1 14.3, of 64 15.6 15.1;  524,288 of 16 13.1 14.8, of 32 15.3 15.7, of 64 20.8 16.9
+//   1,048,576 of 2 12.0 15.8, of 8 15.1 17.8, of 16 18.1 18.4, of 32 24.5 19.8;  16,777,216 of 16 133 135
+constexpr int kSelfCounts = 16384;
 constexpr int kPlanWaves = 4;          // wavefronts of a workgroup of the three launches
 
 // Beyond, a workgroup takes a job's kPart slots at least.

@@ -25,7 +25,8 @@ class Gate:
     renormalise    the weights of a token are divided by their sum
     scale          factor of all weights
 
-    An expert whose logit is -infinity is closed to the token."""
+    An expert whose logit is -infinity is closed to the token; a token to which all
+    are goes nowhere (padding atoms: scores of 0 are scores like any other)."""
 
     def __init__(self, nexpert, topk, score="softmax", groups=1, keep=1, best=1, bias=None, renormalise=False, scale=1.0):
         if score not in _SCORES:
