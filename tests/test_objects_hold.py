@@ -1,6 +1,6 @@
 """What an object was given may be replaced or changed afterwards: a call goes by what
 is there when it is made, or refuses it.  Without a GPU: descriptions of tensors, and
-a recorder for a library."""
+a recorder for a library; one test has tensors on the GPU."""
 import contextlib
 
 import pytest
@@ -238,3 +238,33 @@ def test_a_layer_of_8_bits_refuses_a_bias_that_no_constructor_takes(calls, what)
     with pytest.raises(ValueError, match="bias"):
         layer(Tensor((4, 100)), out=out)
     assert len(calls) == 2
+
+
+@pytest.mark.gpu
+def test_exchanged_tensors_on_the_gpu():
+    """A table whose module goes to 16 bits, a shorter one, and other biases: results are those of new objects."""
+    g = torch.Generator("cuda").manual_seed(0)
+    normal = lambda *shape: torch.randn(*shape, device="cuda", generator=g)
+    ids = torch.tensor([0, 5, 2, -1, 7, 4], dtype=I32, device="cuda")
+    module = torch.nn.Embedding(6, 40, device="cuda")
+    emb = P.Embedding(module.weight, 0.5)
+    emb(ids)
+    module.half()
+    assert emb.table is module.weight and emb.table.dtype == F16
+    assert torch.equal(emb(ids), P.Embedding(module.weight.detach().clone(), 0.5)(ids)) and emb(ids).dtype == F16
+    emb.table = normal(3, 50)[:, :7]
+    assert torch.equal(emb(ids), P.Embedding(emb.table.clone(), 0.5)(ids))
+    assert not emb(ids)[1].any() and emb.backward(ids, normal(6, 7)).shape == (3, 7)      # id 5 is none of three
+    z, gate = normal(50, 12), P.Gate(12, 3, "sigmoid", bias=torch.zeros(12, device="cuda"))
+    gate(z)
+    gate.bias = normal(12)
+    for a, b in zip(gate(z), P.Gate(12, 3, "sigmoid", bias=gate.bias)(z)):
+        assert torch.equal(a, b)
+    w, x = normal(9, 70), normal(5, 70)
+    for kind in (P.Mx4Linear, P.Int8Linear):
+        layer = kind.from_weight(w, normal(9))
+        layer(x)
+        layer.bias = normal(1, 9)
+        assert torch.equal(layer(x), kind.from_weight(w, layer.bias[0])(x))
+        layer.bias = None
+        assert torch.equal(layer(x), kind.from_weight(w)(x))
